@@ -59,7 +59,7 @@ def listed():
         # a training step at 1024 x 1024 pixels
         dict(_gated(512 + 64 * 64, 2432, 6528, "silu", True), name="gated-train-1024"),
         # inference at 2048 x 2048 pixels with a short prompt, no row count a multiple of a tile
-        dict(_gated(333 + 128 * 128, 2432, 9728, "gelu", False), name="gated-image-2048"),
+        dict(_gated(333 + 128 * 128, 2432, 9728, "gelu_tanh", False), name="gated-image-2048"),
         # the norms and adapters of a small model: many tensors of a few hundred elements, launch bound
         dict(_adamw(2, 96, 250, "f32", 32, False, 7), name="adamw-small"),
         # the weights of four blocks in bf16 with fp32 masters and fp32 states
@@ -96,7 +96,7 @@ def _draw_once(rng):
                      rng.random() < 0.4, rng.random() < 0.6, rng.random() < 0.4)
     if op == "gated":
         M = rng.choice([1, rng.randint(2, 64)]) if rng.random() < 0.3 else _log_int(rng, 64, 16896)
-        return _gated(M, 8 * _log_int(rng, 32, 512), 8 * _log_int(rng, 64, 1408), rng.choice(["silu", "gelu"]), M > 64 and rng.random() < 0.5)
+        return _gated(M, 8 * _log_int(rng, 32, 512), 8 * _log_int(rng, 64, 1408), rng.choice(["silu", "gelu_tanh"]), M > 64 and rng.random() < 0.5)
     dtype = rng.choice(["f32", "bf16"])
     return _adamw(rng.randint(1, 8), _log_int(rng, 64, 2432), _log_int(rng, 100, 6528), dtype, rng.choice([32, 32, 8]), dtype == "bf16" and rng.random() < 0.5,
                   _log_int(rng, 1, 10000))
