@@ -4,4 +4,4 @@ Importing the package loads nothing; `paper_2412_16112_amd.clear_attn` opens the
 (and fails loudly if it has not been built), `paper_2412_16112_amd.inputs` holds the seeded
 synthetic-input recipes shared by the tests and the bench.
 """
-__all__ = ["clear_attn", "inputs"]
+__all__ = ["clear_attn", "clear_block", "inputs"]

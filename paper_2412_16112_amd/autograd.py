@@ -1,5 +1,5 @@
-"""torch.autograd entry point for the CLEAR local attention (argument marshalling only: forward and backward
-both run in the HIP library).
+"""torch.autograd entry points for the CLEAR local attention and for the operators around it - rotary, layer_norm, gated_ff -
+(argument marshalling only: forward and backward both run in the HIP library).
 
     from paper_2412_16112_amd.autograd import clear_attention
     O = clear_attention(Q, K, V, n_text=512, gridH=64, gridW=64, r=16)   # [B, H, N, 128] bf16, differentiable
@@ -12,6 +12,7 @@ a call that asks for gradients of fp32 tensors is refused in the forward pass, n
 import torch
 
 from . import clear_attn as ca
+from . import clear_block as cb
 
 MAX_CACHED_CONTEXTS = 16
 _contexts = {}  # insertion order = least recently used first
@@ -77,3 +78,80 @@ def clear_attention(Q, K, V, n_text, gridH, gridW, r, mask_kind=ca.CLEAR_MASK_DI
     """softmax(Q K^T / sqrt(d) under the CLEAR mask) V for [B, H, n_text + gridH*gridW, d] device tensors.
     mask_kind / shift select one of the compared local masks instead of the disc (clear_attn_create_masked)."""
     return ClearAttentionFunction.apply(Q, K, V, n_text, gridH, gridW, r, mask_kind, shift)
+
+
+# ---- the operators around the attention (clear_block) -------------------------------------------------------------------------
+
+class RotaryFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(fctx, q, k, positions, freqs, interleaved, scale):
+        fctx.save_for_backward(positions, freqs)
+        fctx.how = (interleaved, scale)
+        fctx.has_k = k is not None
+        return cb.rotary(q, k, positions, freqs, interleaved=interleaved, scale=scale)
+
+    @staticmethod
+    def backward(fctx, dq, dk):
+        positions, freqs = fctx.saved_tensors
+        interleaved, scale = fctx.how
+        fix = lambda t: t if t is None or t.stride(-1) == 1 else t.contiguous()
+        # (the transposed map: the negative angle, the same scale)
+        dq, dk = cb.rotary(fix(dq), fix(dk) if fctx.has_k else None, positions, freqs, interleaved=interleaved, scale=scale, inverse=True)
+        return dq, dk, None, None, None, None
+
+
+def rotary(q, k, positions, freqs, interleaved=True, scale=1.0):
+    """clear_block.rotary, differentiable in q and k (k may be None)."""
+    fix = lambda t: t if t is None or t.stride(-1) == 1 else t.contiguous()
+    return RotaryFunction.apply(fix(q), fix(k), positions, freqs, interleaved, scale)
+
+
+class LayerNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(fctx, x, weight, bias, eps, weight_offset):
+        if not any(fctx.needs_input_grad[:3]):
+            return cb.layer_norm(x, weight, bias, eps=eps, weight_offset=weight_offset)
+        y, stats = cb.layer_norm(x, weight, bias, eps=eps, weight_offset=weight_offset, save_stats=True)
+        fctx.save_for_backward(x, weight, bias, stats)
+        fctx.weight_offset = weight_offset
+        return y
+
+    @staticmethod
+    def backward(fctx, dy):
+        x, weight, bias, stats = fctx.saved_tensors
+        dx, dw, db = cb.layer_norm_backward(_rows_ok(dy), x, weight, bias, stats, weight_offset=fctx.weight_offset, need=fctx.needs_input_grad[:3])
+        return dx, dw, db, None, None
+
+
+def _rows_ok(t):
+    """t, or a contiguous copy where its rows are not evenly spaced or its channels not contiguous (an expanded gradient, say)."""
+    return t if t.stride(-1) == 1 and t.dim() in (2, 3) else t.contiguous()
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0):
+    """clear_block.layer_norm, differentiable in x, weight and bias."""
+    own = lambda t: t if t is None else t.contiguous()
+    return LayerNormFunction.apply(_rows_ok(x), own(weight), own(bias), eps, weight_offset)
+
+
+class GatedFFFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(fctx, x, w_gate, w_up, activation):
+        if not any(fctx.needs_input_grad[:3]):
+            return cb.gated_ff(x, w_gate, w_up, activation=activation)
+        h, pre = cb.gated_ff(x, w_gate, w_up, activation=activation, save_pre=True)
+        fctx.save_for_backward(x, w_gate, w_up, pre)
+        fctx.activation = activation
+        return h
+
+    @staticmethod
+    def backward(fctx, dh):
+        x, w_gate, w_up, pre = fctx.saved_tensors
+        need = fctx.needs_input_grad
+        dx, dg, du = cb.gated_ff_backward(dh.contiguous(), x, w_gate, w_up, pre, activation=fctx.activation, need=(need[0], need[1] or need[2]))
+        return dx, dg if need[1] else None, du if need[2] else None, None
+
+
+def gated_ff(x, w_gate, w_up, activation="silu"):
+    """clear_block.gated_ff, differentiable in x, w_gate and w_up."""
+    return GatedFFFunction.apply(x if x.dim() == 2 and x.stride(1) == 1 else x.contiguous(), w_gate, w_up, activation)

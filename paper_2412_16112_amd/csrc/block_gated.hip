@@ -1,0 +1,467 @@
+// The gated feed-forward projection H = act(X Wg^T) * (X Wu^T) and its gradients, on bf16 matrix instructions.
+//
+// Three products share one tile kernel: the fused forward product (both weights' tiles side by side, so that a lane ends up with
+// gate and up of the same outputs and the activation is an epilogue on registers), dX = dG Wg + dU Wu (the contraction runs through both
+// halves) and dWg = dG^T X, dWu = dU^T X.  Operand A is the one whose rows become the contiguous axis of the output, B gives its rows.
+// An operand is stored along the contraction ("rows": X and the weights forward, dG and dU for dX) or across it ("columns": the weights
+// for dX, everything for the weight gradients); the latter are read from LDS with the 16-bit transpose load.
+#include <algorithm>
+
+#include "block_internal.h"
+
+namespace clear {
+namespace block {
+namespace {
+
+constexpr int kStep = 64;  // of the contraction, a stage of LDS
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(4))) short short4v;
+typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_ptr;
+typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
+
+enum Kind { kForward, kInputGrad, kWeightGrad };
+
+// ---- buffer loads to LDS ------------------------------------------------------------------------------------------------
+// A buffer descriptor bounds a load: what lies at or past `bytes` reads as 0 and nothing past it is touched.
+__device__ __forceinline__ i32x4 buffer_of(const void* base, long long bytes)
+{
+    const unsigned long long b = (unsigned long long)base;
+    const int size = bytes < 0 ? 0 : (int)(bytes < 0x7fffffffLL ? bytes : 0x7fffffffLL);
+    return i32x4{__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32)), __builtin_amdgcn_readfirstlane(size), 0x00020000};
+}
+constexpr unsigned kOutside = 0x80000000u;  // an offset past every buffer
+// 16 bytes a lane from buffer + voff to LDS at lds + 16 * lane (lds: wave-uniform); counted by vmcnt.  The whole offset is in the vector register, which
+// the bounds check looks at.  The wait states that the compiler does not put into asm: one between the write of M0 and the load, five after a
+// vector instruction that wrote its descriptor.
+__device__ __forceinline__ void load_to_lds(const i32x4& buffer, unsigned voff, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buffer) : "memory", "m0");
+}
+
+// ---- a tile of ROWS rows (or columns) x kStep of the contraction in LDS, 128 ROWS bytes ---------------------------------------
+// Stored along the contraction: rows of 128 bytes, 16-byte chunk c of row r in slot c ^ (r & 7).  A load instruction fills 8 rows; the operand
+// read takes 16 bytes of 32 rows a half wave, 8 neighbouring lanes from 8 different slots.
+struct RowsTile {
+    __device__ __forceinline__ static unsigned load_offset(int lane, long long ld) { return (unsigned)((lane >> 3) * ld * 2 + (((lane & 7) ^ (lane >> 3)) << 4)); }
+    __device__ __forceinline__ static int chunk(int lane) { return (lane & 7) ^ (lane >> 3); }
+};
+// Stored across: kStep rows of 2 ROWS bytes; 32-byte granule g (16 columns) of contraction row k in slot g ^ spread(k & 3).  A load instruction
+// fills 1 KB, 2 or 4 contraction rows.  The transpose read takes, for 16 lanes, 32 bytes of 4 contraction rows: with the spread of 0, 5, 2, 7 these lie in
+// different banks, those of the neighbouring 16 lanes (the granule beside) too.
+__device__ __forceinline__ int spread(int k) { return (k & 3) ^ ((k & 1) << 2); }
+
+template <int KIND, int WA, int WB, int NB>
+struct Shape {
+    static constexpr int TA = 64 * WA, TB = 32 * NB * WB, WAVES = WA * WB, THREADS = 64 * WAVES;
+    static constexpr bool A_COLUMNS = KIND != kForward, B_COLUMNS = KIND == kWeightGrad;
+    static constexpr int A_BYTES = TA * 2 * kStep, B_BYTES = TB * 2 * kStep, STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
+    static constexpr int A_LOADS = TA / 8 / WAVES, B_LOADS = TB / 8 / WAVES;  // instructions a wave, 1 KB each
+    static_assert(TA / 8 % WAVES == 0 && TB / 8 % WAVES == 0, "the waves share the loads of a stage evenly");
+};
+
+struct TileArgs {
+    const __bf16 *a0, *a1, *b0, *b1;  // the operands, and the second of those that come in two
+    long long ld_a0, ld_a1, ld_b0, ld_b1;
+    int rows_a;          // extent of A's rows (the contiguous axis of the output)
+    long long rows_b;    // of B's rows
+    long long depth;     // the contraction (of each half)
+    int tiles_a, tiles_b, act;
+    __bf16 *out0, *out1;
+    long long ld_out0, ld_out1;
+    float* pre;
+};
+
+__device__ __forceinline__ float activation(float g, int act)
+{
+    if (act == CLEAR_ACT_SILU) return g / (1.f + __expf(-g));
+    if (act == CLEAR_ACT_GELU_TANH) {
+        // (1 + tanh z) / 2 = 1 / (1 + e^(-2 z))
+        const float z = 0.7978845608028654f * (g + 0.044715f * g * g * g);
+        return g / (1.f + __expf(-2.f * z));
+    }
+    return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
+}
+// act(g) and act'(g).
+__device__ __forceinline__ void activation_slope(float g, int act, float* value, float* slope)
+{
+    if (act == CLEAR_ACT_SILU) {
+        const float s = 1.f / (1.f + __expf(-g));
+        *value = g * s;
+        *slope = s + g * s * (1.f - s);
+    } else if (act == CLEAR_ACT_GELU_TANH) {
+        const float c = fabsf(g) > 30.f ? copysignf(30.f, g) : g;  // (s is 0 or 1 long before; a square that overflows would make 0 * inf of it)
+        const float z = 0.7978845608028654f * (c + 0.044715f * c * c * c);
+        const float s = 1.f / (1.f + __expf(-2.f * z));
+        *value = g * s;
+        *slope = s + 2.f * c * s * (1.f - s) * 0.7978845608028654f * (1.f + 3.f * 0.044715f * c * c);
+    } else {
+        const float s = 0.5f * (1.f + erff(g * 0.7071067811865476f));
+        *value = g * s;
+        *slope = s + g * 0.3989422804014327f * __expf(-0.5f * g * g);
+    }
+}
+
+template <int KIND, int WA, int WB, int NB>
+__global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
+{
+    typedef Shape<KIND, WA, WB, NB> S;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds_bytes[];
+    const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_bytes;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wa = wave % WA, wb = wave / WA;
+    const int tile_a = blockIdx.x % t.tiles_a, tile_b = blockIdx.x / t.tiles_a;
+
+    // origin of the tile; forward: the tile's A rows are TA / 2 rows of the gate weight and the same of the up weight;
+    // weight gradient: the first half of the tiles of B is dG's, the second dU's
+    const int half_tiles = KIND == kWeightGrad ? t.tiles_b / 2 : 0;
+    const bool second = KIND == kWeightGrad && tile_b >= half_tiles;
+    const int a_first = tile_a * (KIND == kForward ? S::TA / 2 : S::TA);
+    const long long b_first = (long long)(second ? tile_b - half_tiles : tile_b) * S::TB;
+    const int steps_each = (int)((t.depth + kStep - 1) / kStep), steps = KIND == kInputGrad ? 2 * steps_each : steps_each;
+
+    // ---- loads of a stage
+    constexpr int A_CHUNKS = S::TA / 8, B_CHUNKS = S::TB / 8;  // 16-byte chunks of a contraction row where an operand is stored across
+    auto issue = [&](int it) {
+        const unsigned to = lds + (it & 1) * S::STAGE;
+        const bool upper = KIND == kInputGrad && it >= steps_each;
+        const long long k0 = (long long)(upper ? it - steps_each : it) * kStep;
+        const long long k_left = t.depth - k0;
+        if (!S::A_COLUMNS) {
+            const int c = RowsTile::chunk(lane);
+            const bool in = c * 8 < k_left;
+#pragma unroll
+            for (int i = 0; i < S::A_LOADS; ++i) {
+                const int n = wave * S::A_LOADS + i;
+                const bool up = n >= S::TA / 16;  // (uniform)
+                const long long ld = up ? t.ld_a1 : t.ld_a0;
+                const long long rows = t.rows_a - a_first;
+                const i32x4 buf = buffer_of((up ? t.a1 : t.a0) + (long long)a_first * ld, ((min(rows, (long long)S::TA / 2) - 1) * ld + t.depth) * 2);
+                const unsigned at = (unsigned)((n - (up ? S::TA / 16 : 0)) * 8 * ld * 2 + k0 * 2);
+                load_to_lds(buf, in ? RowsTile::load_offset(lane, ld) + at : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
+            }
+        } else {
+            const __bf16* const p = upper ? t.a1 : t.a0;
+            const long long ld = upper ? t.ld_a1 : t.ld_a0;
+            const i32x4 buf = buffer_of(p + k0 * ld + a_first, ((min(k_left, (long long)kStep) - 1) * ld + t.rows_a - a_first) * 2);
+            constexpr int EACH = 64 / A_CHUNKS;  // contraction rows an instruction
+#pragma unroll
+            for (int i = 0; i < S::A_LOADS; ++i) {
+                const int n = wave * S::A_LOADS + i, k = n * EACH + lane / A_CHUNKS, slot = lane % A_CHUNKS;
+                const int c = ((slot >> 1) ^ spread(k)) << 1 | (slot & 1);
+                const unsigned off = (unsigned)(k * ld * 2 + c * 16);
+                load_to_lds(buf, a_first + c * 8 < t.rows_a ? off : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
+            }
+        }
+        const unsigned to_b = to + S::A_BYTES;
+        const __bf16* const p = upper || second ? t.b1 : t.b0;
+        const long long ld = upper || second ? t.ld_b1 : t.ld_b0;
+        if (!S::B_COLUMNS) {
+            const int c = RowsTile::chunk(lane);
+            const bool in = c * 8 < k_left;
+            const long long rows = t.rows_b - b_first;
+            const i32x4 buf = buffer_of(p + b_first * ld, ((min(rows, (long long)S::TB) - 1) * ld + t.depth) * 2);
+#pragma unroll
+            for (int i = 0; i < S::B_LOADS; ++i) {
+                const int n = wave * S::B_LOADS + i;
+                load_to_lds(buf, in ? RowsTile::load_offset(lane, ld) + (unsigned)(n * 8 * ld * 2 + k0 * 2) : kOutside, __builtin_amdgcn_readfirstlane(to_b + n * 1024));
+            }
+        } else {
+            const i32x4 buf = buffer_of(p + k0 * ld + b_first, ((min(k_left, (long long)kStep) - 1) * ld + t.rows_b - b_first) * 2);
+            constexpr int EACH = 64 / B_CHUNKS;
+#pragma unroll
+            for (int i = 0; i < S::B_LOADS; ++i) {
+                const int n = wave * S::B_LOADS + i, k = n * EACH + lane / B_CHUNKS, slot = lane % B_CHUNKS;
+                const int c = ((slot >> 1) ^ spread(k)) << 1 | (slot & 1);
+                const unsigned off = (unsigned)(k * ld * 2 + c * 16);
+                load_to_lds(buf, b_first + c * 8 < t.rows_b ? off : kOutside, __builtin_amdgcn_readfirstlane(to_b + n * 1024));
+            }
+        }
+    };
+
+    // ---- operand reads: 32 rows (columns) from `first` of the tile on, 16 s .. 16 s + 15 of the stage's contraction; lane l has row l % 32 and
+    // elements 8 (l / 32) .. + 7 of them
+    auto rows_address = [&](int first) { return (unsigned)((first + (lane & 31)) * 128 + (((lane >> 5) ^ (lane & 7)) << 4)); };
+    auto read_rows = [&](unsigned base, int s) { return *(lds_bf16x8_ptr)(size_t)(base ^ (unsigned)(s << 5)); };
+    auto columns_address = [&](int first, int row_bytes) {
+        const int j = lane & 15, k = 8 * (lane >> 5) + (j >> 2);
+        return (unsigned)(k * row_bytes + ((((first >> 4) + ((lane >> 4) & 1)) ^ spread(j >> 2)) << 5) + 8 * (j & 3));
+    };
+    auto read_columns = [&](unsigned base, int s, int row_bytes) {
+        union {
+            struct {
+                short4v lo, hi;
+            } h;
+            bf16x8 v;
+        } u;
+        u.h.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(size_t)(base + (unsigned)(16 * s * row_bytes)));
+        u.h.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(size_t)(base + (unsigned)((16 * s + 4) * row_bytes)));
+        return u.v;
+    };
+    unsigned a_at[2], b_at[NB];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int first = KIND == kForward ? 32 * wa + i * (S::TA / 2) : 64 * wa + 32 * i;
+        a_at[i] = lds + (S::A_COLUMNS ? columns_address(first, 2 * S::TA) : rows_address(first));
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int first = 32 * (NB * wb + i);
+        b_at[i] = lds + S::A_BYTES + (S::B_COLUMNS ? columns_address(first, 2 * S::TB) : rows_address(first));
+    }
+
+    f32x16 acc[2][NB];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+    if (steps > 0) issue(0);
+    for (int it = 0; it < steps; ++it) {
+        // this wave's loads of the stage have arrived and its reads of the other one are done; after the barrier everybody's
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (it + 1 < steps) issue(it + 1);
+        const unsigned stage = (it & 1) * S::STAGE;
+#pragma unroll
+        for (int s = 0; s < kStep / 16; ++s) {
+            bf16x8 a[2], b[NB];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) a[i] = S::A_COLUMNS ? read_columns(a_at[i] + stage, s, 2 * S::TA) : read_rows(a_at[i] + stage, s);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) b[j] = S::B_COLUMNS ? read_columns(b_at[j] + stage, s, 2 * S::TB) : read_rows(b_at[j] + stage, s);
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+        }
+    }
+
+    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const long long row = b_first + 32 * (NB * wb + j) + (lane & 31);
+        if (row >= t.rows_b) continue;
+        if (KIND == kForward) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int f = a_first + 32 * wa + 8 * q + 4 * (lane >> 5);
+                if (f >= t.rows_a) continue;
+                bf16x4 o;
+                f32x4 g, u;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    g[r] = acc[0][j][4 * q + r];
+                    u[r] = acc[1][j][4 * q + r];
+                    o[r] = (__bf16)(activation(g[r], t.act) * u[r]);
+                }
+                *(bf16x4*)(t.out0 + row * t.ld_out0 + f) = o;
+                if (t.pre) {
+                    *(f32x4*)(t.pre + row * t.rows_a + f) = g;
+                    *(f32x4*)(t.pre + (t.rows_b + row) * t.rows_a + f) = u;
+                }
+            }
+        } else {
+            __bf16* const out = (second ? t.out1 : t.out0) + row * (second ? t.ld_out1 : t.ld_out0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = a_first + 64 * wa + 32 * i + 8 * q + 4 * (lane >> 5);
+                    if (c >= t.rows_a) continue;
+                    bf16x4 o;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[r] = (__bf16)acc[i][j][4 * q + r];
+                    *(bf16x4*)(out + c) = o;
+                }
+        }
+    }
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------------------------
+// Up to 16 MT tokens: bound by the one reading of the weights.  A workgroup takes 16 hidden channels (gate and up) and all of the contraction,
+// its 8 waves every eighth 32 of it: weights go straight from memory to the operand registers (no other wave needs them), X comes from the caches.  The
+// waves' sums are added in order in LDS.
+constexpr int kFewWaves = 8;
+template <int MT>
+__global__ void __launch_bounds__(64 * kFewWaves) few_tokens_kernel(const GatedArgs g)
+{
+    __shared__ f32x4 part[kFewWaves][2 * MT][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, C = g.channels;
+    const int f0 = blockIdx.x * 16;
+    const int f = min(f0 + (lane & 15), g.hidden - 1), sub = 8 * (lane >> 4);
+    const __bf16* const wg = (const __bf16*)g.wg + f * g.ld_g + sub;
+    const __bf16* const wu = (const __bf16*)g.wu + f * g.ld_u + sub;
+    const __bf16* x[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x[m] = (const __bf16*)g.x + min((long long)(16 * m + (lane & 15)), g.tokens - 1) * g.ld_x + sub;
+    f32x4 acc[2][MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[0][m] = acc[1][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bf16x8 zero = {};
+    constexpr int AHEAD = MT > 2 ? 2 : 4;  // pieces whose loads are in flight together
+    for (int k0 = 32 * wave; k0 < C; k0 += 32 * kFewWaves * AHEAD) {
+        bf16x8 a[AHEAD], b[AHEAD], v[AHEAD][MT];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int k = k0 + 32 * kFewWaves * i;
+            const bool in = k + sub < C;  // (channels come in eights)
+            a[i] = in ? *(const bf16x8*)(wg + k) : zero;
+            b[i] = in ? *(const bf16x8*)(wu + k) : zero;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) v[i][m] = in ? *(const bf16x8*)(x[m] + k) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                acc[0][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], v[i][m], acc[0][m], 0, 0, 0);
+                acc[1][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[i], v[i][m], acc[1][m], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        part[wave][m][lane] = acc[0][m];
+        part[wave][MT + m][lane] = acc[1][m];
+    }
+    __syncthreads();
+    // register r of lane l: hidden channel 4 (l / 16) + r, token l % 16
+    for (int at = threadIdx.x; at < MT * 64; at += 64 * kFewWaves) {
+        const int m = at >> 6, l = at & 63;
+        f32x4 a = part[0][m][l], u = part[0][MT + m][l];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) {
+            a += part[w][m][l];
+            u += part[w][MT + m][l];
+        }
+        const long long token = 16 * m + (l & 15);
+        const int c = f0 + 4 * (l >> 4);
+        if (token < g.tokens && c < g.hidden) {
+            bf16x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = (__bf16)(activation(a[r], g.act) * u[r]);
+            *(bf16x4*)((__bf16*)g.h + token * g.ld_h + c) = o;
+            if (g.pre) {
+                *(f32x4*)(g.pre + token * g.hidden + c) = a;
+                *(f32x4*)(g.pre + (g.tokens + token) * g.hidden + c) = u;
+            }
+        }
+    }
+}
+
+// dG = dH u act'(g) and dU = dH act(g) in bf16 [2][tokens][hidden], 8 channels a thread.
+__global__ void __launch_bounds__(256) gated_gradient_kernel(const GatedArgs g, long long n)
+{
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= n) return;
+    const int each = g.hidden / 8;
+    const long long row = id / each;
+    const int c = (int)(id - row * each) * 8;
+    const bf16x8 dh = *(const bf16x8*)((const __bf16*)g.dh + row * g.ld_dh + c);
+    const long long at = row * g.hidden + c, plane = g.tokens * g.hidden;
+    f32x4 gate[2], up[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        gate[i] = *(const f32x4*)(g.pre + at + 4 * i);
+        up[i] = *(const f32x4*)(g.pre + plane + at + 4 * i);
+    }
+    bf16x8 dg, du;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float value, slope;
+        activation_slope(gate[j >> 2][j & 3], g.act, &value, &slope);
+        dg[j] = (__bf16)((float)dh[j] * up[j >> 2][j & 3] * slope);
+        du[j] = (__bf16)((float)dh[j] * value);
+    }
+    __bf16* const ws = (__bf16*)g.ws;
+    *(bf16x8*)(ws + at) = dg;
+    *(bf16x8*)(ws + plane + at) = du;
+}
+
+template <int KIND, int WA, int WB, int NB>
+hipError_t launch_tiles(TileArgs t, hipStream_t stream)
+{
+    typedef Shape<KIND, WA, WB, NB> S;
+    const int a_rows = KIND == kForward ? S::TA / 2 : S::TA;
+    t.tiles_a = (t.rows_a + a_rows - 1) / a_rows;
+    const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB * (KIND == kWeightGrad ? 2 : 1);
+    if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffffffffLL / S::THREADS) return hipErrorInvalidValue;
+    t.tiles_b = (int)tiles_b;
+    static const hipError_t limit =
+        hipFuncSetAttribute((const void*)tile_kernel<KIND, WA, WB, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    if (limit != hipSuccess) return limit;
+    tile_kernel<KIND, WA, WB, NB><<<dim3((unsigned)(tiles_b * t.tiles_a)), dim3(S::THREADS), S::LDS, stream>>>(t);
+    return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t launch_shape(const TileArgs& t, hipStream_t stream)
+{
+    const long long tiles = (t.rows_a + 255) / 256 * ((t.rows_b + 255) / 256) * (KIND == kInputGrad ? 1 : 2);
+    return tiles >= 192 ? launch_tiles<KIND, 4, 2, 4>(t, stream) : launch_tiles<KIND, 2, 2, 2>(t, stream);
+}
+
+constexpr int kFewTokens = 64;
+
+}  // namespace
+
+hipError_t launch_gated_forward(const GatedArgs& a, hipStream_t stream)
+{
+    if (a.tokens <= kFewTokens) {
+        const dim3 grid((a.hidden + 15) / 16), block(64 * kFewWaves);
+        if (a.tokens <= 16) few_tokens_kernel<1><<<grid, block, 0, stream>>>(a);
+        else if (a.tokens <= 32) few_tokens_kernel<2><<<grid, block, 0, stream>>>(a);
+        else few_tokens_kernel<4><<<grid, block, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    TileArgs t = {};
+    t.a0 = (const __bf16*)a.wg, t.a1 = (const __bf16*)a.wu, t.b0 = (const __bf16*)a.x;
+    t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = a.ld_x;
+    t.rows_a = a.hidden, t.rows_b = a.tokens, t.depth = a.channels;
+    t.act = a.act;
+    t.out0 = (__bf16*)a.h, t.ld_out0 = a.ld_h;
+    t.pre = a.pre;
+    return launch_shape<kForward>(t, stream);
+}
+
+size_t gated_workspace_bytes(long long tokens, int channels, int hidden)
+{
+    (void)channels;
+    return (size_t)tokens * hidden * 4;  // dG and dU
+}
+
+hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
+{
+    const __bf16* const dg = (const __bf16*)a.ws;
+    const __bf16* const du = dg + a.tokens * a.hidden;
+    hipError_t e = hipSuccess;
+    if (a.tokens > 0) {
+        const long long n = a.tokens * (a.hidden / 8), blocks = (n + 255) / 256;
+        if (blocks > 0xffffffffLL / 256) return hipErrorInvalidValue;
+        gated_gradient_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, n);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && a.dx && a.tokens > 0) {
+        TileArgs t = {};
+        t.a0 = (const __bf16*)a.wg, t.a1 = (const __bf16*)a.wu, t.b0 = dg, t.b1 = du;
+        t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = t.ld_b1 = a.hidden;
+        t.rows_a = a.channels, t.rows_b = a.tokens, t.depth = a.hidden;
+        t.out0 = (__bf16*)a.dx, t.ld_out0 = a.ld_dx;
+        e = launch_shape<kInputGrad>(t, stream);
+    }
+    if (e == hipSuccess && a.dwg) {
+        TileArgs t = {};
+        t.a0 = (const __bf16*)a.x, t.b0 = dg, t.b1 = du;
+        t.ld_a0 = a.ld_x, t.ld_b0 = t.ld_b1 = a.hidden;
+        t.rows_a = a.channels, t.rows_b = a.hidden, t.depth = a.tokens;
+        t.out0 = (__bf16*)a.dwg, t.ld_out0 = a.ld_dwg;
+        t.out1 = (__bf16*)a.dwu, t.ld_out1 = a.ld_dwu;
+        e = launch_shape<kWeightGrad>(t, stream);
+    }
+    return e;
+}
+
+}  // namespace block
+}  // namespace clear

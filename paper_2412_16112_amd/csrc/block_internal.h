@@ -1,0 +1,145 @@
+// Launchers of the operators around the attention (block_api.cpp calls them with checked arguments) and the vector types
+// that their kernels share.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "../../include/clear_block.h"
+
+namespace clear {
+namespace block {
+
+// ---- rotary positions
+struct RotaryArgs {
+    const void *q, *k;
+    void *q_out, *k_out;
+    int Hq, Hk;
+    long long st[12];  // (batch, head, token) of q, q_out, k, k_out
+    long long B, N;
+    int head_dim, rot_dim, copy;  // copy: the channels from rot_dim on are copied
+    const void* positions;
+    long long ps[3];
+    int n_axes;
+    const double* freqs;
+    float scale, sign;
+};
+hipError_t launch_rotary(const RotaryArgs& a, bool interleaved, bool wide_positions, int dtype, hipStream_t stream);
+
+// ---- layer norm
+constexpr int kNormMaxChannels = 16384;
+struct NormArgs {
+    const void *x, *w, *b, *dy;
+    void *y, *dx, *dw, *db;
+    float *stats, *ws;
+    int groups, rows, channels;
+    long long st[6];  // forward: (group, row) of x, y; backward: of dy, x, dx
+    int per_group;
+    float eps, offset;
+};
+hipError_t launch_norm_forward(const NormArgs& a, int dtype, int weight_dtype, hipStream_t stream);
+hipError_t launch_norm_backward(const NormArgs& a, int dtype, int weight_dtype, hipStream_t stream);
+int norm_partials(long long groups, long long rows, int channels, int per_group);  // workgroups whose sums of d_weight and d_bias a set is joined from
+
+// ---- gated feed-forward projection
+struct GatedArgs {
+    const void *x, *wg, *wu, *dh;
+    void *h, *dx, *dwg, *dwu;
+    float* pre;
+    long long tokens;
+    int channels, hidden, act;
+    long long ld_x, ld_g, ld_u, ld_h, ld_dh, ld_dx, ld_dwg, ld_dwu;
+    void* ws;
+};
+hipError_t launch_gated_forward(const GatedArgs& a, hipStream_t stream);
+hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream);
+size_t gated_workspace_bytes(long long tokens, int channels, int hidden);
+
+// ---- AdamW
+constexpr int kAdamTensors = 48;  // descriptors that fit the 4 KB of a launch's arguments
+constexpr int kAdamBlock = 256;   // elements that share a scale of 8-bit states
+struct AdamHyper {
+    float beta1, one_minus_beta1, beta2, one_minus_beta2, keep, step_size, inv_root_correction, eps;
+    const float* grad_scale;
+};
+hipError_t launch_adamw(int n, const clear_block_adamw_tensor* tensors, const AdamHyper& h, int dtype, int state_bits, hipStream_t stream);
+hipError_t launch_adamw_decode(const void* m, const float* ms, const void* v, const float* vs, float* m_out, float* v_out, long long n,
+                               hipStream_t stream);
+
+// ---- device types.  Callers' tensors need the alignment of their elements only: global memory takes a wide access at any
+// address, and the types say so to the compiler.
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8), aligned(2))) __bf16 bf16x8_any;
+typedef __attribute__((ext_vector_type(4), aligned(2))) __bf16 bf16x4_any;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
+
+// 8 consecutive elements, of which the first n (>= 8: all) exist; those that do not are 0 / are not written.
+template <typename T>
+struct Chunk8;
+template <>
+struct Chunk8<__bf16> {
+    bf16x8 v;
+    __device__ __forceinline__ void load(const __bf16* p, int n)
+    {
+        if (n >= 8) {
+            v = *(const bf16x8_any*)p;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (__bf16)0.f;
+        }
+    }
+    __device__ __forceinline__ float get(int j) const { return (float)v[j]; }
+    static __device__ __forceinline__ void store(__bf16* p, int n, const float (&x)[8])
+    {
+        bf16x8 o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (__bf16)x[j];
+        if (n >= 8) {
+            *(bf16x8_any*)p = o;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) p[j] = o[j];
+        }
+    }
+};
+template <>
+struct Chunk8<float> {
+    f32x4 lo, hi;
+    __device__ __forceinline__ void load(const float* p, int n)
+    {
+        if (n >= 8) {
+            lo = *(const f32x4_any*)p;
+            hi = *(const f32x4_any*)(p + 4);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lo[j] = j < n ? p[j] : 0.f;
+                hi[j] = 4 + j < n ? p[4 + j] : 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int j) const { return j < 4 ? lo[j & 3] : hi[j & 3]; }
+    static __device__ __forceinline__ void store(float* p, int n, const float (&x)[8])
+    {
+        if (n >= 8) {
+            *(f32x4_any*)p = f32x4{x[0], x[1], x[2], x[3]};
+            *(f32x4_any*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) p[j] = x[j];
+        }
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+}  // namespace block
+}  // namespace clear

@@ -1,0 +1,307 @@
+// Layer norm over the last axis and its backward pass.  Memory-bound: a row is read once and kept in registers between its
+// mean, its variance (of the differences from the mean) and its result; the backward pass reads dy and x once for dX and both
+// weight sums.
+//
+// A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ...: 16 bytes a lane
+// side by side (bf16), any alignment.  Forward, rows of up to 4096 channels take one wave (sums by lane exchange, no barrier), longer ones 4 or 8; backward,
+// where a lane also holds two sums for each of its channels, a wave holds up to 1536 channels and longer rows take 2, 4 or 8 (with 5 chunks a lane
+// the registers no longer suffice).
+#include <algorithm>
+#include <type_traits>
+
+#include "block_internal.h"
+
+namespace clear {
+namespace block {
+namespace {
+
+constexpr int kThreads = 512;
+
+// Sum over a team.  `slots`: LDS floats of the workgroup, one for each wave; every wave of the workgroup calls it.
+template <int TEAM>
+__device__ __forceinline__ float team_sum(float x, float* slots, int wave)
+{
+    x = wave_sum(x);
+    if (TEAM == 1) return x;
+    if ((threadIdx.x & 63) == 0) slots[wave] = x;
+    __syncthreads();
+    float s = 0.f;
+    const int first = wave / TEAM * TEAM;
+#pragma unroll
+    for (int i = 0; i < TEAM; ++i) s += slots[first + i];
+    __syncthreads();
+    return s;
+}
+
+template <typename T, typename TW, int TEAM, int CH>
+__global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
+{
+    constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
+    __shared__ float slots[WAVES];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM);
+    const long long total = (long long)a.groups * a.rows;
+    const long long row = (long long)blockIdx.x * TEAMS + wave / TEAM;
+    const bool live = row < total;
+    const int at = live ? (int)row : 0;
+    const int g = at / a.rows, r = at - g * a.rows;
+    const T* const x = (const T*)a.x + g * a.st[0] + r * a.st[1];
+    const int C = a.channels;
+    Chunk8<T> v[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = 8 * (lane + 64 * TEAM * i);
+        v[i].load(x + c, C - c);
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[i].get(j);  // (channels past the end are 0)
+    const float mean = team_sum<TEAM>(s, slots, wave) / (float)C;
+    float q = 0.f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = 8 * (lane + 64 * TEAM * i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = v[i].get(j) - mean;
+            q += c + j < C ? d * d : 0.f;
+        }
+    }
+    const float rstd = 1.0f / sqrtf(team_sum<TEAM>(q, slots, wave) / (float)C + a.eps);
+    if (!live) return;
+    if (a.stats && lane == 0) {
+        a.stats[row] = mean;
+        a.stats[total + row] = rstd;
+    }
+    const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)g * C : 0) : nullptr;
+    const TW* const b = a.b ? (const TW*)a.b + (a.per_group ? (long long)g * C : 0) : nullptr;
+    T* const y = (T*)a.y + g * a.st[2] + r * a.st[3];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = 8 * (lane + 64 * TEAM * i);
+        if (c >= C) break;
+        Chunk8<TW> cw, cb;
+        if (w) cw.load(w + c, C - c);
+        if (b) cb.load(b + c, C - c);
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            o[j] = (v[i].get(j) - mean) * rstd;
+            if (w) o[j] *= a.offset + cw.get(j);
+            if (b) o[j] += cb.get(j);
+        }
+        Chunk8<T>::store(y + c, C - c, o);
+    }
+}
+
+// Workgroup (p, set) of the grid takes rows p TEAMS + team, then every gridDim.x TEAMS further ones, of the set (a group, or everything when the weight
+// is shared), writes their dX and adds up dy xhat and dy in registers; the teams' sums are added in order and become partial p of the set.
+template <typename T, typename TW, int TEAM, int CH>
+__global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
+{
+    constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
+    extern __shared__ float lds[];  // [2][channels] where a workgroup has several teams
+    __shared__ float slots[WAVES];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM), team = wave / TEAM;
+    const int C = a.channels, set = blockIdx.y;
+    const long long in_set = a.per_group ? a.rows : (long long)a.groups * a.rows;
+    const long long first = a.per_group ? (long long)set * a.rows : 0;
+    const long long total = (long long)a.groups * a.rows;
+    const bool sums = a.dw || a.db;
+    const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)set * C : 0) : nullptr;
+    Chunk8<TW> cw[CH];
+    if (w) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = 8 * (lane + 64 * TEAM * i);
+            cw[i].load(w + c, C - c);
+        }
+    }
+    float dw[CH][8], db[CH][8];
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
+    const long long step = (long long)gridDim.x * TEAMS;
+    for (long long base = (long long)blockIdx.x * TEAMS; base < in_set; base += step) {  // (the same number of turns for every wave)
+        const bool live = base + team < in_set;
+        const long long row = first + (live ? base + team : 0);
+        const int g = (int)row / a.rows, r = (int)row - g * a.rows;
+        const T* const x = (const T*)a.x + g * a.st[2] + r * a.st[3];
+        const T* const dy = (const T*)a.dy + g * a.st[0] + r * a.st[1];
+        const float mean = a.stats[row], rstd = a.stats[total + row];
+        Chunk8<T> vx[CH], vd[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = 8 * (lane + 64 * TEAM * i);
+            vx[i].load(x + c, C - c);
+            vd[i].load(dy + c, live ? C - c : 0);  // (a row that is not there adds nothing)
+        }
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = vd[i].get(j), h = (vx[i].get(j) - mean) * rstd;
+                const float dyw = w ? d * (a.offset + cw[i].get(j)) : d;
+                s1 += dyw;
+                s2 += dyw * h;
+                if (sums && live) {
+                    dw[i][j] += d * h;
+                    db[i][j] += d;
+                }
+            }
+        if (a.dx) {
+            s1 = team_sum<TEAM>(s1, slots, wave) / (float)C;
+            s2 = team_sum<TEAM>(s2, slots, wave) / (float)C;
+            if (live) {
+                T* const dx = (T*)a.dx + g * a.st[4] + r * a.st[5];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const int c = 8 * (lane + 64 * TEAM * i);
+                    if (c >= C) break;
+                    float o[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float d = vd[i].get(j), h = (vx[i].get(j) - mean) * rstd;
+                        o[j] = rstd * ((w ? d * (a.offset + cw[i].get(j)) : d) - s1 - h * s2);
+                    }
+                    Chunk8<T>::store(dx + c, C - c, o);
+                }
+            }
+        }
+    }
+    if (!sums) return;
+    float* const out = a.ws + ((long long)set * gridDim.x + blockIdx.x) * 2 * C;
+    for (int t = 0; t < TEAMS; ++t) {
+        if (team == t) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int c = 8 * (lane + 64 * TEAM * i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < C) {
+                        if (TEAMS > 1 && t > 0) {
+                            dw[i][j] += lds[c + j];
+                            db[i][j] += lds[C + c + j];
+                        }
+                        float* const to = TEAMS > 1 && t + 1 < TEAMS ? lds : out;
+                        to[c + j] = dw[i][j];
+                        to[C + c + j] = db[i][j];
+                    }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// d_weight and d_bias of a set from its partials: a workgroup takes 64 of the 2 C columns, wave w the partials w, w + 16, ...
+template <typename TW>
+__global__ void __launch_bounds__(1024) norm_join_kernel(NormArgs a, int partials)
+{
+    __shared__ float part[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, C = a.channels, set = blockIdx.y;
+    const int col = blockIdx.x * 64 + lane;
+    const float* const from = a.ws + (long long)set * partials * 2 * C;
+    float s = 0.f;
+    if (col < 2 * C)
+        for (int p = wave; p < partials; p += 16) s += from[(long long)p * 2 * C + col];
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && col < 2 * C) {
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += part[i][lane];
+        TW* const to = (TW*)(col < C ? a.dw : a.db);
+        if (to) to[(long long)set * C + (col < C ? col : col - C)] = (TW)s;
+    }
+}
+
+struct Form {
+    int team, ch;
+};
+int chunks_a_lane(int channels, int team) { return (channels + 512 * team - 1) / (512 * team); }
+Form forward_form(int channels)
+{
+    const int team = channels <= 4096 ? 1 : channels <= 8192 ? 4 : 8;
+    return {team, chunks_a_lane(channels, team)};
+}
+Form backward_form(int channels)
+{
+    const int team = channels <= 1536 ? 1 : channels <= 2 * 1536 ? 2 : channels <= 4 * 1536 ? 4 : 8;
+    return {team, chunks_a_lane(channels, team)};
+}
+
+// call(team, ch) with both as integral constants, if (TEAM, CH) is the form.
+template <int TEAM, int CH, typename F>
+bool try_form(const Form& f, F& call)
+{
+    if (f.team != TEAM || f.ch != CH) return false;
+    call(std::integral_constant<int, TEAM>{}, std::integral_constant<int, CH>{});
+    return true;
+}
+
+template <typename T, typename TW>
+hipError_t forward(const NormArgs& a, hipStream_t stream)
+{
+    const Form f = forward_form(a.channels);
+    auto call = [&](auto team, auto ch) {
+        constexpr int TEAM = team, CH = ch, teams = kThreads / 64 / TEAM;
+        const long long rows = (long long)a.groups * a.rows;
+        norm_forward_kernel<T, TW, TEAM, CH><<<dim3((unsigned)((rows + teams - 1) / teams)), dim3(kThreads), 0, stream>>>(a);
+    };
+    const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<1, 4>(f, call) || try_form<1, 5>(f, call) ||
+                    try_form<1, 6>(f, call) || try_form<1, 7>(f, call) || try_form<1, 8>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) ||
+                    try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
+    return ok ? hipGetLastError() : hipErrorInvalidValue;
+}
+
+template <typename T, typename TW>
+hipError_t backward(const NormArgs& a, hipStream_t stream)
+{
+    const Form f = backward_form(a.channels);
+    const int sets = a.per_group ? a.groups : 1;
+    const int partials = norm_partials(a.groups, a.rows, a.channels, a.per_group);
+    hipError_t e = hipSuccess;
+    if (partials > 0) {
+        auto call = [&](auto team, auto ch) {
+            constexpr int TEAM = team, CH = ch, teams = kThreads / 64 / TEAM;
+            const size_t lds = teams > 1 && (a.dw || a.db) ? (size_t)a.channels * 8 : 0;  // (at most 48 KB)
+            norm_backward_kernel<T, TW, TEAM, CH><<<dim3(partials, sets), dim3(kThreads), lds, stream>>>(a);
+        };
+        const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
+                        try_form<4, 2>(f, call) || try_form<4, 3>(f, call) || try_form<8, 2>(f, call) || try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
+        e = ok ? hipGetLastError() : hipErrorInvalidValue;
+    }
+    if (e == hipSuccess && (a.dw || a.db)) {
+        norm_join_kernel<TW><<<dim3((2 * a.channels + 63) / 64, sets), dim3(1024), 0, stream>>>(a, partials);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace
+
+int norm_partials(long long groups, long long rows, int channels, int per_group)
+{
+    // 256 workgroups, one for each CU, or as many as there are rows for; the sets share them.
+    const long long teams = kThreads / 64 / backward_form(channels).team, in_set = per_group ? rows : groups * rows, sets = per_group ? groups : 1;
+    if (in_set == 0 || sets == 0) return 0;
+    return (int)std::min<long long>((in_set + teams - 1) / teams, std::max<long long>(1, 256 / sets));
+}
+
+hipError_t launch_norm_forward(const NormArgs& a, int dtype, int weight_dtype, hipStream_t stream)
+{
+    if (dtype == CLEAR_BF16) return weight_dtype == CLEAR_BF16 ? forward<__bf16, __bf16>(a, stream) : forward<__bf16, float>(a, stream);
+    return weight_dtype == CLEAR_BF16 ? forward<float, __bf16>(a, stream) : forward<float, float>(a, stream);
+}
+
+hipError_t launch_norm_backward(const NormArgs& a, int dtype, int weight_dtype, hipStream_t stream)
+{
+    if (dtype == CLEAR_BF16) return weight_dtype == CLEAR_BF16 ? backward<__bf16, __bf16>(a, stream) : backward<__bf16, float>(a, stream);
+    return weight_dtype == CLEAR_BF16 ? backward<float, __bf16>(a, stream) : backward<float, float>(a, stream);
+}
+
+}  // namespace block
+}  // namespace clear

@@ -1,0 +1,60 @@
+"""AdamW over the parameters of a model, one launch for every 48 of them (clear_block_adamw).
+
+    from paper_2412_16112_amd.optim import AdamW
+    opt = AdamW(model.parameters(), lr=1e-4, weight_decay=0.01, state_bits=8)
+    loss.backward(); opt.step(); opt.zero_grad()
+
+The optimizer owns the states, and the fp32 masters if asked for (for bf16 parameters: small steps are not lost in the rounding).  Where tensors lie
+is written down once; a step hands over the gradients."""
+import torch
+
+from . import clear_attn as ca
+from . import clear_block as cb
+
+
+class AdamW:
+    def __init__(self, params, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, state_bits=32, masters=False):
+        self.params = list(params)
+        if state_bits not in (8, 32):
+            raise ca.ClearAttnError(ca.CLEAR_ERR_INVALID_ARG, "state_bits must be 32 or 8")
+        self.hyper = dict(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
+        self.state_bits, self.steps = state_bits, 0
+        self.masters = [p.detach().float().clone() for p in self.params] if masters else None
+        states = [cb.adamw_state(p.detach(), state_bits) for p in self.params]
+        self.exp_avgs, self.exp_avg_sqs = [s[0] for s in states], [s[1] for s in states]
+        self.scales = [s[2] for s in states] if state_bits == 8 else None
+        # one table of descriptors for each (device, dtype)
+        self._tables = []
+        places = {}
+        for i, p in enumerate(self.params):
+            if not p.is_cuda:
+                raise ca.ClearAttnError(ca.CLEAR_ERR_INVALID_ARG, "parameters must be device tensors")
+            places.setdefault((p.device, ca._dtype_code(p)), []).append(i)
+        for (device, dtype), members in places.items():
+            table = (cb.AdamWTensor * len(members))()
+            for entry, i in zip(table, members):
+                cb._describe(entry, self.params[i].detach(), self.exp_avgs[i], self.exp_avg_sqs[i], self.masters[i] if masters else None,
+                             self.scales[i] if state_bits == 8 else None, state_bits == 8)
+            self._tables.append((device, dtype, members, table))
+
+    def step(self, grads=None, grad_scale=None, stream=None, **hyper):
+        """One step with the parameters' .grad, or with `grads` (a list in their order); entries that are None are skipped.  Keyword arguments
+        (lr, ...) hold for this step only.  grad_scale: an fp32 device scalar that the gradients are multiplied by."""
+        grads = [p.grad for p in self.params] if grads is None else list(grads)
+        if len(grads) != len(self.params):
+            raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
+        h = dict(self.hyper, **hyper)
+        for _, _, members, table in self._tables:  # (everything is checked before anything is updated)
+            for entry, i in zip(table, members):
+                p = self.params[i]
+                if p.data_ptr() != entry.param:
+                    raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "parameter %d has moved since the optimizer was made" % i)
+                cb._grad(entry, p, grads[i])
+        self.steps += 1
+        for device, dtype, members, table in self._tables:
+            cb._launch(table, len(members), dtype, device, self.state_bits == 8, self.steps, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"],
+                       grad_scale, stream)
+
+    def zero_grad(self):
+        for p in self.params:
+            p.grad = None
