@@ -101,6 +101,19 @@ __device__ __forceinline__ void activation_slope(float g, int act, float* value,
     }
 }
 
+// Workgroups are dealt to the 8 XCDs in turn, each with its own L2: every XCD gets a contiguous range of an order that goes through the tiles in bands of 4
+// of B, so that the 32 tiles in flight on it are 4 x 8 and share 12 operand tiles instead of 30 and more.
+__device__ __forceinline__ void tile_of(unsigned id, unsigned n, int tiles_a, int tiles_b, int* tile_a, int* tile_b)
+{
+    constexpr unsigned XCDS = 8, BAND = 4;
+    const unsigned x = id % XCDS, each = n / XCDS, more = n % XCDS;
+    const unsigned at = x * each + min(x, more) + id / XCDS;
+    const unsigned band = at / (BAND * tiles_a), in = at - band * (BAND * tiles_a);
+    const unsigned width = min(BAND, (unsigned)tiles_b - band * BAND);
+    *tile_a = (int)(in / width);
+    *tile_b = (int)(band * BAND + in % width);
+}
+
 template <int KIND, int WA, int WB, int NB>
 __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
 {
@@ -109,7 +122,8 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_bytes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wa = wave % WA, wb = wave / WA;
-    const int tile_a = blockIdx.x % t.tiles_a, tile_b = blockIdx.x / t.tiles_a;
+    int tile_a, tile_b;
+    tile_of(blockIdx.x, gridDim.x, t.tiles_a, t.tiles_b, &tile_a, &tile_b);
 
     // origin of the tile; forward: the tile's A rows are TA / 2 rows of the gate weight and the same of the up weight;
     // weight gradient: the first half of the tiles of B is dG's, the second dU's
@@ -217,26 +231,66 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    if (steps > 0) issue(0);
-    for (int it = 0; it < steps; ++it) {
-        // this wave's loads of the stage have arrived and its reads of the other one are done; after the barrier everybody's
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // ---- the loop.  A stage is kStep / 16 slots; in each the operands of the next slot are read while the matrix instructions of this one run, across the
+    // barrier too: its last slot's operands are in registers when the stage is given up, and the next stage's first are read beside its products.
+    constexpr int SLOTS = kStep / 16;
+    bf16x8 a[2][2], b[2][NB];
+    auto read = [&](int into, unsigned stage, int s) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) a[into][i] = S::A_COLUMNS ? read_columns(a_at[i] + stage, s, 2 * S::TA) : read_rows(a_at[i] + stage, s);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) b[into][j] = S::B_COLUMNS ? read_columns(b_at[j] + stage, s, 2 * S::TB) : read_rows(b_at[j] + stage, s);
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[from][i], b[from][j], acc[i][j], 0, 0, 0);
+    };
+    // A slot's order: reads and products in turn.
+    auto interleave = [&] {
+        constexpr int READS = (S::A_COLUMNS ? 4 : 2) + (S::B_COLUMNS ? 2 : 1) * NB, PRODUCTS = 2 * NB;
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            constexpr int each = (READS + PRODUCTS - 1) / PRODUCTS;
+            __builtin_amdgcn_sched_group_barrier(0x100, each, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // this wave's loads have arrived and its reads are done; after the barrier everybody's
+    auto settle = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt 0, lgkmcnt 0, expcnt unconstrained
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (it + 1 < steps) issue(it + 1);
-        const unsigned stage = (it & 1) * S::STAGE;
+    };
+    auto slots = [&](unsigned stage) {  // all but the last
 #pragma unroll
-        for (int s = 0; s < kStep / 16; ++s) {
-            bf16x8 a[2], b[NB];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) a[i] = S::A_COLUMNS ? read_columns(a_at[i] + stage, s, 2 * S::TA) : read_rows(a_at[i] + stage, s);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) b[j] = S::B_COLUMNS ? read_columns(b_at[j] + stage, s, 2 * S::TB) : read_rows(b_at[j] + stage, s);
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+        for (int s = 0; s + 1 < SLOTS; ++s) {
+            __builtin_amdgcn_sched_barrier(0);
+            read((s + 1) & 1, stage, s + 1);
+            multiply(s & 1);
+            interleave();
         }
+    };
+    if (steps > 0) {
+        issue(0);
+        settle();
+        if (steps > 1) issue(1);
+        read(0, 0, 0);
+        for (int it = 0; it + 1 < steps; ++it) {
+            const unsigned stage = (it & 1) * S::STAGE;
+            slots(stage);
+            settle();
+            if (it + 2 < steps) issue(it + 2);  // (into the stage just read)
+            __builtin_amdgcn_sched_barrier(0);
+            read(0, S::STAGE - stage, 0);
+            multiply((SLOTS - 1) & 1);
+            interleave();
+        }
+        slots(((steps - 1) & 1) * S::STAGE);
+        multiply((SLOTS - 1) & 1);
     }
 
     // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks
