@@ -39,12 +39,9 @@ __device__ __forceinline__ void load_to_lds(const i32x4& buffer, unsigned voff, 
 }
 
 // ---- a tile of ROWS rows (or columns) x kStep of the contraction in LDS, 128 ROWS bytes ---------------------------------------
-// Stored along the contraction: rows of 128 bytes, 16-byte chunk c of row r in slot c ^ (r & 7).  A load instruction fills 8 rows; the operand
-// read takes 16 bytes of 32 rows a half wave, 8 neighbouring lanes from 8 different slots.
-struct RowsTile {
-    __device__ __forceinline__ static unsigned load_offset(int lane, long long ld) { return (unsigned)((lane >> 3) * ld * 2 + (((lane & 7) ^ (lane >> 3)) << 4)); }
-    __device__ __forceinline__ static int chunk(int lane) { return (lane & 7) ^ (lane >> 3); }
-};
+// Stored along the contraction: rows of 128 bytes, 16-byte chunk c of row r in slot c ^ (r / 2 & 7).  A load instruction fills 8 rows; the operand read
+// takes 16 bytes of 32 rows a half wave, and 16 neighbouring rows (two of them to the 256 bytes that LDS is wide) lie in different banks.
+__device__ __forceinline__ int turn_of(int row) { return (row >> 1) & 7; }
 // Stored across: kStep rows of 2 ROWS bytes; 32-byte granule g (16 columns) of contraction row k in slot g ^ spread(k & 3).  A load instruction
 // fills 1 KB, 2 or 4 contraction rows.  The transpose read takes, for 16 lanes, 32 bytes of 4 contraction rows: with the spread of 0, 5, 2, 7 these lie in
 // different banks, those of the neighbouring 16 lanes (the granule beside) too.
@@ -61,7 +58,7 @@ struct Shape {
 
 struct TileArgs {
     const __bf16 *a0, *a1, *b0, *b1;  // the operands, and the second of those that come in two
-    long long ld_a0, ld_a1, ld_b0, ld_b1;
+    long long ld_a0, ld_a1, ld_b0;
     int rows_a;          // extent of A's rows (the contiguous axis of the output)
     long long rows_b;    // of B's rows
     long long depth;     // the contraction (of each half)
@@ -133,68 +130,75 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     const long long b_first = (long long)(second ? tile_b - half_tiles : tile_b) * S::TB;
     const int steps_each = (int)((t.depth + kStep - 1) / kStep), steps = KIND == kInputGrad ? 2 * steps_each : steps_each;
 
-    // ---- loads of a stage
+    // ---- loads of a stage: instruction i of this wave is i-th of its share of A's, then of B's
     constexpr int A_CHUNKS = S::TA / 8, B_CHUNKS = S::TB / 8;  // 16-byte chunks of a contraction row where an operand is stored across
-    auto issue = [&](int it) {
-        const unsigned to = lds + (it & 1) * S::STAGE;
+    constexpr int LOADS = S::A_LOADS + S::B_LOADS;
+    static_assert(S::A_LOADS % 2 == 0 && S::B_LOADS % 2 == 0, "whether a share's instruction is an even one of its tile is known in advance");
+    i32x4 buf_a, buf_b;
+    unsigned lds_to = 0, k_bytes = 0;
+    int k_left = 0;
+    const bool up = !S::A_COLUMNS && wave * S::A_LOADS >= S::TA / 16;  // forward: this wave loads the up weight's rows
+    static_assert(S::A_COLUMNS || (S::TA / 16) % S::A_LOADS == 0, "a wave's share of A is of one weight");
+    const long long ld_a_rows = up ? t.ld_a1 : t.ld_a0;  // (the two halves of B are in one workspace and have one stride; those of A need not)
+    long long ld_a = 0;
+    // (The pointers and strides that the loop chooses between are pinned in registers: a choice between two arguments becomes a scalar load from the chosen
+    // place otherwise, whose wait counts the LDS reads in flight too.)
+    const __bf16 *a0 = t.a0, *a1 = t.a1, *b0 = second ? t.b1 : t.b0, *b1 = t.b1;
+    long long ld_a0 = t.ld_a0, ld_a1 = t.ld_a1;
+    asm("" : "+s"(a0), "+s"(a1), "+s"(b0), "+s"(b1), "+s"(ld_a0), "+s"(ld_a1));
+    if (!S::A_COLUMNS)
+        buf_a = buffer_of((up ? a1 : a0) + a_first * ld_a_rows, ((min((long long)t.rows_a - a_first, (long long)S::TA / 2) - 1) * ld_a_rows + t.depth) * 2);
+    const long long b_bytes = ((min(t.rows_b - b_first, (long long)S::TB) - 1) * t.ld_b0 + t.depth) * 2;
+    // What the loads of stage `it` have in common.  Along the contraction the buffer stays and the offset moves; across, the buffer moves.
+    auto aim = [&](int it) {
+        lds_to = lds + (it & 1) * S::STAGE;
         const bool upper = KIND == kInputGrad && it >= steps_each;
         const long long k0 = (long long)(upper ? it - steps_each : it) * kStep;
-        const long long k_left = t.depth - k0;
-        if (!S::A_COLUMNS) {
-            const int c = RowsTile::chunk(lane);
-            const bool in = c * 8 < k_left;
-#pragma unroll
-            for (int i = 0; i < S::A_LOADS; ++i) {
-                const int n = wave * S::A_LOADS + i;
-                const bool up = n >= S::TA / 16;  // (uniform)
-                const long long ld = up ? t.ld_a1 : t.ld_a0;
-                const long long rows = t.rows_a - a_first;
-                const i32x4 buf = buffer_of((up ? t.a1 : t.a0) + (long long)a_first * ld, ((min(rows, (long long)S::TA / 2) - 1) * ld + t.depth) * 2);
-                const unsigned at = (unsigned)((n - (up ? S::TA / 16 : 0)) * 8 * ld * 2 + k0 * 2);
-                load_to_lds(buf, in ? RowsTile::load_offset(lane, ld) + at : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
-            }
-        } else {
-            const __bf16* const p = upper ? t.a1 : t.a0;
-            const long long ld = upper ? t.ld_a1 : t.ld_a0;
-            const i32x4 buf = buffer_of(p + k0 * ld + a_first, ((min(k_left, (long long)kStep) - 1) * ld + t.rows_a - a_first) * 2);
-            constexpr int EACH = 64 / A_CHUNKS;  // contraction rows an instruction
-#pragma unroll
-            for (int i = 0; i < S::A_LOADS; ++i) {
-                const int n = wave * S::A_LOADS + i, k = n * EACH + lane / A_CHUNKS, slot = lane % A_CHUNKS;
-                const int c = ((slot >> 1) ^ spread(k)) << 1 | (slot & 1);
-                const unsigned off = (unsigned)(k * ld * 2 + c * 16);
-                load_to_lds(buf, a_first + c * 8 < t.rows_a ? off : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
-            }
+        k_left = (int)max(min(t.depth - k0, (long long)kStep), 0LL);  // 0: no such stage
+        k_bytes = (unsigned)(k0 * 2);
+        if (S::A_COLUMNS) {
+            ld_a = upper ? ld_a1 : ld_a0;
+            buf_a = buffer_of((upper ? a1 : a0) + k0 * ld_a + a_first, ((k_left - 1) * ld_a + t.rows_a - a_first) * 2);
         }
-        const unsigned to_b = to + S::A_BYTES;
-        const __bf16* const p = upper || second ? t.b1 : t.b0;
-        const long long ld = upper || second ? t.ld_b1 : t.ld_b0;
-        if (!S::B_COLUMNS) {
-            const int c = RowsTile::chunk(lane);
-            const bool in = c * 8 < k_left;
-            const long long rows = t.rows_b - b_first;
-            const i32x4 buf = buffer_of(p + b_first * ld, ((min(rows, (long long)S::TB) - 1) * ld + t.depth) * 2);
-#pragma unroll
-            for (int i = 0; i < S::B_LOADS; ++i) {
-                const int n = wave * S::B_LOADS + i;
-                load_to_lds(buf, in ? RowsTile::load_offset(lane, ld) + (unsigned)(n * 8 * ld * 2 + k0 * 2) : kOutside, __builtin_amdgcn_readfirstlane(to_b + n * 1024));
-            }
+        if (S::B_COLUMNS)
+            buf_b = buffer_of(b0 + k0 * t.ld_b0 + b_first, ((k_left - 1) * t.ld_b0 + t.rows_b - b_first) * 2);
+        else
+            buf_b = buffer_of((upper ? b1 : b0) + b_first * t.ld_b0, b_bytes);
+    };
+    auto load_rows = [&](const i32x4& buf, int n, int even, long long ld, unsigned to) {
+        const int r = lane >> 3, c = (lane & 7) ^ turn_of(even * 8 + r);
+        const unsigned off = (unsigned)(r * ld * 2 + c * 16) + (unsigned)(n * 8 * ld * 2) + k_bytes;
+        load_to_lds(buf, c * 8 < k_left ? off : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
+    };
+    auto load_columns = [&](const i32x4& buf, int n, int chunks, long long ld, long long left, unsigned to) {
+        const int each = 64 / chunks, k = n * each + lane / chunks, slot = lane % chunks;
+        const int c = ((slot >> 1) ^ spread(k)) << 1 | (slot & 1);
+        load_to_lds(buf, c * 8 < left ? (unsigned)(k * ld * 2 + c * 16) : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
+    };
+    auto load = [&](int i) {
+        if (i < S::A_LOADS) {
+            const int n = wave * S::A_LOADS + i;
+            if (S::A_COLUMNS)
+                load_columns(buf_a, n, A_CHUNKS, ld_a, (long long)t.rows_a - a_first, lds_to);
+            else
+                load_rows(buf_a, n - (up ? S::TA / 16 : 0), i & 1, ld_a_rows, lds_to + (up ? S::TA / 16 * 1024 : 0));
         } else {
-            const i32x4 buf = buffer_of(p + k0 * ld + b_first, ((min(k_left, (long long)kStep) - 1) * ld + t.rows_b - b_first) * 2);
-            constexpr int EACH = 64 / B_CHUNKS;
-#pragma unroll
-            for (int i = 0; i < S::B_LOADS; ++i) {
-                const int n = wave * S::B_LOADS + i, k = n * EACH + lane / B_CHUNKS, slot = lane % B_CHUNKS;
-                const int c = ((slot >> 1) ^ spread(k)) << 1 | (slot & 1);
-                const unsigned off = (unsigned)(k * ld * 2 + c * 16);
-                load_to_lds(buf, b_first + c * 8 < t.rows_b ? off : kOutside, __builtin_amdgcn_readfirstlane(to_b + n * 1024));
-            }
+            const int n = wave * S::B_LOADS + i - S::A_LOADS;
+            if (S::B_COLUMNS)
+                load_columns(buf_b, n, B_CHUNKS, t.ld_b0, t.rows_b - b_first, lds_to + S::A_BYTES);
+            else
+                load_rows(buf_b, n, i & 1, t.ld_b0, lds_to + S::A_BYTES);
         }
+    };
+    auto issue = [&](int it) {
+        aim(it);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(i);
     };
 
     // ---- operand reads: 32 rows (columns) from `first` of the tile on, 16 s .. 16 s + 15 of the stage's contraction; lane l has row l % 32 and
     // elements 8 (l / 32) .. + 7 of them
-    auto rows_address = [&](int first) { return (unsigned)((first + (lane & 31)) * 128 + (((lane >> 5) ^ (lane & 7)) << 4)); };
+    auto rows_address = [&](int first) { return (unsigned)((first + (lane & 31)) * 128 + (((lane >> 5) ^ turn_of(lane)) << 4)); };
     auto read_rows = [&](unsigned base, int s) { return *(lds_bf16x8_ptr)(size_t)(base ^ (unsigned)(s << 5)); };
     auto columns_address = [&](int first, int row_bytes) {
         const int j = lane & 15, k = 8 * (lane >> 5) + (j >> 2);
@@ -241,11 +245,12 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
 #pragma unroll
         for (int j = 0; j < NB; ++j) b[into][j] = S::B_COLUMNS ? read_columns(b_at[j] + stage, s, 2 * S::TB) : read_rows(b_at[j] + stage, s);
     };
+    auto product = [&](int from, int n) {
+        acc[n & 1][n >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[from][n & 1], b[from][n >> 1], acc[n & 1][n >> 1], 0, 0, 0);
+    };
     auto multiply = [&](int from) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[from][i], b[from][j], acc[i][j], 0, 0, 0);
+        for (int n = 0; n < 2 * NB; ++n) product(from, n);
     };
     // A slot's order: reads and products in turn.
     auto interleave = [&] {
@@ -274,23 +279,31 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
             interleave();
         }
     };
+    // The loads of the stage after the last fall outside their buffers, all of them: nothing is read, and the loop has no branch for them.
     if (steps > 0) {
         issue(0);
         settle();
-        if (steps > 1) issue(1);
+        issue(1);
         read(0, 0, 0);
         for (int it = 0; it + 1 < steps; ++it) {
             const unsigned stage = (it & 1) * S::STAGE;
             slots(stage);
             settle();
-            if (it + 2 < steps) issue(it + 2);  // (into the stage just read)
             __builtin_amdgcn_sched_barrier(0);
             read(0, S::STAGE - stage, 0);
-            multiply((SLOTS - 1) & 1);
-            interleave();
+            aim(it + 2);
+            constexpr int PRODUCTS = 2 * NB;
+#pragma unroll
+            for (int n = 0; n < PRODUCTS; ++n) {  // loads into the stage just read, each beside a product
+                product((SLOTS - 1) & 1, n);
+#pragma unroll
+                for (int i = n * LOADS / PRODUCTS; i < (n + 1) * LOADS / PRODUCTS; ++i) load(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         slots(((steps - 1) & 1) * S::STAGE);
         multiply((SLOTS - 1) & 1);
+        settle();  // (nothing may still be on its way to this workgroup's LDS when it ends)
     }
 
     // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks
@@ -453,8 +466,13 @@ hipError_t launch_tiles(TileArgs t, hipStream_t stream)
 template <int KIND>
 hipError_t launch_shape(const TileArgs& t, hipStream_t stream)
 {
-    const long long tiles = (t.rows_a + 255) / 256 * ((t.rows_b + 255) / 256) * (KIND == kInputGrad ? 1 : 2);
-    return tiles >= 192 ? launch_tiles<KIND, 4, 2, 4>(t, stream) : launch_tiles<KIND, 2, 2, 2>(t, stream);
+    // Rounds over the 256 CUs, in the time that a CU takes for a 256 x 256 tile: it runs two of 128 x 128 at once, at a lower rate.
+    const long long twice = KIND == kWeightGrad ? 2 : 1;
+    const int half = KIND == kForward ? 2 : 1;
+    const long long large = ((long long)t.rows_a * half + 255) / 256 * ((t.rows_b + 255) / 256) * twice;
+    const long long small = ((long long)t.rows_a * half + 127) / 128 * ((t.rows_b + 127) / 128) * twice;
+    const double large_cost = (double)((large + 255) / 256), small_cost = 0.62 * (double)((small + 511) / 512);
+    return large_cost <= small_cost ? launch_tiles<KIND, 4, 2, 4>(t, stream) : launch_tiles<KIND, 2, 2, 2>(t, stream);
 }
 
 constexpr int kFewTokens = 64;
@@ -500,7 +518,7 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
     if (e == hipSuccess && a.dx && a.tokens > 0) {
         TileArgs t = {};
         t.a0 = (const __bf16*)a.wg, t.a1 = (const __bf16*)a.wu, t.b0 = dg, t.b1 = du;
-        t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = t.ld_b1 = a.hidden;
+        t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = a.hidden;
         t.rows_a = a.channels, t.rows_b = a.tokens, t.depth = a.hidden;
         t.out0 = (__bf16*)a.dx, t.ld_out0 = a.ld_dx;
         e = launch_shape<kInputGrad>(t, stream);
@@ -508,7 +526,7 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
     if (e == hipSuccess && a.dwg) {
         TileArgs t = {};
         t.a0 = (const __bf16*)a.x, t.b0 = dg, t.b1 = du;
-        t.ld_a0 = a.ld_x, t.ld_b0 = t.ld_b1 = a.hidden;
+        t.ld_a0 = a.ld_x, t.ld_b0 = a.hidden;
         t.rows_a = a.channels, t.rows_b = a.hidden, t.depth = a.tokens;
         t.out0 = (__bf16*)a.dwg, t.ld_out0 = a.ld_dwg;
         t.out1 = (__bf16*)a.dwu, t.ld_out1 = a.ld_dwu;
