@@ -63,38 +63,40 @@ struct TileArgs {
     long long rows_b;    // of B's rows
     long long depth;     // the contraction (of each half)
     int tiles_a, tiles_b, act;
-    __bf16 *out0, *out1;
-    long long ld_out0, ld_out1;
+    __bf16 *out0, *out1;   // the output, and where its rows from rows_out0 on go (weight gradient)
+    long long ld_out0, ld_out1, rows_out0;
     float* pre;
 };
 
+// 1 / (1 + 2^e).  The hardware's exponential and reciprocal, each good to an ulp or two, are far below the rounding of the result to bf16; an IEEE division
+// made the epilogue of a 256 x 256 tile 4 us longer (of 70).
+__device__ __forceinline__ float logistic2(float e) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(e)); }
+constexpr float kLog2E = 1.4426950408889634f;
+// tanh form: (1 + tanh z) / 2 = 1 / (1 + e^(-2 z)) with z = sqrt(2 / pi) (g + 0.044715 g^3); -2 z log2(e) = g (kTanh1 + kTanh3 g^2)
+constexpr float kTanh1 = -2.f * 0.7978845608028654f * kLog2E, kTanh3 = kTanh1 * 0.044715f;
+
 __device__ __forceinline__ float activation(float g, int act)
 {
-    if (act == CLEAR_ACT_SILU) return g / (1.f + __expf(-g));
-    if (act == CLEAR_ACT_GELU_TANH) {
-        // (1 + tanh z) / 2 = 1 / (1 + e^(-2 z))
-        const float z = 0.7978845608028654f * (g + 0.044715f * g * g * g);
-        return g / (1.f + __expf(-2.f * z));
-    }
+    if (act == CLEAR_ACT_SILU) return g * logistic2(-kLog2E * g);
+    if (act == CLEAR_ACT_GELU_TANH) return g * logistic2(g * __builtin_fmaf(g * g, kTanh3, kTanh1));
     return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
 }
 // act(g) and act'(g).
 __device__ __forceinline__ void activation_slope(float g, int act, float* value, float* slope)
 {
     if (act == CLEAR_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-g));
+        const float s = logistic2(-kLog2E * g);
         *value = g * s;
         *slope = s + g * s * (1.f - s);
     } else if (act == CLEAR_ACT_GELU_TANH) {
         const float c = fabsf(g) > 30.f ? copysignf(30.f, g) : g;  // (s is 0 or 1 long before; a square that overflows would make 0 * inf of it)
-        const float z = 0.7978845608028654f * (c + 0.044715f * c * c * c);
-        const float s = 1.f / (1.f + __expf(-2.f * z));
+        const float s = logistic2(c * __builtin_fmaf(c * c, kTanh3, kTanh1));
         *value = g * s;
         *slope = s + 2.f * c * s * (1.f - s) * 0.7978845608028654f * (1.f + 3.f * 0.044715f * c * c);
     } else {
         const float s = 0.5f * (1.f + erff(g * 0.7071067811865476f));
         *value = g * s;
-        *slope = s + g * 0.3989422804014327f * __expf(-0.5f * g * g);
+        *slope = s + g * 0.3989422804014327f * __builtin_amdgcn_exp2f(-0.5f * kLog2E * g * g);
     }
 }
 
@@ -122,12 +124,9 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     int tile_a, tile_b;
     tile_of(blockIdx.x, gridDim.x, t.tiles_a, t.tiles_b, &tile_a, &tile_b);
 
-    // origin of the tile; forward: the tile's A rows are TA / 2 rows of the gate weight and the same of the up weight;
-    // weight gradient: the first half of the tiles of B is dG's, the second dU's
-    const int half_tiles = KIND == kWeightGrad ? t.tiles_b / 2 : 0;
-    const bool second = KIND == kWeightGrad && tile_b >= half_tiles;
+    // origin of the tile; forward: the tile's A rows are TA / 2 rows of the gate weight and the same of the up weight
     const int a_first = tile_a * (KIND == kForward ? S::TA / 2 : S::TA);
-    const long long b_first = (long long)(second ? tile_b - half_tiles : tile_b) * S::TB;
+    const long long b_first = (long long)tile_b * S::TB;
     const int steps_each = (int)((t.depth + kStep - 1) / kStep), steps = KIND == kInputGrad ? 2 * steps_each : steps_each;
 
     // ---- loads of a stage: instruction i of this wave is i-th of its share of A's, then of B's
@@ -143,7 +142,7 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     long long ld_a = 0;
     // (The pointers and strides that the loop chooses between are pinned in registers: a choice between two arguments becomes a scalar load from the chosen
     // place otherwise, whose wait counts the LDS reads in flight too.)
-    const __bf16 *a0 = t.a0, *a1 = t.a1, *b0 = second ? t.b1 : t.b0, *b1 = t.b1;
+    const __bf16 *a0 = t.a0, *a1 = t.a1, *b0 = t.b0, *b1 = t.b1;
     long long ld_a0 = t.ld_a0, ld_a1 = t.ld_a1;
     asm("" : "+s"(a0), "+s"(a1), "+s"(b0), "+s"(b1), "+s"(ld_a0), "+s"(ld_a1));
     if (!S::A_COLUMNS)
@@ -306,42 +305,63 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
         settle();  // (nothing may still be on its way to this workgroup's LDS when it ends)
     }
 
-    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks
+    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Lanes l and l + 32 hold the
+    // two halves of 8 consecutive outputs; of two such eights each of them takes one, so that a lane stores 16 bytes.
+    auto store = [&](__bf16* out, const float (&x)[8], int first) {  // x: its part of outputs first .. + 7 and of the 8 behind
+        union {
+            bf16x4 v[2];
+            unsigned w[4];
+        } u;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) u.v[r >> 2][r & 3] = (__bf16)x[r];
+        const auto lo = __builtin_amdgcn_permlane32_swap(u.w[0], u.w[2], false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(u.w[1], u.w[3], false, false);
+        union {
+            unsigned w[4];
+            bf16x8 v;
+        } o = {{lo[0], hi[0], lo[1], hi[1]}};
+        const int c = first + 8 * (lane >> 5);
+        if (c < t.rows_a) *(bf16x8*)(out + c) = o.v;
+    };
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         const long long row = b_first + 32 * (NB * wb + j) + (lane & 31);
-        if (row >= t.rows_b) continue;
+        const bool in = row < t.rows_b;  // (a lane and its partner have the same row)
         if (KIND == kForward) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int f = a_first + 32 * wa + 8 * q + 4 * (lane >> 5);
-                if (f >= t.rows_a) continue;
-                bf16x4 o;
-                f32x4 g, u;
+            for (int q = 0; q < 2; ++q) {
+                const int f = a_first + 32 * wa + 16 * q;
+                float h[8];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    g[r] = acc[0][j][4 * q + r];
-                    u[r] = acc[1][j][4 * q + r];
-                    o[r] = (__bf16)(activation(g[r], t.act) * u[r]);
-                }
-                *(bf16x4*)(t.out0 + row * t.ld_out0 + f) = o;
-                if (t.pre) {
-                    *(f32x4*)(t.pre + row * t.rows_a + f) = g;
-                    *(f32x4*)(t.pre + (t.rows_b + row) * t.rows_a + f) = u;
+                for (int r = 0; r < 8; ++r) h[r] = activation(acc[0][j][8 * q + r], t.act) * acc[1][j][8 * q + r];
+                if (in) store(t.out0 + row * t.ld_out0, h, f);
+                if (t.pre && in) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int c = f + 8 * e + 4 * (lane >> 5);
+                        if (c >= t.rows_a) continue;
+                        f32x4 g, u;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            g[r] = acc[0][j][8 * q + 4 * e + r];
+                            u[r] = acc[1][j][8 * q + 4 * e + r];
+                        }
+                        *(f32x4*)(t.pre + row * t.rows_a + c) = g;
+                        *(f32x4*)(t.pre + (t.rows_b + row) * t.rows_a + c) = u;
+                    }
                 }
             }
-        } else {
-            __bf16* const out = (second ? t.out1 : t.out0) + row * (second ? t.ld_out1 : t.ld_out0);
+        } else if (in) {
+            const bool second = KIND == kWeightGrad && row >= t.rows_out0;
+            __bf16* const out = second ? t.out1 + (row - t.rows_out0) * t.ld_out1 : t.out0 + row * t.ld_out0;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int c = a_first + 64 * wa + 32 * i + 8 * q + 4 * (lane >> 5);
-                    if (c >= t.rows_a) continue;
-                    bf16x4 o;
+                for (int q = 0; q < 2; ++q) {
+                    float x[8];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[r] = (__bf16)acc[i][j][4 * q + r];
-                    *(bf16x4*)(out + c) = o;
+                    for (int r = 0; r < 8; ++r) x[r] = acc[i][j][8 * q + r];
+                    store(out, x, a_first + 64 * wa + 32 * i + 16 * q);
                 }
         }
     }
@@ -418,7 +438,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_tokens_kernel(const GatedA
     }
 }
 
-// dG = dH u act'(g) and dU = dH act(g) in bf16 [2][tokens][hidden], 8 channels a thread.
+// dG = dH u act'(g) and dU = dH act(g) in bf16 [tokens][2 hidden], gate first, 8 channels a thread.
 __global__ void __launch_bounds__(256) gated_gradient_kernel(const GatedArgs g, long long n)
 {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -443,8 +463,8 @@ __global__ void __launch_bounds__(256) gated_gradient_kernel(const GatedArgs g, 
         du[j] = (__bf16)((float)dh[j] * value);
     }
     __bf16* const ws = (__bf16*)g.ws;
-    *(bf16x8*)(ws + at) = dg;
-    *(bf16x8*)(ws + plane + at) = du;
+    *(bf16x8*)(ws + row * 2 * g.hidden + c) = dg;
+    *(bf16x8*)(ws + row * 2 * g.hidden + g.hidden + c) = du;
 }
 
 template <int KIND, int WA, int WB, int NB>
@@ -453,7 +473,7 @@ hipError_t launch_tiles(TileArgs t, hipStream_t stream)
     typedef Shape<KIND, WA, WB, NB> S;
     const int a_rows = KIND == kForward ? S::TA / 2 : S::TA;
     t.tiles_a = (t.rows_a + a_rows - 1) / a_rows;
-    const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB * (KIND == kWeightGrad ? 2 : 1);
+    const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB;
     if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffffffffLL / S::THREADS) return hipErrorInvalidValue;
     t.tiles_b = (int)tiles_b;
     static const hipError_t limit =
@@ -467,10 +487,9 @@ template <int KIND>
 hipError_t launch_shape(const TileArgs& t, hipStream_t stream)
 {
     // Rounds over the 256 CUs, in the time that a CU takes for a 256 x 256 tile: it runs two of 128 x 128 at once, at a lower rate.
-    const long long twice = KIND == kWeightGrad ? 2 : 1;
     const int half = KIND == kForward ? 2 : 1;
-    const long long large = ((long long)t.rows_a * half + 255) / 256 * ((t.rows_b + 255) / 256) * twice;
-    const long long small = ((long long)t.rows_a * half + 127) / 128 * ((t.rows_b + 127) / 128) * twice;
+    const long long large = ((long long)t.rows_a * half + 255) / 256 * ((t.rows_b + 255) / 256);
+    const long long small = ((long long)t.rows_a * half + 127) / 128 * ((t.rows_b + 127) / 128);
     const double large_cost = (double)((large + 255) / 256), small_cost = 0.62 * (double)((small + 511) / 512);
     return large_cost <= small_cost ? launch_tiles<KIND, 4, 2, 4>(t, stream) : launch_tiles<KIND, 2, 2, 2>(t, stream);
 }
@@ -507,7 +526,7 @@ size_t gated_workspace_bytes(long long tokens, int channels, int hidden)
 hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
 {
     const __bf16* const dg = (const __bf16*)a.ws;
-    const __bf16* const du = dg + a.tokens * a.hidden;
+    const __bf16* const du = dg + a.hidden;
     hipError_t e = hipSuccess;
     if (a.tokens > 0) {
         const long long n = a.tokens * (a.hidden / 8), blocks = (n + 255) / 256;
@@ -518,16 +537,17 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
     if (e == hipSuccess && a.dx && a.tokens > 0) {
         TileArgs t = {};
         t.a0 = (const __bf16*)a.wg, t.a1 = (const __bf16*)a.wu, t.b0 = dg, t.b1 = du;
-        t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = a.hidden;
+        t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = 2LL * a.hidden;
         t.rows_a = a.channels, t.rows_b = a.tokens, t.depth = a.hidden;
         t.out0 = (__bf16*)a.dx, t.ld_out0 = a.ld_dx;
         e = launch_shape<kInputGrad>(t, stream);
     }
     if (e == hipSuccess && a.dwg) {
         TileArgs t = {};
-        t.a0 = (const __bf16*)a.x, t.b0 = dg, t.b1 = du;
-        t.ld_a0 = a.ld_x, t.ld_b0 = a.hidden;
-        t.rows_a = a.channels, t.rows_b = a.hidden, t.depth = a.tokens;
+        t.a0 = (const __bf16*)a.x, t.b0 = dg;
+        t.ld_a0 = a.ld_x, t.ld_b0 = 2LL * a.hidden;
+        t.rows_a = a.channels, t.rows_b = 2LL * a.hidden, t.depth = a.tokens;
+        t.rows_out0 = a.hidden;
         t.out0 = (__bf16*)a.dwg, t.ld_out0 = a.ld_dwg;
         t.out1 = (__bf16*)a.dwu, t.ld_out1 = a.ld_dwu;
         e = launch_shape<kWeightGrad>(t, stream);
