@@ -231,7 +231,7 @@ long long clear_block_layer_norm_workspace(long long groups, long long rows, int
 {
     const long long none[4] = {};
     if (check_norm(groups, rows, channels, none, 4, CLEAR_F32, CLEAR_F32) != CLEAR_OK) return -1;
-    return (long long)norm_partials(groups, rows, channels, per_group != 0) * (per_group ? groups : 1) * 2 * channels;
+    return (long long)norm_partials(groups, rows, channels, per_group != 0) * (per_group ? groups : 1) * 2 * ((channels + 7) / 8 * 8);
 }
 
 int clear_block_adamw(int n_tensors, const clear_block_adamw_tensor* tensors, int dtype, int state_bits, double lr, double beta1, double beta2, double eps,

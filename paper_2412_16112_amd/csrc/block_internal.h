@@ -3,6 +3,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "../../include/clear_block.h"
 
 namespace clear {
@@ -134,11 +136,21 @@ struct Chunk8<float> {
     }
 };
 
+// Sum over the wave, in every lane (exchanges inside rows of 16 lanes, then between rows: no LDS).
 __device__ __forceinline__ float wave_sum(float x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
-    return x;
+    const auto add = [](float v, auto ctrl) {
+        constexpr int c = ctrl;
+        return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), c, 0xf, 0xf, true));
+    };
+    x = add(x, std::integral_constant<int, 0xb1>{});   // lane ^ 1
+    x = add(x, std::integral_constant<int, 0x4e>{});   // lane ^ 2
+    x = add(x, std::integral_constant<int, 0x141>{});  // the other half of 8 lanes
+    x = add(x, std::integral_constant<int, 0x140>{});  // the other half of 16
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
 }  // namespace block

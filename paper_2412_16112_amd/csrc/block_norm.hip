@@ -3,7 +3,7 @@
 // weight sums.
 //
 // A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ...: 16 bytes a lane
-// side by side (bf16), any alignment.  Forward, rows of up to 4096 channels take one wave (sums by lane exchange, no barrier), longer ones 4 or 8; backward,
+// side by side (bf16), any alignment.  Forward, rows of up to 2560 channels take one wave (sums by lane exchange, no barrier), longer ones 2, 4 or 8; backward,
 // where a lane also holds two sums for each of its channels, a wave holds up to 1536 channels and longer rows take 2, 4 or 8 (with 5 chunks a lane
 // the registers no longer suffice).
 #include <algorithm>
@@ -16,28 +16,35 @@ namespace block {
 namespace {
 
 constexpr int kThreads = 512;
+__host__ __device__ constexpr int padded(int channels) { return (channels + 7) & ~7; }  // channels of a partial sum: whole chunks
 
-// Sum over a team.  `slots`: LDS floats of the workgroup, one for each wave; every wave of the workgroup calls it.
-template <int TEAM>
-__device__ __forceinline__ float team_sum(float x, float* slots, int wave)
+// Sums over a team.  `slots`: N floats for each wave of the workgroup; every wave of the workgroup calls it.  With one barrier: the next call must be given other
+// slots, and the one after that may have these again.
+template <int TEAM, int N>
+__device__ __forceinline__ void team_sum(float (&x)[N], float (*slots)[N], int wave)
 {
-    x = wave_sum(x);
-    if (TEAM == 1) return x;
-    if ((threadIdx.x & 63) == 0) slots[wave] = x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+    if (TEAM == 1) return;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) slots[wave][i] = x[i];
+    }
     __syncthreads();
-    float s = 0.f;
     const int first = wave / TEAM * TEAM;
 #pragma unroll
-    for (int i = 0; i < TEAM; ++i) s += slots[first + i];
-    __syncthreads();
-    return s;
+    for (int i = 0; i < N; ++i) {
+        x[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < TEAM; ++w) x[i] += slots[first + w][i];
+    }
 }
 
 template <typename T, typename TW, int TEAM, int CH>
 __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
 {
     constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
-    __shared__ float slots[WAVES];
+    __shared__ float slots[2][WAVES][1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM);
     const long long total = (long long)a.groups * a.rows;
     const long long row = (long long)blockIdx.x * TEAMS + wave / TEAM;
@@ -52,44 +59,50 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
         const int c = 8 * (lane + 64 * TEAM * i);
         v[i].load(x + c, C - c);
     }
-    float s = 0.f;
+    const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)g * C : 0) : nullptr;
+    const TW* const b = a.b ? (const TW*)a.b + (a.per_group ? (long long)g * C : 0) : nullptr;
+    Chunk8<TW> cw[CH], cb[CH];  // (asked for here: they arrive while the sums are formed)
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = 8 * (lane + 64 * TEAM * i);
+        if (w) cw[i].load(w + c, C - c);
+        if (b) cb[i].load(b + c, C - c);
+    }
+    float s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s += v[i].get(j);  // (channels past the end are 0)
-    const float mean = team_sum<TEAM>(s, slots, wave) / (float)C;
-    float q = 0.f;
+        for (int j = 0; j < 8; ++j) s[0] += v[i].get(j);  // (channels past the end are 0)
+    team_sum<TEAM>(s, slots[0], wave);
+    const float mean = s[0] / (float)C;
+    float q[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = 8 * (lane + 64 * TEAM * i);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float d = v[i].get(j) - mean;
-            q += c + j < C ? d * d : 0.f;
+            q[0] += c + j < C ? d * d : 0.f;
         }
     }
-    const float rstd = 1.0f / sqrtf(team_sum<TEAM>(q, slots, wave) / (float)C + a.eps);
+    team_sum<TEAM>(q, slots[1], wave);
+    const float rstd = 1.0f / sqrtf(q[0] / (float)C + a.eps);
     if (!live) return;
     if (a.stats && lane == 0) {
         a.stats[row] = mean;
         a.stats[total + row] = rstd;
     }
-    const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)g * C : 0) : nullptr;
-    const TW* const b = a.b ? (const TW*)a.b + (a.per_group ? (long long)g * C : 0) : nullptr;
     T* const y = (T*)a.y + g * a.st[2] + r * a.st[3];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = 8 * (lane + 64 * TEAM * i);
         if (c >= C) break;
-        Chunk8<TW> cw, cb;
-        if (w) cw.load(w + c, C - c);
-        if (b) cb.load(b + c, C - c);
         float o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             o[j] = (v[i].get(j) - mean) * rstd;
-            if (w) o[j] *= a.offset + cw.get(j);
-            if (b) o[j] += cb.get(j);
+            if (w) o[j] *= a.offset + cw[i].get(j);
+            if (b) o[j] += cb[i].get(j);
         }
         Chunk8<T>::store(y + c, C - c, o);
     }
@@ -101,8 +114,8 @@ template <typename T, typename TW, int TEAM, int CH>
 __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
 {
     constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
-    extern __shared__ float lds[];  // [2][channels] where a workgroup has several teams
-    __shared__ float slots[WAVES];
+    extern __shared__ __attribute__((aligned(16))) float lds[];  // [2][padded channels] where a workgroup has several teams
+    __shared__ float slots[2][WAVES][2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM), team = wave / TEAM;
     const int C = a.channels, set = blockIdx.y;
     const long long in_set = a.per_group ? a.rows : (long long)a.groups * a.rows;
@@ -124,39 +137,61 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.f;
     const long long step = (long long)gridDim.x * TEAMS;
-    for (long long base = (long long)blockIdx.x * TEAMS; base < in_set; base += step) {  // (the same number of turns for every wave)
-        const bool live = base + team < in_set;
-        const long long row = first + (live ? base + team : 0);
-        const int g = (int)row / a.rows, r = (int)row - g * a.rows;
-        const T* const x = (const T*)a.x + g * a.st[2] + r * a.st[3];
-        const T* const dy = (const T*)a.dy + g * a.st[0] + r * a.st[1];
-        const float mean = a.stats[row], rstd = a.stats[total + row];
-        Chunk8<T> vx[CH], vd[CH];
+    struct Row {
+        Chunk8<T> x[CH], dy[CH];
+        float mean, rstd;
+        int g, r;
+        bool live;
+    };
+    auto fetch = [&](long long base, Row* to) {  // (a row that is not there: the set's first, with a dy of 0)
+        to->live = base + team < in_set;
+        const long long row = first + (to->live ? base + team : 0);
+        to->g = (int)row / a.rows;
+        to->r = (int)row - to->g * a.rows;
+        const T* const x = (const T*)a.x + to->g * a.st[2] + to->r * a.st[3];
+        const T* const dy = (const T*)a.dy + to->g * a.st[0] + to->r * a.st[1];
+        to->mean = a.stats[row];
+        to->rstd = a.stats[total + row];
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = 8 * (lane + 64 * TEAM * i);
-            vx[i].load(x + c, C - c);
-            vd[i].load(dy + c, live ? C - c : 0);  // (a row that is not there adds nothing)
+            to->x[i].load(x + c, C - c);
+            to->dy[i].load(dy + c, to->live ? C - c : 0);
         }
-        float s1 = 0.f, s2 = 0.f;
+    };
+    constexpr bool AHEAD = CH < 4;  // the next row's loads are under way while a row is worked on; with 4 chunks a lane there are no registers for it
+    Row now, next;
+    if (AHEAD) fetch((long long)blockIdx.x * TEAMS, &next);
+    int turn = 0;
+    for (long long base = (long long)blockIdx.x * TEAMS; base < in_set; base += step, turn ^= 1) {  // (the same number of turns for every wave)
+        if (AHEAD) {
+            now = next;
+            if (base + step < in_set) fetch(base + step, &next);
+        } else {
+            fetch(base, &now);
+        }
+        const Chunk8<T>(&vx)[CH] = now.x, (&vd)[CH] = now.dy;
+        const float mean = now.mean, rstd = now.rstd;
+        const bool live = now.live;
+        float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float d = vd[i].get(j), h = (vx[i].get(j) - mean) * rstd;
                 const float dyw = w ? d * (a.offset + cw[i].get(j)) : d;
-                s1 += dyw;
-                s2 += dyw * h;
+                s[0] += dyw;
+                s[1] += dyw * h;
                 if (sums && live) {
                     dw[i][j] += d * h;
                     db[i][j] += d;
                 }
             }
         if (a.dx) {
-            s1 = team_sum<TEAM>(s1, slots, wave) / (float)C;
-            s2 = team_sum<TEAM>(s2, slots, wave) / (float)C;
+            team_sum<TEAM>(s, slots[turn], wave);
+            const float s1 = s[0] / (float)C, s2 = s[1] / (float)C;
             if (live) {
-                T* const dx = (T*)a.dx + g * a.st[4] + r * a.st[5];
+                T* const dx = (T*)a.dx + now.g * a.st[4] + now.r * a.st[5];
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
                     const int c = 8 * (lane + 64 * TEAM * i);
@@ -173,48 +208,59 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
         }
     }
     if (!sums) return;
-    float* const out = a.ws + ((long long)set * gridDim.x + blockIdx.x) * 2 * C;
+    const int wide = padded(C);
+    float* const out = a.ws + ((long long)set * gridDim.x + blockIdx.x) * 2 * wide;
     for (int t = 0; t < TEAMS; ++t) {
         if (team == t) {
+            float* const to = t + 1 < TEAMS ? lds : out;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const int c = 8 * (lane + 64 * TEAM * i);
+                if (c < C) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < C) {
-                        if (TEAMS > 1 && t > 0) {
-                            dw[i][j] += lds[c + j];
-                            db[i][j] += lds[C + c + j];
+                    for (int h = 0; h < 8; h += 4) {
+                        f32x4 sw = {dw[i][h], dw[i][h + 1], dw[i][h + 2], dw[i][h + 3]}, sb = {db[i][h], db[i][h + 1], db[i][h + 2], db[i][h + 3]};
+                        if (t > 0) {
+                            sw += *(const f32x4*)(lds + c + h);
+                            sb += *(const f32x4*)(lds + wide + c + h);
                         }
-                        float* const to = TEAMS > 1 && t + 1 < TEAMS ? lds : out;
-                        to[c + j] = dw[i][j];
-                        to[C + c + j] = db[i][j];
+                        *(f32x4_any*)(to + c + h) = sw;
+                        *(f32x4_any*)(to + wide + c + h) = sb;
                     }
+                }
             }
         }
         __syncthreads();
     }
 }
 
-// d_weight and d_bias of a set from its partials: a workgroup takes 64 of the 2 C columns, wave w the partials w, w + 16, ...
+// d_weight and d_bias of a set from its partials: a workgroup takes 64 of their columns, wave w the partials w, w + 16, ...
 template <typename TW>
 __global__ void __launch_bounds__(1024) norm_join_kernel(NormArgs a, int partials)
 {
     __shared__ float part[16][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, C = a.channels, set = blockIdx.y;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wide = padded(a.channels), set = blockIdx.y;
     const int col = blockIdx.x * 64 + lane;
-    const float* const from = a.ws + (long long)set * partials * 2 * C;
+    const float* const from = a.ws + (long long)set * partials * 2 * wide + col;
     float s = 0.f;
-    if (col < 2 * C)
-        for (int p = wave; p < partials; p += 16) s += from[(long long)p * 2 * C + col];
+    if (col < 2 * wide) {
+        int p = wave;
+        for (; p + 48 < partials; p += 64) {  // (four loads in flight)
+            const float x0 = from[(long long)p * 2 * wide], x1 = from[(long long)(p + 16) * 2 * wide];
+            const float x2 = from[(long long)(p + 32) * 2 * wide], x3 = from[(long long)(p + 48) * 2 * wide];
+            s += (x0 + x1) + (x2 + x3);
+        }
+        for (; p < partials; p += 16) s += from[(long long)p * 2 * wide];
+    }
     part[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && col < 2 * C) {
+    if (wave == 0) {
         s = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s += part[i][lane];
-        TW* const to = (TW*)(col < C ? a.dw : a.db);
-        if (to) to[(long long)set * C + (col < C ? col : col - C)] = (TW)s;
+        const int c = col < wide ? col : col - wide;
+        TW* const to = (TW*)(col < wide ? a.dw : a.db);
+        if (to && c < a.channels) to[(long long)set * a.channels + c] = (TW)s;
     }
 }
 
@@ -224,7 +270,7 @@ struct Form {
 int chunks_a_lane(int channels, int team) { return (channels + 512 * team - 1) / (512 * team); }
 Form forward_form(int channels)
 {
-    const int team = channels <= 4096 ? 1 : channels <= 8192 ? 4 : 8;
+    const int team = channels <= 2560 ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
     return {team, chunks_a_lane(channels, team)};
 }
 Form backward_form(int channels)
@@ -252,8 +298,8 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
         norm_forward_kernel<T, TW, TEAM, CH><<<dim3((unsigned)((rows + teams - 1) / teams)), dim3(kThreads), 0, stream>>>(a);
     };
     const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<1, 4>(f, call) || try_form<1, 5>(f, call) ||
-                    try_form<1, 6>(f, call) || try_form<1, 7>(f, call) || try_form<1, 8>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) ||
-                    try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
+                    try_form<2, 3>(f, call) || try_form<2, 4>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) || try_form<8, 3>(f, call) ||
+                    try_form<8, 4>(f, call);
     return ok ? hipGetLastError() : hipErrorInvalidValue;
 }
 
@@ -267,7 +313,7 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
     if (partials > 0) {
         auto call = [&](auto team, auto ch) {
             constexpr int TEAM = team, CH = ch, teams = kThreads / 64 / TEAM;
-            const size_t lds = teams > 1 && (a.dw || a.db) ? (size_t)a.channels * 8 : 0;  // (at most 48 KB)
+            const size_t lds = teams > 1 && (a.dw || a.db) ? (size_t)padded(a.channels) * 8 : 0;  // (at most 48 KB)
             norm_backward_kernel<T, TW, TEAM, CH><<<dim3(partials, sets), dim3(kThreads), lds, stream>>>(a);
         };
         const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
@@ -275,7 +321,7 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
         e = ok ? hipGetLastError() : hipErrorInvalidValue;
     }
     if (e == hipSuccess && (a.dw || a.db)) {
-        norm_join_kernel<TW><<<dim3((2 * a.channels + 63) / 64, sets), dim3(1024), 0, stream>>>(a, partials);
+        norm_join_kernel<TW><<<dim3((2 * padded(a.channels) + 63) / 64, sets), dim3(1024), 0, stream>>>(a, partials);
         e = hipGetLastError();
     }
     return e;
@@ -285,7 +331,8 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
 
 int norm_partials(long long groups, long long rows, int channels, int per_group)
 {
-    // 256 workgroups, one for each CU, or as many as there are rows for; the sets share them.
+    // 256 workgroups, one for each CU, or as many as there are rows for; the sets share them.  (With two or four a CU at narrow widths the sums written and read back
+    // cost more than the rows gained: 16896 x 1024 36 -> 47 us.)
     const long long teams = kThreads / 64 / backward_form(channels).team, in_set = per_group ? rows : groups * rows, sets = per_group ? groups : 1;
     if (in_set == 0 || sets == 0) return 0;
     return (int)std::min<long long>((in_set + teams - 1) / teams, std::max<long long>(1, 256 / sets));
