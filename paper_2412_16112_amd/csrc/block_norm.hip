@@ -3,7 +3,7 @@
 // weight sums.
 //
 // A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ...: 16 bytes a lane
-// side by side (bf16), any alignment.  Forward, rows of up to 2560 channels take one wave (sums by lane exchange, no barrier), longer ones 2, 4 or 8; backward,
+// side by side (bf16), any alignment.  Forward, rows of up to 1536 channels take one wave (sums by lane exchange, no barrier), longer ones 2, 4 or 8; backward,
 // where a lane also holds two sums for each of its channels, a wave holds up to 1536 channels and longer rows take 2, 4 or 8 (with 5 chunks a lane
 // the registers no longer suffice).
 #include <algorithm>
@@ -270,7 +270,7 @@ struct Form {
 int chunks_a_lane(int channels, int team) { return (channels + 512 * team - 1) / (512 * team); }
 Form forward_form(int channels)
 {
-    const int team = channels <= 2560 ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
+    const int team = channels <= 1536 ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
     return {team, chunks_a_lane(channels, team)};
 }
 Form backward_form(int channels)
@@ -297,7 +297,7 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
         const long long rows = (long long)a.groups * a.rows;
         norm_forward_kernel<T, TW, TEAM, CH><<<dim3((unsigned)((rows + teams - 1) / teams)), dim3(kThreads), 0, stream>>>(a);
     };
-    const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<1, 4>(f, call) || try_form<1, 5>(f, call) ||
+    const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) ||
                     try_form<2, 3>(f, call) || try_form<2, 4>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) || try_form<8, 3>(f, call) ||
                     try_form<8, 4>(f, call);
     return ok ? hipGetLastError() : hipErrorInvalidValue;
