@@ -5,6 +5,8 @@ device memory, workspaces and streams; every step runs in the HIP kernels, and t
 Refusals raise ClearAttnError, as in clear_attn.  Each call enqueues on `stream` (default: torch's current stream of the tensors' device)."""
 import ctypes
 
+import torch
+
 from . import clear_attn as ca
 from .clear_attn import CLEAR_BF16, CLEAR_ERR_INVALID_ARG, CLEAR_ERR_MISMATCH, CLEAR_ERR_UNSUPPORTED, CLEAR_F32, CLEAR_OK, ClearAttnError  # noqa: F401
 
@@ -26,6 +28,7 @@ class AdamWTensor(ctypes.Structure):
                 ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n", ctypes.c_longlong)]
 
 
+_Strides3, _Strides4, _Strides6, _Strides7, _Strides12 = (ctypes.c_longlong * n for n in (3, 4, 6, 7, 12))
 _lib = None
 
 
@@ -68,34 +71,34 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-class _On:
-    """The tensors' device as the current one for the time of a call, and the stream's handle."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.guard = torch.cuda.device(device)
-        self.device, self.stream = device, stream
-
-    def __enter__(self):
-        import torch
-        self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream if self.stream is None else self.stream
-
-    def __exit__(self, *e):
-        return self.guard.__exit__(*e)
+def _call(name, device, stream, *args):
+    """The C function on the tensors' device and on `stream` (a handle; None: torch's current stream of that device).  Returns the stream's handle."""
+    s = torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+    f = getattr(_lib or lib(), name)
+    if torch.cuda.current_device() == device.index:
+        status = f(*args, s)
+    else:
+        with torch.cuda.device(device):
+            status = f(*args, s)
+    if status != CLEAR_OK:
+        _check(status)
+    return s
 
 
-def _on_device(ref, **named):
-    for name, t in named.items():
-        if t is not None and not (t.is_cuda and t.device == ref.device):
-            _refuse("%s must be a device tensor on the device of the others" % name)
+def _on_device(ref, *others):
+    """Refuses tensors (None skipped) that are not on ref's device, and a ref that is not on a GPU."""
+    if not ref.is_cuda:
+        _refuse("tensors must be device tensors")
+    device = ref.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            _refuse("tensors must be on one device")
 
 
 # ---- rotary positions ---------------------------------------------------------------------------------------------------
 
 def rotary_frequencies(rot_dim, theta=10000.0, scaling="plain", factor=1.0, original_length=0.0, slow=1.0, fast=32.0, device="cpu"):
     """clear_block_rotary_frequencies: fp64 [rot_dim / 2], radians a position, of one axis.  scaling: "plain", "linear", "base", "parts"."""
-    import torch
     if scaling not in SCALINGS:
         _refuse("unknown scaling %r" % (scaling,))
     out = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
@@ -109,16 +112,16 @@ def rotary(q, k, positions, freqs, interleaved=True, scale=1.0, inverse=False, o
     q and k may have any batch / head / token strides with contiguous channels.  positions: int32 or int64, [N], [B, N] or
     [axes, B, N] (any of the leading axes expanded); freqs: fp64 [axes, rot_dim / 2] or [rot_dim / 2].  out_q=q, out_k=k turns in place;
     by default new tensors laid out like q and k.  inverse=True is the way back, and the gradient's."""
-    import torch
     if q.dim() != 4 or (k is not None and k.dim() != 4):
         _refuse("q and k must be [B, H, N, head_dim]")
     B, Hq, N, d = q.shape
     if k is not None and (k.shape[0], k.shape[2], k.shape[3], k.dtype) != (B, N, d, q.dtype):
         _refuse("q and k must agree in batch, tokens, head_dim and dtype", CLEAR_ERR_MISMATCH)
     dtype = ca._dtype_code(q)
-    out_q = _like(q) if out_q is None else out_q
-    out_k = None if k is None else _like(k) if out_k is None else out_k
-    _on_device(q, q=q, k=k, out_q=out_q, out_k=out_k, positions=positions, freqs=freqs)
+    # (a new tensor keeps the order of a dense one's strides)
+    out_q = torch.empty_like(q) if out_q is None else out_q
+    out_k = None if k is None else torch.empty_like(k) if out_k is None else out_k
+    _on_device(q, k, out_q, out_k, positions, freqs)
     for x, y in ((q, out_q), (k, out_k)):
         if x is not None and not (y.shape == x.shape and y.dtype == x.dtype and x.stride(3) == 1 and y.stride(3) == 1):
             _refuse("an output must have its input's shape and dtype, and channels must be contiguous")
@@ -133,18 +136,12 @@ def rotary(q, k, positions, freqs, interleaved=True, scale=1.0, inverse=False, o
             (positions.shape[0] if positions.dim() == 3 else 1) != axes:
         _refuse("positions must be [N], [B, N] or [axes, B, N]")
     ps = [0] * (3 - positions.dim()) + list(positions.stride())
-    strides = (ctypes.c_longlong * 12)(*[t.stride(a) if t is not None else 0 for t in (q, out_q, k, out_k) for a in (0, 1, 2)])
-    with _On(q.device, stream) as s:
-        _check(lib().clear_block_rotary(q.data_ptr(), out_q.data_ptr(), Hq, _ptr(k), _ptr(out_k), 0 if k is None else k.shape[1], strides, B, N, d, 2 * half,
-                                        int(bool(interleaved)), positions.data_ptr(), 64 if positions.dtype == torch.int64 else 32,
-                                        (ctypes.c_longlong * 3)(*ps), axes, freqs.data_ptr(), scale, int(bool(inverse)), dtype, s))
+    sk = (0, 0, 0, 0, 0, 0) if k is None else (*k.stride()[:3], *out_k.stride()[:3])
+    strides = _Strides12(*q.stride()[:3], *out_q.stride()[:3], *sk)
+    _call("clear_block_rotary", q.device, stream, q.data_ptr(), out_q.data_ptr(), Hq, _ptr(k), _ptr(out_k), 0 if k is None else k.shape[1], strides, B, N, d,
+          2 * half, int(bool(interleaved)), positions.data_ptr(), 64 if positions.dtype == torch.int64 else 32, _Strides3(*ps), axes, freqs.data_ptr(), scale,
+          int(bool(inverse)), dtype)
     return out_q, out_k
-
-
-def _like(t):
-    """A new tensor laid out like t where t's elements are each their own, else contiguous."""
-    import torch
-    return torch.empty_like(t)  # (keeps the order of the strides of a dense tensor)
 
 
 # ---- layer norm -----------------------------------------------------------------------------------------------------------
@@ -177,7 +174,6 @@ def _row_strides(t, name):
 
 def _norm_weights(x, weight, bias):
     """(per_group, weight dtype code): weight and bias are [C], or [B, C] for x [B, N, C]."""
-    import torch
     some = weight if weight is not None else bias
     for name, w in (("weight", weight), ("bias", bias)):
         if w is None:
@@ -196,30 +192,26 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, out=None,
 
     weight and bias: [C], or [B, C] for x [B, N, C] (scale and shift per batch item; weight_offset=1 for 1 + scale).  x: bf16 or fp32, rows at
     any stride; out=x works in place.  Returns y, or (y, stats) with save_stats (fp32 [2, ...]: mean and 1/sqrt(var + eps) of every row)."""
-    import torch
     dtype = ca._dtype_code(x)
     groups, rows, C = _rows(x)
     per_group, wcode, _ = _norm_weights(x, weight, bias)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    _on_device(x, x=x, weight=weight, bias=bias, out=y)
+    _on_device(x, weight, bias, y)
     if y.shape != x.shape or y.dtype != x.dtype:
         _refuse("out must have the shape and dtype of x", CLEAR_ERR_MISMATCH)
     stats = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if save_stats else None
-    strides = (ctypes.c_longlong * 4)(*_row_strides(x, "x"), *_row_strides(y, "out"))
-    with _On(x.device, stream) as s:
-        _check(lib().clear_block_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(stats), groups, rows, C, strides, per_group, eps,
-                                            weight_offset, dtype, wcode, s))
+    _call("clear_block_layer_norm", x.device, stream, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(stats), groups, rows, C,
+          _Strides4(*_row_strides(x, "x"), *_row_strides(y, "out")), per_group, eps, weight_offset, dtype, wcode)
     return (y, stats) if save_stats else y
 
 
 def layer_norm_backward(dy, x, weight, bias, stats, weight_offset=0.0, need=(True, True, True), stream=None):
     """clear_block_layer_norm_backward: (dx, d_weight, d_bias) for what layer_norm(..., save_stats=True) was called with; None for a weight or bias
     that is None and where `need` says so."""
-    import torch
     dtype = ca._dtype_code(x)
     groups, rows, C = _rows(x)
     per_group, wcode, wdtype = _norm_weights(x, weight, bias)
-    _on_device(x, dy=dy, x=x, weight=weight, bias=bias, stats=stats)
+    _on_device(x, dy, weight, bias, stats)
     if dy.shape != x.shape or dy.dtype != x.dtype:
         _refuse("dy must have the shape and dtype of x", CLEAR_ERR_MISMATCH)
     if stats.dtype != torch.float32 or not stats.is_contiguous() or tuple(stats.shape) != (2,) + tuple(x.shape[:-1]):
@@ -235,18 +227,16 @@ def layer_norm_backward(dy, x, weight, bias, stats, weight_offset=0.0, need=(Tru
         if floats < 0:
             _check(CLEAR_ERR_UNSUPPORTED)
         ws = torch.empty(max(1, floats), dtype=torch.float32, device=x.device)
-    strides = (ctypes.c_longlong * 6)(*_row_strides(dy, "dy"), *_row_strides(x, "x"), *(_row_strides(dx, "dx") if dx is not None else (0, 0)))
-    with _On(x.device, stream) as s:
-        _check(lib().clear_block_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), stats.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), groups, rows, C,
-                                                     strides, per_group, weight_offset, dtype, wcode, _ptr(ws), s))
-        if ws is not None:
-            _record(ws, s)
+    strides = _Strides6(*_row_strides(dy, "dy"), *_row_strides(x, "x"), *(_row_strides(dx, "dx") if dx is not None else (0, 0)))
+    s = _call("clear_block_layer_norm_backward", x.device, stream, dy.data_ptr(), x.data_ptr(), _ptr(weight), stats.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db),
+              groups, rows, C, strides, per_group, weight_offset, dtype, wcode, _ptr(ws))
+    if ws is not None and stream is not None:
+        _record(ws, s)
     return dx, dw, db
 
 
 def _record(t, stream):
     """A workspace that was used on another stream than torch's current one may not be handed out before that stream is done with it."""
-    import torch
     if stream != torch.cuda.current_stream(t.device).cuda_stream:
         t.record_stream(torch.cuda.ExternalStream(stream, device=t.device))
 
@@ -255,7 +245,6 @@ def _record(t, stream):
 
 def _matrix(t, name, width):
     """(rows, row stride) of a bf16 tensor [..., width] whose leading axes are one axis of evenly spaced rows."""
-    import torch
     if t.dtype != torch.bfloat16:
         _refuse("%s must be bfloat16: the gated projection is built for bf16 only" % name, CLEAR_ERR_UNSUPPORTED)
     if t.dim() < 1 or t.shape[-1] != width:
@@ -278,7 +267,6 @@ def _activation(name):
 def gated_ff(x, w_gate, w_up, activation="silu", out=None, save_pre=False, stream=None):
     """clear_block_gated_ff: act(x w_gate^T) * (x w_up^T) for bf16 x [..., C] and weights [F, C] (rows at any stride: halves of one packed
     [2 F, C] weight will do).  activation: "silu", "gelu_tanh", "gelu_erf".  Returns h [..., F], or (h, pre) with save_pre (fp32 [2, rows, F]: both products)."""
-    import torch
     act = _activation(activation)
     if w_gate.dim() != 2 or w_up.shape != w_gate.shape:
         _refuse("w_gate and w_up must be [F, C], of one shape", CLEAR_ERR_MISMATCH)
@@ -290,17 +278,15 @@ def gated_ff(x, w_gate, w_up, activation="silu", out=None, save_pre=False, strea
     rows, ld_h = _matrix(h, "out", F)
     if rows != M:
         _refuse("out must have a row for each of x", CLEAR_ERR_MISMATCH)
-    _on_device(x, x=x, w_gate=w_gate, w_up=w_up, out=h)
+    _on_device(x, w_gate, w_up, h)
     pre = torch.empty((2, M, F), dtype=torch.float32, device=x.device) if save_pre else None
-    with _On(x.device, stream) as s:
-        _check(lib().clear_block_gated_ff(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(pre), M, C, F, ld_x, ld_g, ld_u, ld_h, act, s))
+    _call("clear_block_gated_ff", x.device, stream, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(pre), M, C, F, ld_x, ld_g, ld_u, ld_h, act)
     return (h, pre) if save_pre else h
 
 
 def gated_ff_backward(dh, x, w_gate, w_up, pre, activation="silu", need=(True, True), stream=None):
     """clear_block_gated_ff_backward: (dx, d_w_gate, d_w_up) for what gated_ff(..., save_pre=True) was called with.  need: whether dx, and whether
     the weights' gradients are wanted (None otherwise)."""
-    import torch
     act = _activation(activation)
     F, C = w_gate.shape
     M, ld_x = _matrix(x, "x", C)
@@ -311,7 +297,7 @@ def gated_ff_backward(dh, x, w_gate, w_up, pre, activation="silu", need=(True, T
         _refuse("dh must have a row for each of x, and the weights one shape", CLEAR_ERR_MISMATCH)
     if pre.dtype != torch.float32 or not pre.is_contiguous() or tuple(pre.shape) != (2, M, F):
         _refuse("pre must be what gated_ff(..., save_pre=True) gave for x")
-    _on_device(x, dh=dh, x=x, w_gate=w_gate, w_up=w_up, pre=pre)
+    _on_device(x, dh, w_gate, w_up, pre)
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
     dw = torch.empty((2, F, C), dtype=x.dtype, device=x.device) if need[1] else (None, None)
     if not need[0] and not need[1]:
@@ -320,10 +306,9 @@ def gated_ff_backward(dh, x, w_gate, w_up, pre, activation="silu", need=(True, T
     if size < 0:
         _check(CLEAR_ERR_UNSUPPORTED)
     ws = torch.empty(max(16, size), dtype=torch.uint8, device=x.device)
-    ld = (ctypes.c_longlong * 7)(ld_dh, ld_x, ld_g, ld_u, C, C, C)
-    with _On(x.device, stream) as s:
-        _check(lib().clear_block_gated_ff_backward(dh.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), pre.data_ptr(), _ptr(dx), _ptr(dw[0]), _ptr(dw[1]),
-                                                   M, C, F, ld, act, ws.data_ptr(), s))
+    s = _call("clear_block_gated_ff_backward", x.device, stream, dh.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), pre.data_ptr(), _ptr(dx), _ptr(dw[0]),
+              _ptr(dw[1]), M, C, F, _Strides7(ld_dh, ld_x, ld_g, ld_u, C, C, C), act, ws.data_ptr())
+    if stream is not None:
         _record(ws, s)
     return dx, dw[0], dw[1]
 
@@ -332,7 +317,6 @@ def gated_ff_backward(dh, x, w_gate, w_up, pre, activation="silu", need=(True, T
 
 def adamw_state(param, state_bits=32):
     """Zero states of a parameter: (m, v) fp32 of its shape, or for 8 bits (m int8, v uint8, (m_scale, v_scale) fp32 [ceil(n / 256)])."""
-    import torch
     if state_bits == 32:
         return torch.zeros_like(param, dtype=torch.float32), torch.zeros_like(param, dtype=torch.float32)
     if state_bits != 8:
@@ -342,41 +326,52 @@ def adamw_state(param, state_bits=32):
     return torch.zeros_like(param, dtype=torch.int8), torch.zeros_like(param, dtype=torch.uint8), scales
 
 
-def _describe(entry, p, m, v, master, scales, eight):
-    import torch
-    states = (torch.int8, torch.uint8) if eight else (torch.float32, torch.float32)
-    n = p.numel()
-    if not (m.dtype == states[0] and v.dtype == states[1] and m.numel() == n and v.numel() == n):
-        _refuse("states must have the parameter's size and be fp32, or int8 and uint8 with scales")
-    if master is not None and (master.dtype != torch.float32 or master.numel() != n):
-        _refuse("a master must be fp32 and of its parameter's size")
-    if eight and any(s.dtype != torch.float32 or s.numel() != -(-n // STATE_BLOCK) for s in scales):
-        _refuse("scales must be fp32, one for every 256 elements")
-    _on_device(p, param=p, m=m, v=v, master=master, m_scale=scales[0] if eight else None, v_scale=scales[1] if eight else None)
-    for t in (p, m, v, master) + (tuple(scales) if eight else ()):
-        if t is not None and not t.is_contiguous():
-            _refuse("parameters, states and scales must be contiguous")
-    entry.param, entry.m, entry.v, entry.n = p.data_ptr(), m.data_ptr(), v.data_ptr(), n
-    entry.master = _ptr(master)
-    if eight:
-        entry.m_scale, entry.v_scale = scales[0].data_ptr(), scales[1].data_ptr()
+def _table(params, exp_avgs, exp_avg_sqs, masters, scales):
+    """The descriptors of a call, gradients left out."""
+    first, table = params[0], (AdamWTensor * len(params))()
+    if not first.is_cuda:
+        _refuse("parameters must be device tensors")
+    dtype, device = first.dtype, first.get_device()
+    eight = scales is not None
+    m_type, v_type = (torch.int8, torch.uint8) if eight else (torch.float32, torch.float32)
+    f32 = torch.float32
+    for i, p in enumerate(params):
+        m, v, n = exp_avgs[i], exp_avg_sqs[i], p.numel()
+        if p.dtype != dtype or p.get_device() != device:
+            _refuse("the parameters of a call must be of one dtype and on one device", CLEAR_ERR_MISMATCH)
+        if not (m.dtype == m_type and v.dtype == v_type and m.numel() == n and v.numel() == n and m.get_device() == device and v.get_device() == device):
+            _refuse("states must be on the parameter's device, of its size, and fp32, or int8 and uint8 with scales")
+        if not (p.is_contiguous() and m.is_contiguous() and v.is_contiguous()):
+            _refuse("parameters and states must be contiguous")
+        e = table[i]
+        e.param, e.m, e.v, e.n = p.data_ptr(), m.data_ptr(), v.data_ptr(), n
+        if masters is not None:
+            w = masters[i]
+            if not (w.dtype == f32 and w.numel() == n and w.get_device() == device and w.is_contiguous()):
+                _refuse("a master must be contiguous fp32, of its parameter's size and on its device")
+            e.master = w.data_ptr()
+        if eight:
+            for s in scales[i]:
+                if not (s.dtype == f32 and s.numel() == -(-n // STATE_BLOCK) and s.get_device() == device and s.is_contiguous()):
+                    _refuse("scales must be contiguous fp32, one for every 256 elements, on the parameter's device")
+            e.m_scale, e.v_scale = scales[i][0].data_ptr(), scales[i][1].data_ptr()
+    return table
 
 
-def _grad(entry, p, g):
-    if g is None:
-        entry.grad = None
-        return
-    if not (g.shape == p.shape and g.dtype == p.dtype and g.device == p.device and g.is_contiguous()):
-        _refuse("a gradient must be contiguous and have its parameter's shape, dtype and device")
-    entry.grad = g.data_ptr()
+def _set_grads(table, params, grads):
+    for e, p, g in zip(table, params, grads):
+        if g is None:
+            e.grad = None
+        elif g.shape == p.shape and g.dtype == p.dtype and g.get_device() == p.get_device() and g.is_contiguous():
+            e.grad = g.data_ptr()
+        else:
+            _refuse("a gradient must be contiguous and have its parameter's shape, dtype and device")
 
 
-def _launch(table, count, dtype, device, eight, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream):
-    import torch
-    if grad_scale is not None and not (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == device):
+def _launch(table, first, eight, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream):
+    if grad_scale is not None and not (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == first.device):
         _refuse("grad_scale must be one fp32 value on the parameters' device")
-    with _On(device, stream) as s:
-        _check(lib().clear_block_adamw(count, table, dtype, 8 if eight else 32, lr, beta1, beta2, eps, weight_decay, step, _ptr(grad_scale), s))
+    _call("clear_block_adamw", first.device, stream, len(table), table, ca._dtype_code(first), 8 if eight else 32, lr, beta1, beta2, eps, weight_decay, step, _ptr(grad_scale))
 
 
 def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, masters=None, scales=None,
@@ -389,30 +384,20 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1=0.9, beta2=
         _refuse("the lists must have one entry for each parameter", CLEAR_ERR_MISMATCH)
     if count == 0:
         return
-    table = (AdamWTensor * count)()
-    first = params[0]
-    for i in range(count):
-        p = params[i]
-        if p.dtype != first.dtype or p.device != first.device:
-            _refuse("the parameters of a call must be of one dtype and on one device", CLEAR_ERR_MISMATCH)
-        _describe(table[i], p, exp_avgs[i], exp_avg_sqs[i], None if masters is None else masters[i], None if scales is None else scales[i], scales is not None)
-        _grad(table[i], p, grads[i])
-    if not first.is_cuda:
-        _refuse("parameters must be device tensors")
-    _launch(table, count, ca._dtype_code(first), first.device, scales is not None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream)
+    table = _table(params, exp_avgs, exp_avg_sqs, masters, scales)
+    _set_grads(table, params, grads)
+    _launch(table, params[0], scales is not None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream)
 
 
 def adamw_decode(m, m_scale, v, v_scale, stream=None):
     """clear_block_adamw_decode: the fp32 values of 8-bit states m (int8, with its scales) and v (uint8, with its scales)."""
-    import torch
     n = m.numel()
     blocks = -(-n // STATE_BLOCK)
     if not (m.dtype == torch.int8 and v.dtype == torch.uint8 and v.numel() == n and all(s.dtype == torch.float32 and s.numel() == blocks for s in (m_scale, v_scale))):
         _refuse("m must be int8, v uint8 of its size, scales fp32, one for every 256 elements")
-    _on_device(m, m=m, v=v, m_scale=m_scale, v_scale=v_scale)
+    _on_device(m, v, m_scale, v_scale)
     if not all(t.is_contiguous() for t in (m, v, m_scale, v_scale)):
         _refuse("states and scales must be contiguous")
     out = [torch.empty(m.shape, dtype=torch.float32, device=m.device) for _ in range(2)]
-    with _On(m.device, stream) as s:
-        _check(lib().clear_block_adamw_decode(m.data_ptr(), m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), n, s))
+    _call("clear_block_adamw_decode", m.device, stream, m.data_ptr(), m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), n)
     return out[0], out[1]

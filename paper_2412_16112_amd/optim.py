@@ -27,15 +27,12 @@ class AdamW:
         self._tables = []
         places = {}
         for i, p in enumerate(self.params):
-            if not p.is_cuda:
-                raise ca.ClearAttnError(ca.CLEAR_ERR_INVALID_ARG, "parameters must be device tensors")
-            places.setdefault((p.device, ca._dtype_code(p)), []).append(i)
-        for (device, dtype), members in places.items():
-            table = (cb.AdamWTensor * len(members))()
-            for entry, i in zip(table, members):
-                cb._describe(entry, self.params[i].detach(), self.exp_avgs[i], self.exp_avg_sqs[i], self.masters[i] if masters else None,
-                             self.scales[i] if state_bits == 8 else None, state_bits == 8)
-            self._tables.append((device, dtype, members, table))
+            places.setdefault((p.device, p.dtype), []).append(i)
+        for members in places.values():
+            of = lambda kept: None if kept is None else [kept[i] for i in members]
+            params = [self.params[i].detach() for i in members]
+            ca._dtype_code(params[0])
+            self._tables.append((members, params, cb._table(params, of(self.exp_avgs), of(self.exp_avg_sqs), of(self.masters), of(self.scales))))
 
     def step(self, grads=None, grad_scale=None, stream=None, **hyper):
         """One step with the parameters' .grad, or with `grads` (a list in their order); entries that are None are skipped.  Keyword arguments
@@ -44,16 +41,13 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
         h = dict(self.hyper, **hyper)
-        for _, _, members, table in self._tables:  # (everything is checked before anything is updated)
-            for entry, i in zip(table, members):
-                p = self.params[i]
-                if p.data_ptr() != entry.param:
-                    raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "parameter %d has moved since the optimizer was made" % i)
-                cb._grad(entry, p, grads[i])
+        for members, params, table in self._tables:  # (everything is checked before anything is updated)
+            if any(self.params[i].data_ptr() != p.data_ptr() for i, p in zip(members, params)):
+                raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "a parameter has moved since the optimizer was made")
+            cb._set_grads(table, params, [grads[i] for i in members])
         self.steps += 1
-        for device, dtype, members, table in self._tables:
-            cb._launch(table, len(members), dtype, device, self.state_bits == 8, self.steps, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"],
-                       grad_scale, stream)
+        for members, params, table in self._tables:
+            cb._launch(table, params[0], self.state_bits == 8, self.steps, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], grad_scale, stream)
 
     def zero_grad(self):
         for p in self.params:
