@@ -112,7 +112,7 @@ long long clear_block_gated_ff_workspace(long long tokens, int channels, int hid
 
 /* ---- AdamW --------------------------------------------------------------------------------------------------------------
  *
- * One optimizer step over n_tensors tensors in one launch per 48 of them.  For every element, in fp32,
+ * One optimizer step over n_tensors tensors in one launch per 56 of them.  For every element, in fp32,
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * with g multiplied by *grad_scale first where grad_scale (a device fp32 scalar: a clipping factor) is not NULL.  param and grad are of

@@ -56,7 +56,7 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream);
 size_t gated_workspace_bytes(long long tokens, int channels, int hidden);
 
 // ---- AdamW
-constexpr int kAdamTensors = 48;  // descriptors that fit the 4 KB of a launch's arguments
+constexpr int kAdamTensors = 56;  // as many descriptors as fit the 4 KB of a launch's arguments
 constexpr int kAdamBlock = 256;   // elements that share a scale of 8-bit states
 struct AdamHyper {
     float beta1, one_minus_beta1, beta2, one_minus_beta2, keep, step_size, inv_root_correction, eps;
@@ -136,21 +136,26 @@ struct Chunk8<float> {
     }
 };
 
-// Sum over the wave, in every lane (exchanges inside rows of 16 lanes, then between rows: no LDS).
+// join over the wave's values, in every lane (exchanges inside rows of 16 lanes, then between rows: no LDS).
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float x, F&& join)
+{
+    const auto beside = [](float v, auto ctrl) {
+        constexpr int c = ctrl;
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), c, 0xf, 0xf, true));
+    };
+    x = join(x, beside(x, std::integral_constant<int, 0xb1>{}));   // lane ^ 1
+    x = join(x, beside(x, std::integral_constant<int, 0x4e>{}));   // lane ^ 2
+    x = join(x, beside(x, std::integral_constant<int, 0x141>{}));  // the other half of 8 lanes
+    x = join(x, beside(x, std::integral_constant<int, 0x140>{}));  // the other half of 16
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = join(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return join(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
 __device__ __forceinline__ float wave_sum(float x)
 {
-    const auto add = [](float v, auto ctrl) {
-        constexpr int c = ctrl;
-        return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), c, 0xf, 0xf, true));
-    };
-    x = add(x, std::integral_constant<int, 0xb1>{});   // lane ^ 1
-    x = add(x, std::integral_constant<int, 0x4e>{});   // lane ^ 2
-    x = add(x, std::integral_constant<int, 0x141>{});  // the other half of 8 lanes
-    x = add(x, std::integral_constant<int, 0x140>{});  // the other half of 16
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    return wave_reduce(x, [](float a, float b) { return a + b; });
 }
 
 }  // namespace block

@@ -1,4 +1,4 @@
-"""AdamW over the parameters of a model, one launch for every 48 of them (clear_block_adamw).
+"""AdamW over the parameters of a model, one launch for every 56 of them (clear_block_adamw).
 
     from paper_2412_16112_amd.optim import AdamW
     opt = AdamW(model.parameters(), lr=1e-4, weight_decay=0.01, state_bits=8)
