@@ -47,11 +47,11 @@ __device__ __forceinline__ int turn_of(int row) { return (row >> 1) & 7; }
 // different banks, those of the neighbouring 16 lanes (the granule beside) too.
 __device__ __forceinline__ int spread(int k) { return (k & 3) ^ ((k & 1) << 2); }
 
-template <int KIND, int WA, int WB, int NB>
+template <int KIND, int WA, int WB, int NB, int RING>
 struct Shape {
     static constexpr int TA = 64 * WA, TB = 32 * NB * WB, WAVES = WA * WB, THREADS = 64 * WAVES;
     static constexpr bool A_COLUMNS = KIND != kForward, B_COLUMNS = KIND == kWeightGrad;
-    static constexpr int A_BYTES = TA * 2 * kStep, B_BYTES = TB * 2 * kStep, STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
+    static constexpr int A_BYTES = TA * 2 * kStep, B_BYTES = TB * 2 * kStep, STAGE = A_BYTES + B_BYTES, LDS = RING * STAGE;
     static constexpr int A_LOADS = TA / 8 / WAVES, B_LOADS = TB / 8 / WAVES;  // instructions a wave, 1 KB each
     static_assert(TA / 8 % WAVES == 0 && TB / 8 % WAVES == 0, "the waves share the loads of a stage evenly");
 };
@@ -66,6 +66,7 @@ struct TileArgs {
     __bf16 *out0, *out1;   // the output, and where its rows from rows_out0 on go (weight gradient)
     long long ld_out0, ld_out1, rows_out0;
     float* pre;
+    float* parts;  // where the contraction is split: fp32 [gridDim.y][rows_b][rows_a], to be joined; else null
 };
 
 // 1 / (1 + 2^e).  The hardware's exponential and reciprocal, each good to an ulp or two, are far below the rounding of the result to bf16; an IEEE division
@@ -113,10 +114,10 @@ __device__ __forceinline__ void tile_of(unsigned id, unsigned n, int tiles_a, in
     *tile_b = (int)(band * BAND + in % width);
 }
 
-template <int KIND, int WA, int WB, int NB>
+template <int KIND, int WA, int WB, int NB, int RING>
 __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
 {
-    typedef Shape<KIND, WA, WB, NB> S;
+    typedef Shape<KIND, WA, WB, NB, RING> S;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds_bytes[];
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_bytes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -127,7 +128,9 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     // origin of the tile; forward: the tile's A rows are TA / 2 rows of the gate weight and the same of the up weight
     const int a_first = tile_a * (KIND == kForward ? S::TA / 2 : S::TA);
     const long long b_first = (long long)tile_b * S::TB;
-    const int steps_each = (int)((t.depth + kStep - 1) / kStep), steps = KIND == kInputGrad ? 2 * steps_each : steps_each;
+    const int steps_each = (int)((t.depth + kStep - 1) / kStep), steps_all = KIND == kInputGrad ? 2 * steps_each : steps_each;
+    const int it_first = (int)((long long)steps_all * blockIdx.y / gridDim.y), it_end = (int)((long long)steps_all * (blockIdx.y + 1) / gridDim.y);
+    const int steps = it_end - it_first;  // of this part of the contraction
 
     // ---- loads of a stage: instruction i of this wave is i-th of its share of A's, then of B's
     constexpr int A_CHUNKS = S::TA / 8, B_CHUNKS = S::TB / 8;  // 16-byte chunks of a contraction row where an operand is stored across
@@ -149,11 +152,12 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
         buf_a = buffer_of((up ? a1 : a0) + a_first * ld_a_rows, ((min((long long)t.rows_a - a_first, (long long)S::TA / 2) - 1) * ld_a_rows + t.depth) * 2);
     const long long b_bytes = ((min(t.rows_b - b_first, (long long)S::TB) - 1) * t.ld_b0 + t.depth) * 2;
     // What the loads of stage `it` have in common.  Along the contraction the buffer stays and the offset moves; across, the buffer moves.
-    auto aim = [&](int it) {
-        lds_to = lds + (it & 1) * S::STAGE;
+    auto aim = [&](int step, unsigned stage) {
+        const int it = it_first + step;
+        lds_to = lds + stage;
         const bool upper = KIND == kInputGrad && it >= steps_each;
         const long long k0 = (long long)(upper ? it - steps_each : it) * kStep;
-        k_left = (int)max(min(t.depth - k0, (long long)kStep), 0LL);  // 0: no such stage
+        k_left = it < it_end ? (int)min(t.depth - k0, (long long)kStep) : 0;  // 0: no such stage, nothing is read
         k_bytes = (unsigned)(k0 * 2);
         if (S::A_COLUMNS) {
             ld_a = upper ? ld_a1 : ld_a0;
@@ -189,8 +193,8 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
                 load_rows(buf_b, n, i & 1, t.ld_b0, lds_to + S::A_BYTES);
         }
     };
-    auto issue = [&](int it) {
-        aim(it);
+    auto issue = [&](int step, unsigned stage) {
+        aim(step, stage);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) load(i);
     };
@@ -262,10 +266,12 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // this wave's loads have arrived and its reads are done; after the barrier everybody's
-    auto settle = [] {
+    // All but `more` of this wave's loads have arrived and its reads are done; after the barrier everybody's.
+    auto settle = [](auto more) {
+        constexpr int n = more;
+        static_assert(n < 64, "vmcnt is 6 bits");
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt 0, lgkmcnt 0, expcnt unconstrained
+        __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | (n >> 4) << 14);  // lgkmcnt 0, expcnt unconstrained
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -278,31 +284,33 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
             interleave();
         }
     };
-    // The loads of the stage after the last fall outside their buffers, all of them: nothing is read, and the loop has no branch for them.
+    // The loads of the stages after the last fall outside their buffers, all of them: nothing is read, and the loop has no branch for them.
     if (steps > 0) {
-        issue(0);
-        settle();
-        issue(1);
+#pragma unroll
+        for (int i = 0; i < RING; ++i) issue(i, i * S::STAGE);
+        settle(std::integral_constant<int, (RING - 1) * LOADS>{});
         read(0, 0, 0);
+        unsigned stage = 0;
         for (int it = 0; it + 1 < steps; ++it) {
-            const unsigned stage = (it & 1) * S::STAGE;
+            const unsigned next = stage + S::STAGE == S::LDS ? 0 : stage + S::STAGE;
             slots(stage);
-            settle();
+            settle(std::integral_constant<int, (RING - 2) * LOADS>{});
             __builtin_amdgcn_sched_barrier(0);
-            read(0, S::STAGE - stage, 0);
-            aim(it + 2);
+            read(0, next, 0);
+            aim(it + RING, stage);
             constexpr int PRODUCTS = 2 * NB;
 #pragma unroll
-            for (int n = 0; n < PRODUCTS; ++n) {  // loads into the stage just read, each beside a product
+            for (int n = 0; n < PRODUCTS; ++n) {  // loads into the stage just read, beside the products
                 product((SLOTS - 1) & 1, n);
 #pragma unroll
                 for (int i = n * LOADS / PRODUCTS; i < (n + 1) * LOADS / PRODUCTS; ++i) load(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            stage = next;
         }
-        slots(((steps - 1) & 1) * S::STAGE);
+        slots(stage);
         multiply((SLOTS - 1) & 1);
-        settle();  // (nothing may still be on its way to this workgroup's LDS when it ends)
+        settle(std::integral_constant<int, 0>{});  // (nothing may still be on its way to this workgroup's LDS when it ends)
     }
 
     // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Lanes l and l + 32 hold the
@@ -351,6 +359,15 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
                     }
                 }
             }
+        } else if (in && t.parts) {
+            float* const out = t.parts + (blockIdx.y * t.rows_b + row) * t.rows_a;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = a_first + 64 * wa + 32 * i + 8 * q + 4 * (lane >> 5);
+                    if (c < t.rows_a) *(f32x4*)(out + c) = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                }
         } else if (in) {
             const bool second = KIND == kWeightGrad && row >= t.rows_out0;
             __bf16* const out = second ? t.out1 + (row - t.rows_out0) * t.ld_out1 : t.out0 + row * t.ld_out0;
@@ -467,40 +484,106 @@ __global__ void __launch_bounds__(256) gated_gradient_kernel(const GatedArgs g, 
     *(bf16x8*)(ws + row * 2 * g.hidden + g.hidden + c) = du;
 }
 
-template <int KIND, int WA, int WB, int NB>
-hipError_t launch_tiles(TileArgs t, hipStream_t stream)
+// The sum of the parts of a split contraction, in order, to the output; 8 outputs a thread.
+__global__ void __launch_bounds__(256) join_kernel(const TileArgs t, int parts, long long n)
 {
-    typedef Shape<KIND, WA, WB, NB> S;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= n) return;
+    const int each = t.rows_a / 8;
+    const long long row = id / each, plane = t.rows_b * t.rows_a;
+    const int c = (int)(id - row * each) * 8;
+    const float* const from = t.parts + row * t.rows_a + c;
+    f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
+#pragma unroll 4
+    for (int p = 1; p < parts; ++p) {
+        lo += *(const f32x4*)(from + p * plane);
+        hi += *(const f32x4*)(from + p * plane + 4);
+    }
+    bf16x8 o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (__bf16)(j < 4 ? lo[j & 3] : hi[j & 3]);
+    const bool second = t.out1 && row >= t.rows_out0;
+    *(bf16x8*)((second ? t.out1 + (row - t.rows_out0) * t.ld_out1 : t.out0 + row * t.ld_out0) + c) = o;
+}
+
+template <int KIND, int WA, int WB, int NB, int RING>
+hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
+{
+    typedef Shape<KIND, WA, WB, NB, RING> S;
     const int a_rows = KIND == kForward ? S::TA / 2 : S::TA;
     t.tiles_a = (t.rows_a + a_rows - 1) / a_rows;
     const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB;
     if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffffffffLL / S::THREADS) return hipErrorInvalidValue;
     t.tiles_b = (int)tiles_b;
+    if (parts == 1) t.parts = nullptr;
     static const hipError_t limit =
-        hipFuncSetAttribute((const void*)tile_kernel<KIND, WA, WB, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+        hipFuncSetAttribute((const void*)tile_kernel<KIND, WA, WB, NB, RING>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     if (limit != hipSuccess) return limit;
-    tile_kernel<KIND, WA, WB, NB><<<dim3((unsigned)(tiles_b * t.tiles_a)), dim3(S::THREADS), S::LDS, stream>>>(t);
+    tile_kernel<KIND, WA, WB, NB, RING><<<dim3((unsigned)(tiles_b * t.tiles_a), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || parts == 1) return e;
+    const long long n = t.rows_b * (t.rows_a / 8), blocks = (n + 255) / 256;
+    if (blocks > 0xffffffffLL / 256) return hipErrorInvalidValue;
+    join_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(t, parts, n);
     return hipGetLastError();
 }
 
-template <int KIND>
-hipError_t launch_shape(const TileArgs& t, hipStream_t stream)
+// Tile shape and number of parts that the contraction is split into, by the time they are expected to take: rounds of workgroups over the 256 CUs, each of a
+// part's steps (64 of the contraction) and of what a tile costs beside (first loads, epilogue).  The constants, in us, were fitted to 700 timings of the three products
+// in all three shapes and 1 to 16 parts, at 100 to 8192 tokens and widths of 1000 x 2048 to 4096 x 11264: the chosen form takes up to 5 % longer than the
+// best of them, 1 % on average.  (At 2432 x 6528 dX of 100 tokens takes 267 us in 256 x 256 tiles, 120 in deep ones and 28 in those with the contraction in 12 parts; of
+// 4608 tokens 285 in 256 x 256 tiles and 335 in small ones.)
+enum TileShape { kLarge, kPair, kDeep };  // 256 x 256; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
+struct Plan {
+    TileShape shape;
+    int parts;
+};
+Plan plan_of(int kind, long long rows_a, long long rows_b, long long depth)
 {
-    // Rounds over the 256 CUs, in the time that a CU takes for a 256 x 256 tile: it runs two of 128 x 128 at once, at a lower rate.
-    const int half = KIND == kForward ? 2 : 1;
-    const long long large = ((long long)t.rows_a * half + 255) / 256 * ((t.rows_b + 255) / 256);
-    const long long small = ((long long)t.rows_a * half + 127) / 128 * ((t.rows_b + 127) / 128);
-    const double large_cost = (double)((large + 255) / 256), small_cost = 0.62 * (double)((small + 511) / 512);
-    return large_cost <= small_cost ? launch_tiles<KIND, 4, 2, 4>(t, stream) : launch_tiles<KIND, 2, 2, 2>(t, stream);
+    const long long a = kind == kForward ? 2 * rows_a : rows_a, steps = (depth + kStep - 1) / kStep * (kind == kInputGrad ? 2 : 1);
+    const auto up = [](long long x, long long by) { return (x + by - 1) / by; };
+    const long long large = up(a, 256) * up(rows_b, 256), small = up(a, 128) * up(rows_b, 128);
+    Plan best = {kLarge, 1};
+    double best_us = 0;
+    for (int parts = 1; parts <= (kind == kForward ? 1 : 16); ++parts) {
+        if (parts > 1 && steps < 8 * parts) break;
+        const double each = (double)up(steps, parts);
+        // (the parts are written and read once more)
+        const double join = parts == 1 ? 0 : 2.8 + (1.265 * parts + 0.5) * rows_a * rows_b * 4 / 4e6;
+        const double us[3] = {up(large * parts, 256) * (each * 1.38 + 9.0) + join,
+                              (small * parts <= 256 ? each * 0.612 + 6.3 : up(small * parts, 512) * (each * 0.893 + 6.3)) + join,  // (a CU to itself where there are enough)
+                              up(small * parts, 256) * (each * 0.52 + 6.9) + join};
+        for (int s = 0; s < 3; ++s)
+            if (best_us == 0 || us[s] < best_us) {
+                best_us = us[s];
+                best = {(TileShape)s, parts};
+            }
+    }
+    return best;
+}
+Plan input_plan(long long tokens, int channels, int hidden) { return plan_of(kInputGrad, channels, tokens, hidden); }
+Plan weight_plan(long long tokens, int channels, int hidden) { return plan_of(kWeightGrad, channels, 2LL * hidden, tokens); }
+
+template <int KIND>
+hipError_t launch_plan(const TileArgs& t, const Plan& p, hipStream_t stream)
+{
+    if (p.shape == kLarge) return launch_tiles<KIND, 4, 2, 4, 2>(t, p.parts, stream);
+    return p.shape == kPair ? launch_tiles<KIND, 2, 2, 2, 2>(t, p.parts, stream) : launch_tiles<KIND, 2, 2, 2, 4>(t, p.parts, stream);
 }
 
-constexpr int kFewTokens = 64;
+// Whether the form for few tokens is the faster one: it reads X again for every 16 hidden channels, so its time grows with tokens and weights together (us at 25, 63 and 184 MB
+// of weights: 16 tokens 13, 16, 47; 32 tokens 13, 20, 56; 64 tokens 13, 28, 78), that of the tiles up to 128 tokens with the weights alone (17, 24, 44).
+bool few_tokens(const GatedArgs& a)
+{
+    const double megabytes = 4e-6 * a.channels * a.hidden;
+    return a.tokens <= 16 || (a.tokens <= 32 && megabytes <= 96) || (a.tokens <= 64 && megabytes <= 48);
+}
 
 }  // namespace
 
 hipError_t launch_gated_forward(const GatedArgs& a, hipStream_t stream)
 {
-    if (a.tokens <= kFewTokens) {
+    if (few_tokens(a)) {
         const dim3 grid((a.hidden + 15) / 16), block(64 * kFewWaves);
         if (a.tokens <= 16) few_tokens_kernel<1><<<grid, block, 0, stream>>>(a);
         else if (a.tokens <= 32) few_tokens_kernel<2><<<grid, block, 0, stream>>>(a);
@@ -514,19 +597,25 @@ hipError_t launch_gated_forward(const GatedArgs& a, hipStream_t stream)
     t.act = a.act;
     t.out0 = (__bf16*)a.h, t.ld_out0 = a.ld_h;
     t.pre = a.pre;
-    return launch_shape<kForward>(t, stream);
+    return launch_plan<kForward>(t, plan_of(kForward, t.rows_a, t.rows_b, t.depth), stream);
 }
+
+// dG and dU at the head of the workspace.
+static size_t gradient_bytes(long long tokens, int hidden) { return (size_t)tokens * hidden * 4; }
 
 size_t gated_workspace_bytes(long long tokens, int channels, int hidden)
 {
-    (void)channels;
-    return (size_t)tokens * hidden * 4;  // dG and dU
+    if (tokens == 0) return 0;
+    const int in = input_plan(tokens, channels, hidden).parts, w = weight_plan(tokens, channels, hidden).parts;
+    const size_t in_bytes = in > 1 ? (size_t)in * tokens * channels * 4 : 0, w_bytes = w > 1 ? (size_t)w * 2 * hidden * channels * 4 : 0;
+    return gradient_bytes(tokens, hidden) + std::max(in_bytes, w_bytes);  // dG and dU, then the parts of one of the products at a time
 }
 
 hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
 {
     const __bf16* const dg = (const __bf16*)a.ws;
     const __bf16* const du = dg + a.hidden;
+    float* const parts = (float*)((unsigned char*)a.ws + gradient_bytes(a.tokens, a.hidden));  // (16-byte aligned: hidden is a multiple of 8)
     hipError_t e = hipSuccess;
     if (a.tokens > 0) {
         const long long n = a.tokens * (a.hidden / 8), blocks = (n + 255) / 256;
@@ -540,7 +629,8 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
         t.ld_a0 = a.ld_g, t.ld_a1 = a.ld_u, t.ld_b0 = 2LL * a.hidden;
         t.rows_a = a.channels, t.rows_b = a.tokens, t.depth = a.hidden;
         t.out0 = (__bf16*)a.dx, t.ld_out0 = a.ld_dx;
-        e = launch_shape<kInputGrad>(t, stream);
+        t.parts = parts;
+        e = launch_plan<kInputGrad>(t, input_plan(a.tokens, a.channels, a.hidden), stream);
     }
     if (e == hipSuccess && a.dwg) {
         TileArgs t = {};
@@ -550,7 +640,8 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t stream)
         t.rows_out0 = a.hidden;
         t.out0 = (__bf16*)a.dwg, t.ld_out0 = a.ld_dwg;
         t.out1 = (__bf16*)a.dwu, t.ld_out1 = a.ld_dwu;
-        e = launch_shape<kWeightGrad>(t, stream);
+        t.parts = parts;
+        e = launch_plan<kWeightGrad>(t, weight_plan(a.tokens, a.channels, a.hidden), stream);
     }
     return e;
 }
