@@ -4,7 +4,9 @@ device memory, workspaces and streams; every step runs in the HIP kernels, and t
 
 Refusals raise ClearAttnError, as in clear_attn.  Each call enqueues on `stream` (default: torch's current stream of the tensors' device)."""
 import ctypes
+import operator
 
+import numpy as np
 import torch
 
 from . import clear_attn as ca
@@ -326,52 +328,59 @@ def adamw_state(param, state_bits=32):
     return torch.zeros_like(param, dtype=torch.int8), torch.zeros_like(param, dtype=torch.uint8), scales
 
 
+_dtype_of = operator.attrgetter("dtype")
+_device_of, _ptr_of, _numel, _contiguous = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous
+
+
+def _alike(tensors, dtype, device):
+    """Whether all are contiguous, of one dtype and on one device."""
+    return set(map(_dtype_of, tensors)) == {dtype} and set(map(_device_of, tensors)) == {device} and all(map(_contiguous, tensors))
+
+
 def _table(params, exp_avgs, exp_avg_sqs, masters, scales):
-    """The descriptors of a call, gradients left out."""
-    first, table = params[0], (AdamWTensor * len(params))()
+    """The descriptors of a call (rows of clear_block_adamw_tensor's eight words), gradients left out."""
+    first = params[0]
     if not first.is_cuda:
         _refuse("parameters must be device tensors")
-    dtype, device = first.dtype, first.get_device()
-    eight = scales is not None
-    m_type, v_type = (torch.int8, torch.uint8) if eight else (torch.float32, torch.float32)
-    f32 = torch.float32
-    for i, p in enumerate(params):
-        m, v, n = exp_avgs[i], exp_avg_sqs[i], p.numel()
-        if p.dtype != dtype or p.get_device() != device:
-            _refuse("the parameters of a call must be of one dtype and on one device", CLEAR_ERR_MISMATCH)
-        if not (m.dtype == m_type and v.dtype == v_type and m.numel() == n and v.numel() == n and m.get_device() == device and v.get_device() == device):
-            _refuse("states must be on the parameter's device, of its size, and fp32, or int8 and uint8 with scales")
-        if not (p.is_contiguous() and m.is_contiguous() and v.is_contiguous()):
-            _refuse("parameters and states must be contiguous")
-        e = table[i]
-        e.param, e.m, e.v, e.n = p.data_ptr(), m.data_ptr(), v.data_ptr(), n
-        if masters is not None:
-            w = masters[i]
-            if not (w.dtype == f32 and w.numel() == n and w.get_device() == device and w.is_contiguous()):
-                _refuse("a master must be contiguous fp32, of its parameter's size and on its device")
-            e.master = w.data_ptr()
-        if eight:
-            for s in scales[i]:
-                if not (s.dtype == f32 and s.numel() == -(-n // STATE_BLOCK) and s.get_device() == device and s.is_contiguous()):
-                    _refuse("scales must be contiguous fp32, one for every 256 elements, on the parameter's device")
-            e.m_scale, e.v_scale = scales[i][0].data_ptr(), scales[i][1].data_ptr()
+    device, n = first.get_device(), list(map(_numel, params))
+    if not _alike(params, first.dtype, device):
+        _refuse("the parameters of a call must be contiguous, of one dtype and on one device", CLEAR_ERR_MISMATCH)
+    m_type, v_type = (torch.float32, torch.float32) if scales is None else (torch.int8, torch.uint8)
+    if not (_alike(exp_avgs, m_type, device) and _alike(exp_avg_sqs, v_type, device) and list(map(_numel, exp_avgs)) == n and list(map(_numel, exp_avg_sqs)) == n):
+        _refuse("states must be contiguous, on the parameters' device, of their sizes, and fp32, or int8 and uint8 with scales")
+    table = np.zeros((len(n), 8), dtype=np.int64)
+    table[:, 0] = list(map(_ptr_of, params))
+    if masters is not None:
+        if not (_alike(masters, torch.float32, device) and list(map(_numel, masters)) == n):
+            _refuse("masters must be contiguous fp32, of their parameters' sizes and on their device")
+        table[:, 2] = list(map(_ptr_of, masters))
+    table[:, 3] = list(map(_ptr_of, exp_avgs))
+    table[:, 4] = list(map(_ptr_of, exp_avg_sqs))
+    if scales is not None:
+        blocks = [-(-k // STATE_BLOCK) for k in n]
+        for column, side in ((5, [s[0] for s in scales]), (6, [s[1] for s in scales])):
+            if not (_alike(side, torch.float32, device) and list(map(_numel, side)) == blocks):
+                _refuse("scales must be contiguous fp32, one for every 256 elements, on the parameters' device")
+            table[:, column] = list(map(_ptr_of, side))
+    table[:, 7] = n
     return table
 
 
 def _set_grads(table, params, grads):
-    for e, p, g in zip(table, params, grads):
-        if g is None:
-            e.grad = None
-        elif g.shape == p.shape and g.dtype == p.dtype and g.get_device() == p.get_device() and g.is_contiguous():
-            e.grad = g.data_ptr()
-        else:
-            _refuse("a gradient must be contiguous and have its parameter's shape, dtype and device")
+    have = [g for g in grads if g is not None]
+    if not have:
+        table[:, 1] = 0
+        return
+    of = params if len(have) == len(grads) else [p for p, g in zip(params, grads) if g is not None]
+    if not (_alike(have, of[0].dtype, of[0].get_device()) and all(g.shape == p.shape for g, p in zip(have, of))):
+        _refuse("a gradient must be contiguous and have its parameter's shape, dtype and device")
+    table[:, 1] = list(map(_ptr_of, have)) if len(have) == len(grads) else [0 if g is None else g.data_ptr() for g in grads]
 
 
 def _launch(table, first, eight, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream):
     if grad_scale is not None and not (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == first.device):
         _refuse("grad_scale must be one fp32 value on the parameters' device")
-    _call("clear_block_adamw", first.device, stream, len(table), table, ca._dtype_code(first), 8 if eight else 32, lr, beta1, beta2, eps, weight_decay, step, _ptr(grad_scale))
+    _call("clear_block_adamw", first.device, stream, len(table), table.ctypes.data, ca._dtype_code(first), 8 if eight else 32, lr, beta1, beta2, eps, weight_decay, step, _ptr(grad_scale))
 
 
 def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, masters=None, scales=None,
