@@ -6,6 +6,7 @@
 // An operand is stored along the contraction ("rows": X and the weights forward, dG and dU for dX) or across it ("columns": the weights
 // for dX, everything for the weight gradients); the latter are read from LDS with the 16-bit transpose load.
 #include <algorithm>
+#include <mutex>
 
 #include "block_internal.h"
 
@@ -506,6 +507,22 @@ __global__ void __launch_bounds__(256) join_kernel(const TileArgs t, int parts, 
     *(bf16x8*)((second ? t.out1 + (row - t.rows_out0) * t.ld_out1 : t.out0 + row * t.ld_out0) + c) = o;
 }
 
+// A kernel's limit of dynamic LDS is raised once for each device (it belongs to the device's copy of the kernel).
+struct LdsLimit {
+    static constexpr int kDevices = 64;
+    std::once_flag once[kDevices];
+    hipError_t result[kDevices] = {};
+    hipError_t ensure(const void* kernel, int bytes)
+    {
+        int device = 0;
+        const hipError_t e = hipGetDevice(&device);
+        if (e != hipSuccess) return e;
+        if (device < 0 || device >= kDevices) return hipErrorInvalidDevice;
+        std::call_once(once[device], [&] { result[device] = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+        return result[device];
+    }
+};
+
 template <int KIND, int WA, int WB, int NB, int RING>
 hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
 {
@@ -516,9 +533,9 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffffffffLL / S::THREADS) return hipErrorInvalidValue;
     t.tiles_b = (int)tiles_b;
     if (parts == 1) t.parts = nullptr;
-    static const hipError_t limit =
-        hipFuncSetAttribute((const void*)tile_kernel<KIND, WA, WB, NB, RING>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
-    if (limit != hipSuccess) return limit;
+    static LdsLimit limit;
+    const hipError_t allowed = limit.ensure((const void*)tile_kernel<KIND, WA, WB, NB, RING>, S::LDS);
+    if (allowed != hipSuccess) return allowed;
     tile_kernel<KIND, WA, WB, NB, RING><<<dim3((unsigned)(tiles_b * t.tiles_a), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts == 1) return e;
