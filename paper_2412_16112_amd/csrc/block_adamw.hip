@@ -168,24 +168,17 @@ __device__ __forceinline__ f32x4 encode_v(const f32x4& x, float* scale)
     return c;
 }
 
-template <typename T, bool EIGHT>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const Launch l)
+// A wave's groups: block, block + kWaves, ... of tensor t.  FULL: every one has all of its 256 elements (in the other form each access asks how many there are).
+template <typename T, bool EIGHT, bool FULL>
+__device__ __forceinline__ void adamw_groups(const Launch::Tensor& t, const AdamHyper& h, long long block, int lane)
 {
-    int lo = 0, hi = l.n;  // first[lo] <= blockIdx.x < first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (l.first[mid] <= blockIdx.x) lo = mid; else hi = mid;
-    }
-    const Launch::Tensor& t = l.t[lo];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const long long block = (long long)(blockIdx.x - l.first[lo]) * (kWaves * kGroups) + wave;  // this wave's groups: block, block + kWaves, ...
-    const float scale = l.h.grad_scale ? *l.h.grad_scale : 1.f;
+    const float scale = h.grad_scale ? *h.grad_scale : 1.f;
     f32x4 p[kGroups], g[kGroups], m[kGroups], v[kGroups];
     float ms[kGroups], vs[kGroups];
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
-        const long long at = (block + i * kWaves) * kAdamBlock + 4 * lane, left = t.n - at;
-        const bool any = (block + i * kWaves) * kAdamBlock < t.n;
+        const long long at = (block + i * kWaves) * kAdamBlock + 4 * lane, left = FULL ? 4 : t.n - at;
+        const bool any = FULL || (block + i * kWaves) * kAdamBlock < t.n;
         p[i] = t.master ? load4(t.master + at, left) : load4((const T*)t.param + at, left);
         g[i] = load4((const T*)t.grad + at, left);
         if (EIGHT) {
@@ -200,23 +193,25 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const Launch l)
     }
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
-        const long long at = (block + i * kWaves) * kAdamBlock + 4 * lane, left = t.n - at;
-        if ((block + i * kWaves) * kAdamBlock >= t.n) break;
+        const long long at = (block + i * kWaves) * kAdamBlock + 4 * lane, left = FULL ? 4 : t.n - at;
+        if (!FULL && (block + i * kWaves) * kAdamBlock >= t.n) break;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float gr = l.h.grad_scale ? g[i][j] * scale : g[i][j];
+            const float gr = h.grad_scale ? g[i][j] * scale : g[i][j];
             float mm = EIGHT ? decode_m(m[i][j], ms[i]) : m[i][j], vv = EIGHT ? decode_v(v[i][j], vs[i]) : v[i][j];
-            mm = mm * l.h.beta1 + gr * l.h.one_minus_beta1;
-            vv = vv * l.h.beta2 + (gr * gr) * l.h.one_minus_beta2;
-            const float denominator = sqrtf(vv) * l.h.inv_root_correction + l.h.eps;
-            p[i][j] = p[i][j] * l.h.keep - (mm / denominator) * l.h.step_size;
+            mm = mm * h.beta1 + gr * h.one_minus_beta1;
+            vv = vv * h.beta2 + (gr * gr) * h.one_minus_beta2;
+            const float denominator = sqrtf(vv) * h.inv_root_correction + h.eps;
+            p[i][j] = p[i][j] * h.keep - (mm / denominator) * h.step_size;
             m[i][j] = mm;
             v[i][j] = vv;
         }
         if (EIGHT) {
+            if (!FULL) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j >= left) m[i][j] = v[i][j] = 0.f;  // (what lies past the tensor's end has no say in the scale)
+                for (int j = 0; j < 4; ++j)
+                    if (j >= left) m[i][j] = v[i][j] = 0.f;  // (what lies past the tensor's end has no say in the scale)
+            }
             float s;
             const f32x4 mc = encode_m(m[i], &s);
             if (lane == 0) t.m_scale[block + i * kWaves] = s;
@@ -231,6 +226,23 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const Launch l)
         if (t.master) store4(t.master + at, left, p[i]);
         store4((T*)t.param + at, left, p[i]);
     }
+}
+
+template <typename T, bool EIGHT>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const Launch l)
+{
+    int lo = 0, hi = l.n;  // first[lo] <= blockIdx.x < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (l.first[mid] <= blockIdx.x) lo = mid; else hi = mid;
+    }
+    const Launch::Tensor& t = l.t[lo];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const long long block = (long long)(blockIdx.x - l.first[lo]) * (kWaves * kGroups) + wave;
+    if ((block + (kGroups - 1) * kWaves + 1) * kAdamBlock <= t.n)
+        adamw_groups<T, EIGHT, true>(t, l.h, block, lane);
+    else
+        adamw_groups<T, EIGHT, false>(t, l.h, block, lane);
 }
 
 __global__ void __launch_bounds__(kThreads) adamw_decode_kernel(const signed char* m, const float* ms, const unsigned char* v, const float* vs, float* m_out,
