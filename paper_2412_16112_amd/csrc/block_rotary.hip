@@ -52,7 +52,8 @@ __device__ __forceinline__ void store_some(T* p, int count, const typename Vec<T
         if (j < count) p[j] = v[j];
 }
 
-template <typename T, bool INTERLEAVED, typename P>
+// FULL: every unit has all of its channels.
+template <typename T, bool INTERLEAVED, typename P, bool FULL>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a, long long token_first, long long n_threads, int units, int turned_units, int heads_each)
 {
     constexpr int V = Vec<T>::n, PAIRS = INTERLEAVED ? V / 2 : V;
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a, long lon
     const bool turn = u < turned_units;
     // first channel, number of channels and, for the half layout, the distance to the other channel of a pair
     const int c0 = turn ? (INTERLEAVED ? V : PAIRS) * u : a.rot_dim + V * (u - turned_units);
-    const int count = turn ? (INTERLEAVED ? a.rot_dim - c0 : half - c0) : a.head_dim - c0;
+    const int count = FULL ? V : turn ? (INTERLEAVED ? a.rot_dim - c0 : half - c0) : a.head_dim - c0;
     float cs[PAIRS], sn[PAIRS];
     if (turn) {
         double at[4];
@@ -135,6 +136,7 @@ hipError_t launch(const RotaryArgs& a, hipStream_t stream)
 {
     constexpr int V = Vec<T>::n, PAIRS = INTERLEAVED ? V / 2 : V;
     const int turned = (a.rot_dim / 2 + PAIRS - 1) / PAIRS, units = turned + (a.copy ? (a.head_dim - a.rot_dim + V - 1) / V : 0);
+    const bool full = a.rot_dim / 2 % PAIRS == 0 && (!a.copy || (a.head_dim - a.rot_dim) % V == 0);
     const long long tokens = a.B * a.N;
     const int heads = a.Hq + a.Hk;
     // All heads of a token in one thread, so that its angles are formed once; fewer where that would leave CUs without work (under
@@ -146,8 +148,11 @@ hipError_t launch(const RotaryArgs& a, hipStream_t stream)
     const long long most = 0x7fffffffLL / 2 / units;  // tokens a launch can have
     for (long long first = 0; first < tokens; first += most) {
         const long long n = std::min(most, tokens - first) * units;
-        rotary_kernel<T, INTERLEAVED, P><<<dim3((unsigned)((n + kThreads - 1) / kThreads), (heads + heads_each - 1) / heads_each), dim3(kThreads), 0, stream>>>(
-            a, first, n, units, turned, heads_each);
+        const dim3 grid((unsigned)((n + kThreads - 1) / kThreads), (heads + heads_each - 1) / heads_each);
+        if (full)
+            rotary_kernel<T, INTERLEAVED, P, true><<<grid, dim3(kThreads), 0, stream>>>(a, first, n, units, turned, heads_each);
+        else
+            rotary_kernel<T, INTERLEAVED, P, false><<<grid, dim3(kThreads), 0, stream>>>(a, first, n, units, turned, heads_each);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
