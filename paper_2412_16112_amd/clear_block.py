@@ -73,9 +73,13 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# Handle of torch's current stream of a device, without the Stream object around it (2 us a call) where torch offers that.
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(name, device, stream, *args):
     """The C function on the tensors' device and on `stream` (a handle; None: torch's current stream of that device).  Returns the stream's handle."""
-    s = torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+    s = _current(device.index) if stream is None else stream
     f = getattr(_lib or lib(), name)
     if torch.cuda.current_device() == device.index:
         status = f(*args, s)
