@@ -2,7 +2,8 @@
 positions, layer norm, gated feed-forward projection, AdamW step.  Argument marshalling only: PyTorch tensors are used for
 device memory, workspaces and streams; every step runs in the HIP kernels, and there is no fallback.
 
-Refusals raise ClearAttnError, as in clear_attn.  Each call enqueues on `stream` (default: torch's current stream of the tensors' device)."""
+Refusals raise ClearAttnError, as in clear_attn.  Each call enqueues on `stream` (default: torch's current stream of the tensors' device); with another
+one the caller orders it with torch's, before the call (results are allocated for torch's stream) and after it."""
 import ctypes
 import operator
 
