@@ -59,6 +59,8 @@ struct Shape {
     static constexpr int A_BYTES = TA * 2 * kStep, B_BYTES = TB * 2 * kStep, STAGE = A_BYTES + B_BYTES, LDS = RING * STAGE;
     static constexpr int A_LOADS = TA / 8 / WAVES, B_LOADS = TB / 8 / WAVES;  // instructions a wave, 1 KB each
     static_assert(TA / 8 % WAVES == 0 && TB / 8 % WAVES == 0, "the waves share the loads of a stage evenly");
+    static_assert((!A_COLUMNS || 512 % TA == 0) && (!B_COLUMNS || 512 % TB == 0), "an instruction fills whole contraction rows");
+    static_assert(A_LOADS % 2 == 0, "which of a wave's instructions for A are even ones of the tile is known in advance");
 };
 
 struct TileArgs {
@@ -140,7 +142,6 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     // ---- loads of a stage: instruction i of this wave is i-th of its share of A's, then of B's
     constexpr int A_CHUNKS = S::TA / 8, B_CHUNKS = S::TB / 8;  // 16-byte chunks of a contraction row where an operand is stored across
     constexpr int LOADS = S::A_LOADS + S::B_LOADS;
-    static_assert(S::A_LOADS % 2 == 0 && S::B_LOADS % 2 == 0, "whether a share's instruction is an even one of its tile is known in advance");
     i32x4 buf_a, buf_b;
     unsigned lds_to = 0, k_bytes = 0;
     int k_left = 0;
@@ -173,8 +174,8 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
         else
             buf_b = buffer_of((upper ? b1 : b0) + b_first * t.ld_b0, b_bytes);
     };
-    auto load_rows = [&](const i32x4& buf, int n, int even, long long ld, unsigned to) {
-        const int r = lane >> 3, c = (lane & 7) ^ turn_of(even * 8 + r);
+    auto load_rows = [&](const i32x4& buf, int n, int odd, long long ld, unsigned to) {
+        const int r = lane >> 3, c = (lane & 7) ^ turn_of(odd * 8 + r);
         const unsigned off = (unsigned)(r * ld * 2 + c * 16) + (unsigned)(n * 8 * ld * 2) + k_bytes;
         load_to_lds(buf, c * 8 < k_left ? off : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
     };
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
             if (S::B_COLUMNS)
                 load_columns(buf_b, n, B_CHUNKS, t.ld_b0, t.rows_b - b_first, lds_to + S::A_BYTES);
             else
-                load_rows(buf_b, n, i & 1, t.ld_b0, lds_to + S::A_BYTES);
+                load_rows(buf_b, n, S::B_LOADS % 2 ? n & 1 : i & 1, t.ld_b0, lds_to + S::A_BYTES);  // (known in advance where every wave has an even number)
         }
     };
     auto issue = [&](int step, unsigned stage) {
@@ -550,11 +551,11 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
 }
 
 // Tile shape and number of parts that the contraction is split into, by the time they are expected to take: rounds of workgroups over the 256 CUs, each of a
-// part's steps (64 of the contraction) and of what a tile costs beside (first loads, epilogue).  The constants, in us, were fitted to 700 timings of the three products
-// in all three shapes and 1 to 16 parts, at 100 to 8192 tokens and widths of 1000 x 2048 to 4096 x 11264: the chosen form takes up to 5 % longer than the
-// best of them, 1 % on average.  (At 2432 x 6528 dX of 100 tokens takes 267 us in 256 x 256 tiles, 120 in deep ones and 28 in those with the contraction in 12 parts; of
-// 4608 tokens 285 in 256 x 256 tiles and 335 in small ones.)
-enum TileShape { kLarge, kPair, kDeep };  // 256 x 256; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
+// part's steps (64 of the contraction) and of what a tile costs beside (first loads, epilogue).  The constants, in us, were fitted to 1100 timings of the three products
+// in all shapes and 1 to 16 parts, at 100 to 8192 tokens and widths of 512 x 1024 to 4096 x 11264: the chosen form takes up to 4 % longer than the
+// best of them, 1 % on average.  (At 2432 x 6528 dX of 100 tokens takes 169 us in 256 x 256 tiles, 22 in deep ones with the contraction in 12 parts; of 4608 tokens 297 in
+// 256 x 256 tiles, which leave 76 CUs without one, 268 in 256 x 192 and 332 in small ones.)
+enum TileShape { kLarge, kMedium, kPair, kDeep };  // 256 x 256; 256 x 192; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
 struct Plan {
     TileShape shape;
     int parts;
@@ -563,19 +564,19 @@ Plan plan_of(int kind, long long rows_a, long long rows_b, long long depth)
 {
     const long long a = kind == kForward ? 2 * rows_a : rows_a, steps = (depth + kStep - 1) / kStep * (kind == kInputGrad ? 2 : 1);
     const auto up = [](long long x, long long by) { return (x + by - 1) / by; };
-    const long long large = up(a, 256) * up(rows_b, 256), small = up(a, 128) * up(rows_b, 128);
+    const long long large = up(a, 256) * up(rows_b, 256), medium = up(a, 256) * up(rows_b, 192), small = up(a, 128) * up(rows_b, 128);
     Plan best = {kLarge, 1};
     double best_us = 0;
     for (int parts = 1; parts <= (kind == kForward ? 1 : 16); ++parts) {
         if (parts > 1 && steps < 8 * parts) break;
         const double each = (double)up(steps, parts);
         // (the parts are written and read once more)
-        const double join = parts == 1 ? 0 : 2.8 + (1.265 * parts + 0.5) * rows_a * rows_b * 4 / 4e6;
-        const double us[3] = {up(large * parts, 256) * (each * 1.38 + 9.0) + join,
-                              (small * parts <= 256 ? each * 0.612 + 6.3 : up(small * parts, 512) * (each * 0.893 + 6.3)) + join,  // (a CU to itself where there are enough)
-                              up(small * parts, 256) * (each * 0.52 + 6.9) + join};
-        for (int s = 0; s < 3; ++s)
-            if (best_us == 0 || us[s] < best_us) {
+        const double join = parts == 1 ? 0 : 3.37 + (1.14 * parts + 0.5) * rows_a * rows_b * 4 / 4e6;
+        const double us[4] = {up(large * parts, 256) * (each * 1.42 + 9.26) + join, up(medium * parts, 256) * (each * 1.11 + 7.45) + join,
+                              (small * parts <= 256 ? each * 0.625 + 6.43 : up(small * parts, 512) * (each * 0.893 + 6.43)) + join,  // (a CU to itself where there are enough)
+                              up(small * parts, 256) * (each * 0.512 + 7.22) + join};
+        for (int s = 0; s < 4; ++s)
+            if ((best_us == 0 || us[s] < best_us) && !(s == kMedium && kind == kWeightGrad)) {  // (stored across, 192 columns are no whole part of a load instruction)
                 best_us = us[s];
                 best = {(TileShape)s, parts};
             }
@@ -589,6 +590,8 @@ template <int KIND>
 hipError_t launch_plan(const TileArgs& t, const Plan& p, hipStream_t stream)
 {
     if (p.shape == kLarge) return launch_tiles<KIND, 4, 2, 4, 2>(t, p.parts, stream);
+    if constexpr (KIND != kWeightGrad)
+        if (p.shape == kMedium) return launch_tiles<KIND, 4, 2, 3, 2>(t, p.parts, stream);
     return p.shape == kPair ? launch_tiles<KIND, 2, 2, 2, 2>(t, p.parts, stream) : launch_tiles<KIND, 2, 2, 2, 4>(t, p.parts, stream);
 }
 
