@@ -78,7 +78,7 @@ int clear_block_layer_norm(const void* X, const void* weight, const void* bias, 
  *     dX = (dyw - mean(dyw) - xhat * mean(dyw * xhat)) / sqrt(var + eps),  dyw = dy * (weight_offset + weight),
  *     d_weight = sum dy * xhat,  d_bias = sum dy   over the rows (of a group with per_group, else of all groups; 0 for no rows),
  * the latter two laid out and typed like weight.  strides: (group, row) of dY, X, dX, 6 values; dX may be dY itself (same strides).
- * workspace: fp32, clear_block_layer_norm_workspace floats, needed for d_weight or d_bias. */
+ * workspace: fp32, clear_block_layer_norm_workspace floats, needed for d_weight or d_bias.  With per_group at most 65535 groups. */
 int clear_block_layer_norm_backward(const void* dY, const void* X, const void* weight, const float* stats, void* dX, void* d_weight,
                                     void* d_bias, long long groups, long long rows, int channels, const long long* strides,
                                     int per_group, float weight_offset, int dtype, int weight_dtype, float* workspace, void* stream);

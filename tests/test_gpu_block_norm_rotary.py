@@ -167,13 +167,6 @@ NORM = [  # B, N, C: one element, a lane's part, ragged ends, each number of wav
 ]
 
 
-def norm_slacks(x, w, offset, dy):
-    """(y, dx, dw, db) error bounds before the rounding of the outputs, from the magnitudes of the terms."""
-    weight = (offset + w.double().cpu()).abs() if w is not None else torch.ones(1, dtype=torch.float64)
-    weight = weight.unsqueeze(1) if weight.dim() == 2 else weight
-    return 3e-5 * (weight + 1), weight
-
-
 @pytest.mark.parametrize("types", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("shape", NORM)
 def test_layer_norm_and_its_gradients(shape, types):
