@@ -6,9 +6,9 @@
 // An operand is stored along the contraction ("rows": X and the weights forward, dG and dU for dX) or across it ("columns": the weights
 // for dX, everything for the weight gradients); the latter are read from LDS with the 16-bit transpose load.
 //
-// A tile is 256 x 256 for 8 waves of 64 x 128 (6 operand reads for 8 matrix instructions): at 16 717 x 2 432 x 9 728 forward 1.3 to 1.4 ms, 1.11 to 1.2 PFLOP/s, matrix pipe busy 60 % at
-// 1.78 GHz - at the part's power limit, where a deeper pipeline (stages of 32, four in flight) saved 4 % of the cycles and no time.  Four waves of 128 x 128 read a third less
-// from LDS but cannot issue everything beside their own products (+ 20 % time).  4 608 x 2 432 x 6 528 with the products kept: forward 328 us, dX 340, dWg and dWu 257.
+// The largest tile is 256 x 256 for 8 waves of 64 x 128 (6 operand reads for 8 matrix instructions): at 16 717 x 2 432 x 9 728 forward 1.3 to 1.4 ms, 1.12 to 1.2 PFLOP/s, matrix pipe busy
+// 60 % at 1.8 GHz - at the part's power limit, where a deeper pipeline (stages of 32, four in flight) saved 4 % of the cycles and no time.  Four waves of 128 x 128 read a third less
+// from LDS, but a CU then has one wave a SIMD and the epilogue nothing beside it (+ 25 % time).  4 608 x 2 432 x 6 528, forward with the products kept, dX, dWg and dWu: 890 us together.
 #include <algorithm>
 #include <mutex>
 
@@ -18,13 +18,27 @@ namespace clear {
 namespace block {
 namespace {
 
-constexpr int kStep = 64;  // of the contraction, a stage of LDS
+constexpr int kStep = 64;  // of the contraction: the measure of costs, and a stage of LDS of most shapes
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(4))) short short4v;
 typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_ptr;
 typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+#define INLINED __attribute__((always_inline))
+
 enum Kind { kForward, kInputGrad, kWeightGrad };
+
+// f(Int<FROM>{}), ..., f(Int<TO - 1>{}), in order.
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void each_of(F& f)
+{
+    if constexpr (FROM < TO) {
+        f(Int<FROM>{});
+        each_of<FROM + 1, TO>(f);
+    }
+}
 
 // ---- buffer loads to LDS ------------------------------------------------------------------------------------------------
 // A buffer descriptor bounds a load: what lies at or past `bytes` reads as 0 and nothing past it is touched.
@@ -35,32 +49,47 @@ __device__ __forceinline__ i32x4 buffer_of(const void* base, long long bytes)
     return i32x4{__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32)), __builtin_amdgcn_readfirstlane(size), 0x00020000};
 }
 constexpr unsigned kOutside = 0x80000000u;  // an offset past every buffer
-// 16 bytes a lane from buffer + voff to LDS at lds + 16 * lane (lds: wave-uniform); counted by vmcnt.  The whole offset is in the vector register, which
-// the bounds check looks at.  The wait states that the compiler does not put into asm: one between the write of M0 and the load, five after a
-// vector instruction that wrote its descriptor.
+// 16 bytes a lane from buffer + voff to LDS at lds + OFFSET + 16 * lane (lds: wave-uniform); counted by vmcnt.  The whole offset is in the vector register, which
+// the bounds check looks at.  The compiler puts no wait states into asm: the load needs one after the write of M0, written here, and five after a vector
+// instruction that wrote its descriptor, which settled() puts behind the making of descriptors once for all of their loads.
+template <int OFFSET>
 __device__ __forceinline__ void load_to_lds(const i32x4& buffer, unsigned voff, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buffer) : "memory", "m0");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buffer), "n"(OFFSET) : "memory", "m0", "scc");
+}
+__device__ __forceinline__ void settled(i32x4& a, i32x4& b) { asm volatile("s_nop 4" : "+s"(a), "+s"(b)); }
+// The buffer `bytes` further on, by scalar instructions (no wait states).
+__device__ __forceinline__ void move(i32x4& buffer, unsigned bytes)
+{
+    const unsigned long long b = ((unsigned long long)(unsigned)buffer[1] << 32 | (unsigned)buffer[0]) + bytes;
+    buffer[0] = (int)b;
+    buffer[1] = (int)(b >> 32);
 }
 
-// ---- a tile of ROWS rows (or columns) x kStep of the contraction in LDS, 128 ROWS bytes ---------------------------------------
-// Stored along the contraction: rows of 128 bytes, 16-byte chunk c of row r in slot c ^ (r / 2 & 7).  A load instruction fills 8 rows; the operand read
-// takes 16 bytes of 32 rows a half wave, and 16 neighbouring rows (two of them to the 256 bytes that LDS is wide) lie in different banks.
-__device__ __forceinline__ int turn_of(int row) { return (row >> 1) & 7; }
-// Stored across: kStep rows of 2 ROWS bytes; 32-byte granule g (16 columns) of contraction row k in slot g ^ spread(k & 3).  A load instruction
+// ---- a tile of ROWS rows (or columns) x STEP (32 or 64) of the contraction in LDS ----------------------------------------------
+// Stored along the contraction: rows of 2 STEP bytes, 16-byte chunk c of row r in slot c ^ turn_of(r).  A load instruction fills 8 or 16 rows; the operand read
+// takes 16 bytes of 32 rows a half wave, and 16 neighbouring rows (two or four of them to the 256 bytes that LDS is wide) lie in different banks.
+template <int STEP>
+__device__ __forceinline__ int turn_of(int row)
+{
+    return STEP == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+// Stored across: STEP rows of 2 ROWS bytes; 32-byte granule g (16 columns) of contraction row k in slot g ^ spread(k & 3).  A load instruction
 // fills 1 KB, 2 or 4 contraction rows.  The transpose read takes, for 16 lanes, 32 bytes of 4 contraction rows: with the spread of 0, 5, 2, 7 these lie in
 // different banks, those of the neighbouring 16 lanes (the granule beside) too.
 __device__ __forceinline__ int spread(int k) { return (k & 3) ^ ((k & 1) << 2); }
 
-template <int KIND, int WA, int WB, int NB, int RING>
+// A tile: WA x WB waves of NA x NB blocks of 32 x 32, RING stages of STEP of the contraction.
+template <int KIND, int WA, int WB, int NA, int NB, int STEP, int RING>
 struct Shape {
-    static constexpr int TA = 64 * WA, TB = 32 * NB * WB, WAVES = WA * WB, THREADS = 64 * WAVES;
+    static constexpr int TA = 32 * NA * WA, TB = 32 * NB * WB, WAVES = WA * WB, THREADS = 64 * WAVES;
     static constexpr bool A_COLUMNS = KIND != kForward, B_COLUMNS = KIND == kWeightGrad;
-    static constexpr int A_BYTES = TA * 2 * kStep, B_BYTES = TB * 2 * kStep, STAGE = A_BYTES + B_BYTES, LDS = RING * STAGE;
-    static constexpr int A_LOADS = TA / 8 / WAVES, B_LOADS = TB / 8 / WAVES;  // instructions a wave, 1 KB each
-    static_assert(TA / 8 % WAVES == 0 && TB / 8 % WAVES == 0, "the waves share the loads of a stage evenly");
+    static constexpr int A_BYTES = TA * 2 * STEP, B_BYTES = TB * 2 * STEP, STAGE = A_BYTES + B_BYTES, LDS = RING * STAGE;
+    static constexpr int A_LOADS = A_BYTES / 1024 / WAVES, B_LOADS = B_BYTES / 1024 / WAVES, LOADS = A_LOADS + B_LOADS;  // instructions a wave, 1 KB each
+    static_assert(A_BYTES / 1024 % WAVES == 0 && B_BYTES / 1024 % WAVES == 0, "the waves share the loads of a stage evenly");
     static_assert((!A_COLUMNS || 512 % TA == 0) && (!B_COLUMNS || 512 % TB == 0), "an instruction fills whole contraction rows");
-    static_assert(A_LOADS % 2 == 0, "which of a wave's instructions for A are even ones of the tile is known in advance");
+    static_assert(A_COLUMNS || A_BYTES / 2048 % A_LOADS == 0, "a wave's share of A is of one weight");
+    static_assert(STEP % 32 == 0 && NA % 2 == 0 && RING >= 2);
 };
 
 struct TileArgs {
@@ -121,10 +150,10 @@ __device__ __forceinline__ void tile_of(unsigned id, unsigned n, int tiles_a, in
     *tile_b = (int)(band * BAND + in % width);
 }
 
-template <int KIND, int WA, int WB, int NB, int RING>
+template <int KIND, int WA, int WB, int NA, int NB, int STEP, int RING>
 __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
 {
-    typedef Shape<KIND, WA, WB, NB, RING> S;
+    typedef Shape<KIND, WA, WB, NA, NB, STEP, RING> S;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds_bytes[];
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_bytes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -135,85 +164,97 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
     // origin of the tile; forward: the tile's A rows are TA / 2 rows of the gate weight and the same of the up weight
     const int a_first = tile_a * (KIND == kForward ? S::TA / 2 : S::TA);
     const long long b_first = (long long)tile_b * S::TB;
-    const int steps_each = (int)((t.depth + kStep - 1) / kStep), steps_all = KIND == kInputGrad ? 2 * steps_each : steps_each;
+    const int steps_each = (int)((t.depth + STEP - 1) / STEP), steps_all = KIND == kInputGrad ? 2 * steps_each : steps_each;
     const int it_first = (int)((long long)steps_all * blockIdx.y / gridDim.y), it_end = (int)((long long)steps_all * (blockIdx.y + 1) / gridDim.y);
     const int steps = it_end - it_first;  // of this part of the contraction
 
-    // ---- loads of a stage: instruction i of this wave is i-th of its share of A's, then of B's
-    constexpr int A_CHUNKS = S::TA / 8, B_CHUNKS = S::TB / 8;  // 16-byte chunks of a contraction row where an operand is stored across
-    constexpr int LOADS = S::A_LOADS + S::B_LOADS;
-    i32x4 buf_a, buf_b;
-    unsigned lds_to = 0, k_bytes = 0;
-    int k_left = 0;
-    const bool up = !S::A_COLUMNS && wave * S::A_LOADS >= S::TA / 16;  // forward: this wave loads the up weight's rows
-    static_assert(S::A_COLUMNS || (S::TA / 16) % S::A_LOADS == 0, "a wave's share of A is of one weight");
-    const long long ld_a_rows = up ? t.ld_a1 : t.ld_a0;  // (the two halves of B are in one workspace and have one stride; those of A need not)
-    long long ld_a = 0;
+    // ---- loads of a stage: instruction i of this wave is i-th of its share of A's, then of B's.  A lane's offsets stay as they are from stage to stage and the buffers
+    // move on: a load costs the writing of M0 beside itself, a stage two scalar additions.
+    const bool up = !S::A_COLUMNS && wave * S::A_LOADS >= S::A_BYTES / 2048;  // forward: this wave loads the up weight's rows
     // (The pointers and strides that the loop chooses between are pinned in registers: a choice between two arguments becomes a scalar load from the chosen
     // place otherwise, whose wait counts the LDS reads in flight too.)
-    const __bf16 *a0 = t.a0, *a1 = t.a1, *b0 = t.b0, *b1 = t.b1;
-    long long ld_a0 = t.ld_a0, ld_a1 = t.ld_a1;
-    asm("" : "+s"(a0), "+s"(a1), "+s"(b0), "+s"(b1), "+s"(ld_a0), "+s"(ld_a1));
-    if (!S::A_COLUMNS)
-        buf_a = buffer_of((up ? a1 : a0) + a_first * ld_a_rows, ((min((long long)t.rows_a - a_first, (long long)S::TA / 2) - 1) * ld_a_rows + t.depth) * 2);
-    const long long b_bytes = ((min(t.rows_b - b_first, (long long)S::TB) - 1) * t.ld_b0 + t.depth) * 2;
-    // What the loads of stage `it` have in common.  Along the contraction the buffer stays and the offset moves; across, the buffer moves.
-    auto aim = [&](int step, unsigned stage) {
-        const int it = it_first + step;
-        lds_to = lds + stage;
-        const bool upper = KIND == kInputGrad && it >= steps_each;
-        const long long k0 = (long long)(upper ? it - steps_each : it) * kStep;
-        k_left = it < it_end ? (int)min(t.depth - k0, (long long)kStep) : 0;  // 0: no such stage, nothing is read
-        k_bytes = (unsigned)(k0 * 2);
-        if (S::A_COLUMNS) {
-            ld_a = upper ? ld_a1 : ld_a0;
-            buf_a = buffer_of((upper ? a1 : a0) + k0 * ld_a + a_first, ((k_left - 1) * ld_a + t.rows_a - a_first) * 2);
-        }
-        if (S::B_COLUMNS)
-            buf_b = buffer_of(b0 + k0 * t.ld_b0 + b_first, ((k_left - 1) * t.ld_b0 + t.rows_b - b_first) * 2);
-        else
-            buf_b = buffer_of((upper ? b1 : b0) + b_first * t.ld_b0, b_bytes);
+    const __bf16 *a0 = up ? t.a1 : t.a0, *a1 = t.a1, *b0 = t.b0, *b1 = t.b1;
+    long long ld_a0 = up ? t.ld_a1 : t.ld_a0, ld_a1 = t.ld_a1, ld_b = t.ld_b0;  // (the two halves of B are in one workspace and have one stride; those of A need not)
+    asm("" : "+s"(a0), "+s"(a1), "+s"(b0), "+s"(b1), "+s"(ld_a0), "+s"(ld_a1), "+s"(ld_b));
+    const long long rows_a = min((long long)t.rows_a - a_first, (long long)(KIND == kForward ? S::TA / 2 : S::TA)), rows_b = min(t.rows_b - b_first, (long long)S::TB);  // of the tile
+    i32x4 buf_a, buf_b;
+    unsigned voff[S::LOADS], lds_to = lds, move_a = 0, move_b = 0;
+    int aimed = 0, plain_until = 0;  // the step that buffers and offsets are for; the first one behind it that takes more than moving the buffers on
+    auto rows_offset = [&](int n, long long ld, int left) INLINED {
+        constexpr int CHUNKS = STEP / 8, ROWS = 64 / CHUNKS;
+        const int r = lane / CHUNKS, c = (lane % CHUNKS) ^ turn_of<STEP>(n * ROWS + r);
+        return c * 8 < left ? (unsigned)((n * ROWS + r) * ld * 2 + c * 16) : kOutside;
     };
-    auto load_rows = [&](const i32x4& buf, int n, int odd, long long ld, unsigned to) {
-        const int r = lane >> 3, c = (lane & 7) ^ turn_of(odd * 8 + r);
-        const unsigned off = (unsigned)(r * ld * 2 + c * 16) + (unsigned)(n * 8 * ld * 2) + k_bytes;
-        load_to_lds(buf, c * 8 < k_left ? off : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
-    };
-    auto load_columns = [&](const i32x4& buf, int n, int chunks, long long ld, long long left, unsigned to) {
-        const int each = 64 / chunks, k = n * each + lane / chunks, slot = lane % chunks;
+    auto columns_offset = [&](int n, int chunks, long long ld, long long width) INLINED {  // (chunks of 16 bytes a contraction row)
+        const int k = n * (64 / chunks) + lane / chunks, slot = lane % chunks;
         const int c = ((slot >> 1) ^ spread(k)) << 1 | (slot & 1);
-        load_to_lds(buf, c * 8 < left ? (unsigned)(k * ld * 2 + c * 16) : kOutside, __builtin_amdgcn_readfirstlane(to + n * 1024));
+        return c * 8 < width ? (unsigned)(k * ld * 2 + c * 16) : kOutside;
     };
-    auto load = [&](int i) {
-        if (i < S::A_LOADS) {
+    // Buffers and offsets of step `aimed` of this part: the first one, one that is cut short by the contraction's end, the first of the second half, and those behind the
+    // part's last, which read nothing.
+    auto aim = [&]() INLINED {
+        const int it = it_first + aimed;
+        const bool upper = KIND == kInputGrad && it >= steps_each;
+        const long long k0 = (long long)(upper ? it - steps_each : it) * STEP, left = it < it_end ? t.depth - k0 : 0, rows = min(left, (long long)STEP);
+        const long long ld_a = upper ? ld_a1 : ld_a0;
+        const __bf16 *const a = upper ? a1 : a0, *const b = upper ? b1 : b0;
+        buf_a = S::A_COLUMNS ? buffer_of(a + k0 * ld_a + a_first, ((rows - 1) * ld_a + t.rows_a - a_first) * 2)
+                             : buffer_of(a + a_first * ld_a + k0, left > 0 ? ((rows_a - 1) * ld_a + left) * 2 : 0);
+        buf_b = S::B_COLUMNS ? buffer_of(b + k0 * ld_b + b_first, ((rows - 1) * ld_b + t.rows_b - b_first) * 2)
+                             : buffer_of(b + b_first * ld_b + k0, left > 0 ? ((rows_b - 1) * ld_b + left) * 2 : 0);
+        settled(buf_a, buf_b);
+        // (A buffer that moves on along its rows keeps its length, which is still short of the row behind the last: what it lets through behind the last row's part of the
+        // step, no lane's offset reaches.)
+        move_a = left > 0 ? __builtin_amdgcn_readfirstlane((int)(S::A_COLUMNS ? STEP * ld_a * 2 : STEP * 2)) : 0;
+        move_b = left > 0 ? __builtin_amdgcn_readfirstlane((int)(S::B_COLUMNS ? STEP * ld_b * 2 : STEP * 2)) : 0;
+        plain_until = __builtin_amdgcn_readfirstlane(left > 0 ? min((upper ? steps_each : 0) + (int)(t.depth / STEP), it_end) - it_first : 0x7fffffff);
+#pragma unroll
+        for (int i = 0; i < S::A_LOADS; ++i) {
             const int n = wave * S::A_LOADS + i;
-            if (S::A_COLUMNS)
-                load_columns(buf_a, n, A_CHUNKS, ld_a, (long long)t.rows_a - a_first, lds_to);
-            else
-                load_rows(buf_a, n - (up ? S::TA / 16 : 0), i & 1, ld_a_rows, lds_to + (up ? S::TA / 16 * 1024 : 0));
-        } else {
-            const int n = wave * S::B_LOADS + i - S::A_LOADS;
-            if (S::B_COLUMNS)
-                load_columns(buf_b, n, B_CHUNKS, t.ld_b0, t.rows_b - b_first, lds_to + S::A_BYTES);
-            else
-                load_rows(buf_b, n, S::B_LOADS % 2 ? n & 1 : i & 1, t.ld_b0, lds_to + S::A_BYTES);  // (known in advance where every wave has an even number)
+            voff[i] = S::A_COLUMNS ? columns_offset(n, S::TA / 8, ld_a, t.rows_a - a_first) : rows_offset(n - (up ? S::A_BYTES / 2048 : 0), ld_a, (int)rows);
+        }
+#pragma unroll
+        for (int i = 0; i < S::B_LOADS; ++i) {
+            const int n = wave * S::B_LOADS + i;
+            voff[S::A_LOADS + i] = S::B_COLUMNS ? columns_offset(n, S::TB / 8, ld_b, t.rows_b - b_first) : rows_offset(n, ld_b, (int)rows);
         }
     };
-    auto issue = [&](int step, unsigned stage) {
-        aim(step, stage);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load(i);
+    auto advance = [&](unsigned stage) INLINED {  // to the next step, whose place in LDS is `stage`
+        lds_to = lds + stage;
+        if (++aimed < plain_until) {
+            move(buf_a, move_a);
+            move(buf_b, move_b);
+        } else
+            aim();
+    };
+    auto load = [&](auto i) INLINED {
+        if constexpr (i < S::A_LOADS)
+            load_to_lds<i * 1024>(buf_a, voff[i], lds_to + wave * (S::A_LOADS * 1024));
+        else
+            load_to_lds<S::A_BYTES + (i - S::A_LOADS) * 1024>(buf_b, voff[i], lds_to + wave * (S::B_LOADS * 1024));
     };
 
-    // ---- operand reads: 32 rows (columns) from `first` of the tile on, 16 s .. 16 s + 15 of the stage's contraction; lane l has row l % 32 and
-    // elements 8 (l / 32) .. + 7 of them
-    auto rows_address = [&](int first) { return (unsigned)((first + (lane & 31)) * 128 + (((lane >> 5) ^ turn_of(lane)) << 4)); };
-    auto read_rows = [&](unsigned base, int s) { return *(lds_bf16x8_ptr)(size_t)(base ^ (unsigned)(s << 5)); };
-    auto columns_address = [&](int first, int row_bytes) {
+    // ---- operand reads: 32 rows (columns), 16 s .. 16 s + 15 of the stage's contraction; lane l has row l % 32 and elements 8 (l / 32) .. + 7 of them.  Addresses:
+    // along the contraction one for each s, the blocks at constant distances; across it one for each block, the s at constant distances.
+    constexpr int SLOTS = STEP / 16, A_ADDR = S::A_COLUMNS ? NA : SLOTS, B_ADDR = S::B_COLUMNS ? NB : SLOTS;
+    auto rows_address = [&](int first, int s) INLINED { return (unsigned)((first + (lane & 31)) * (2 * STEP) + (((2 * s + (lane >> 5)) ^ turn_of<STEP>(lane)) << 4)); };
+    auto columns_address = [&](int first, int row_bytes) INLINED {
         const int j = lane & 15, k = 8 * (lane >> 5) + (j >> 2);
         return (unsigned)(k * row_bytes + ((((first >> 4) + ((lane >> 4) & 1)) ^ spread(j >> 2)) << 5) + 8 * (j & 3));
     };
-    auto read_columns = [&](unsigned base, int s, int row_bytes) {
+    unsigned a_zero[A_ADDR], b_zero[B_ADDR], a_at[A_ADDR], b_at[B_ADDR];  // in stage 0, and in the present one
+#pragma unroll
+    for (int i = 0; i < A_ADDR; ++i)
+        a_zero[i] = lds + (S::A_COLUMNS ? columns_address(32 * (NA * wa + i), 2 * S::TA) : rows_address((KIND == kForward ? 16 : 32) * NA * wa, i));
+#pragma unroll
+    for (int i = 0; i < B_ADDR; ++i) b_zero[i] = lds + S::A_BYTES + (S::B_COLUMNS ? columns_address(32 * (NB * wb + i), 2 * S::TB) : rows_address(32 * NB * wb, i));
+    auto enter = [&](unsigned stage) INLINED {
+#pragma unroll
+        for (int i = 0; i < A_ADDR; ++i) a_at[i] = a_zero[i] + stage;
+#pragma unroll
+        for (int i = 0; i < B_ADDR; ++i) b_at[i] = b_zero[i] + stage;
+    };
+    auto read_columns = [&](unsigned base, int s, int row_bytes) INLINED {
         union {
             struct {
                 short4v lo, hi;
@@ -224,56 +265,54 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
         u.h.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(size_t)(base + (unsigned)((16 * s + 4) * row_bytes)));
         return u.v;
     };
-    unsigned a_at[2], b_at[NB];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int first = KIND == kForward ? 32 * wa + i * (S::TA / 2) : 64 * wa + 32 * i;
-        a_at[i] = lds + (S::A_COLUMNS ? columns_address(first, 2 * S::TA) : rows_address(first));
-    }
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        const int first = 32 * (NB * wb + i);
-        b_at[i] = lds + S::A_BYTES + (S::B_COLUMNS ? columns_address(first, 2 * S::TB) : rows_address(first));
-    }
+    bf16x8 a[2][NA], b[2][NB];
+    // Read n of slot s, in the order of first use: a[0], b[0], the rest of a, the rest of b.
+    auto read = [&](auto into, auto s, auto n) INLINED {
+        if constexpr (n == 0 || (n >= 2 && n <= NA)) {
+            constexpr int i = n == 0 ? 0 : n - 1;
+            constexpr int away = KIND == kForward ? i / 2 * 64 * STEP + i % 2 * (S::A_BYTES / 2) : i * 64 * STEP;  // (forward: gate and up blocks in turn)
+            if constexpr (S::A_COLUMNS)
+                a[into][i] = read_columns(a_at[i], s, 2 * S::TA);
+            else
+                a[into][i] = *(lds_bf16x8_ptr)(size_t)(a_at[s] + away);
+        } else {
+            constexpr int j = n == 1 ? 0 : n - NA;
+            if constexpr (S::B_COLUMNS)
+                b[into][j] = read_columns(b_at[j], s, 2 * S::TB);
+            else
+                b[into][j] = *(lds_bf16x8_ptr)(size_t)(b_at[s] + j * 64 * STEP);
+        }
+    };
 
-    f32x16 acc[2][NB];
+    f32x16 acc[NA][NB];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    // ---- the loop.  A stage is kStep / 16 slots; in each the operands of the next slot are read while the matrix instructions of this one run, across the
-    // barrier too: its last slot's operands are in registers when the stage is given up, and the next stage's first are read beside its products.
-    constexpr int SLOTS = kStep / 16;
-    bf16x8 a[2][2], b[2][NB];
-    auto read = [&](int into, unsigned stage, int s) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) a[into][i] = S::A_COLUMNS ? read_columns(a_at[i] + stage, s, 2 * S::TA) : read_rows(a_at[i] + stage, s);
-#pragma unroll
-        for (int j = 0; j < NB; ++j) b[into][j] = S::B_COLUMNS ? read_columns(b_at[j] + stage, s, 2 * S::TB) : read_rows(b_at[j] + stage, s);
-    };
-    auto product = [&](int from, int n) {
-        acc[n & 1][n >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[from][n & 1], b[from][n >> 1], acc[n & 1][n >> 1], 0, 0, 0);
-    };
-    auto multiply = [&](int from) {
-#pragma unroll
-        for (int n = 0; n < 2 * NB; ++n) product(from, n);
-    };
-    // A slot's order: reads and products in turn.
-    auto interleave = [&] {
-        constexpr int READS = (S::A_COLUMNS ? 4 : 2) + (S::B_COLUMNS ? 2 : 1) * NB, PRODUCTS = 2 * NB;
-#pragma unroll
-        for (int i = 0; i < PRODUCTS; ++i) {
-            constexpr int each = (READS + PRODUCTS - 1) / PRODUCTS;
-            __builtin_amdgcn_sched_group_barrier(0x100, each, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+    // ---- the loop.  A stage is STEP / 16 slots; in each the operands of the next slot are read beside the products of this one, across the barrier too: its last
+    // slot's operands are in registers when the stage is given up, and the next stage's first are read beside its products.  The order is written out, each read and
+    // load behind a product of its own, as a wave's issue waits while the address unit is busy: loads take half of a stage's last slot and half of the next one's first.
+    constexpr int PRODUCTS = NA * NB, READS = NA + NB, READ_IN = PRODUCTS * 3 / 4, EARLY = S::LOADS / 2;
+    // Products of operands `from`; beside them the reads of slot s of the stage entered (not where s is SLOTS), and loads first .. last - 1.
+    auto slot = [&](auto from, auto s, auto first, auto last) INLINED {
+        auto one = [&](auto n) INLINED {
+            if constexpr (s < SLOTS && n < READ_IN) {
+                auto next = [&](auto r) INLINED { read(Int<1 - from>{}, s, r); };
+                each_of<n * READS / READ_IN, (n + 1) * READS / READ_IN>(next);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            acc[n % NA][n / NA] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[from][n % NA], b[from][n / NA], acc[n % NA][n / NA], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            each_of<first + n * (last - first) / PRODUCTS, first + (n + 1) * (last - first) / PRODUCTS>(load);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each_of<0, PRODUCTS>(one);
     };
     // All but `more` of this wave's loads have arrived and its reads are done; after the barrier everybody's.
-    auto settle = [](auto more) {
+    auto settle = [](auto more) INLINED {
         constexpr int n = more;
         static_assert(n < 64, "vmcnt is 6 bits");
         asm volatile("" ::: "memory");
@@ -281,112 +320,115 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    auto slots = [&](unsigned stage) {  // all but the last
-#pragma unroll
-        for (int s = 0; s + 1 < SLOTS; ++s) {
-            __builtin_amdgcn_sched_barrier(0);
-            read((s + 1) & 1, stage, s + 1);
-            multiply(s & 1);
-            interleave();
-        }
+    // All slots but the last, beside the first of them the rest of the loads begun before.
+    auto slots = [&](auto loads) INLINED {
+        auto one = [&](auto s) INLINED { slot(Int<s % 2>{}, Int<s + 1>{}, Int<EARLY>{}, Int<(s == 0 && loads ? S::LOADS : EARLY)>{}); };
+        each_of<0, SLOTS - 1>(one);
     };
     // The loads of the stages after the last fall outside their buffers, all of them: nothing is read, and the loop has no branch for them.
     if (steps > 0) {
+        aim();
+        each_of<0, S::LOADS>(load);
 #pragma unroll
-        for (int i = 0; i < RING; ++i) issue(i, i * S::STAGE);
-        settle(std::integral_constant<int, (RING - 1) * LOADS>{});
-        read(0, 0, 0);
+        for (int i = 1; i < RING; ++i) {
+            advance(i * S::STAGE);
+            if (i + 1 < RING)
+                each_of<0, S::LOADS>(load);
+            else
+                each_of<0, EARLY>(load);
+        }
+        settle(Int<(RING - 2) * S::LOADS + EARLY>{});
+        enter(0);
+        auto next = [&](auto r) INLINED { read(Int<0>{}, Int<0>{}, r); };
+        each_of<0, READS>(next);
         unsigned stage = 0;
         for (int it = 0; it + 1 < steps; ++it) {
-            const unsigned next = stage + S::STAGE == S::LDS ? 0 : stage + S::STAGE;
-            slots(stage);
-            settle(std::integral_constant<int, (RING - 2) * LOADS>{});
+            const unsigned next_stage = stage + S::STAGE == S::LDS ? 0 : stage + S::STAGE;
+            slots(std::true_type{});
+            settle(Int<(RING - 2) * S::LOADS>{});
+            advance(stage);
+            enter(next_stage);
             __builtin_amdgcn_sched_barrier(0);
-            read(0, next, 0);
-            aim(it + RING, stage);
-            constexpr int PRODUCTS = 2 * NB;
-#pragma unroll
-            for (int n = 0; n < PRODUCTS; ++n) {  // loads into the stage just read, beside the products
-                product((SLOTS - 1) & 1, n);
-#pragma unroll
-                for (int i = n * LOADS / PRODUCTS; i < (n + 1) * LOADS / PRODUCTS; ++i) load(i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            stage = next;
+            slot(Int<1>{}, Int<0>{}, Int<0>{}, Int<EARLY>{});
+            stage = next_stage;
         }
-        slots(stage);
-        multiply((SLOTS - 1) & 1);
-        settle(std::integral_constant<int, 0>{});  // (nothing may still be on its way to this workgroup's LDS when it ends)
+        slots(std::false_type{});
+        slot(Int<1>{}, Int<SLOTS>{}, Int<0>{}, Int<0>{});
+        settle(Int<0>{});  // (nothing may still be on its way to this workgroup's LDS, which is used again, and is given up in the end)
     }
 
-    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Lanes l and l + 32 hold the
-    // two halves of 8 consecutive outputs; of two such eights each of them takes one, so that a lane stores 16 bytes.
-    auto store = [&](__bf16* out, const float (&x)[8], int first) {  // x: its part of outputs first .. + 7 and of the 8 behind
-        union {
-            bf16x4 v[2];
-            unsigned w[4];
-        } u;
+    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Outputs go through a part of LDS of
+    // the wave's own, so that neighbouring lanes store neighbouring 16 bytes of a row: 64 to 256 bytes together, where the registers hold 16 or 32 (4 608 x 2 432 x 6 528
+    // with the products kept 320 -> 286 us).
+    constexpr int OWN = S::LDS / S::WAVES;
+    const unsigned own = lds + wave * OWN;
+    // Of blocks j = from .. until - 1, `width` outputs of type T from `first` on.  value(j, g): this lane's outputs 8 g + 4 (lane / 32) .. + 3 of row lane % 32 of block j;
+    // to(row): where a row is.  As many blocks at once as LDS has room for.
+    auto store = [&](auto type, auto width, auto from, auto until, int first, auto value, auto to) INLINED {
+        typedef decltype(type) T;
+        typedef T four __attribute__((ext_vector_type(4)));
+        constexpr int BLOCKS = until - from, BYTES = width * sizeof(T), PITCH = BYTES + 16, LANES = BYTES / 16, ROWS = 64 / LANES;
+        constexpr int FIT = OWN / (32 * PITCH), TOGETHER = FIT >= BLOCKS ? BLOCKS : FIT >= 2 && BLOCKS % 2 == 0 ? 2 : 1;
+        static_assert(FIT >= 1, "a block fits");
+        const int c = first + lane % LANES * (int)(16 / sizeof(T));
+        auto some = [&](auto k) INLINED {
+            constexpr int j0 = from + k * TOGETHER;
+            auto put_block = [&](auto n) INLINED {
+                auto put = [&](auto g) INLINED {
+                    *(__attribute__((address_space(3))) four*)(size_t)(own + (unsigned)((32 * n + (lane & 31)) * PITCH + (8 * g + 4 * (lane >> 5)) * (int)sizeof(T))) =
+                        __builtin_convertvector(value(Int<j0 + n>{}, g), four);
+                };
+                each_of<0, width / 8>(put);
+            };
+            each_of<0, TOGETHER>(put_block);
+            asm volatile("" ::: "memory");  // (a wave's LDS instructions are executed in order)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) u.v[r >> 2][r & 3] = (__bf16)x[r];
-        const auto lo = __builtin_amdgcn_permlane32_swap(u.w[0], u.w[2], false, false);
-        const auto hi = __builtin_amdgcn_permlane32_swap(u.w[1], u.w[3], false, false);
-        union {
-            unsigned w[4];
-            bf16x8 v;
-        } o = {{lo[0], hi[0], lo[1], hi[1]}};
-        const int c = first + 8 * (lane >> 5);
-        if (c < t.rows_a) *(bf16x8*)(out + c) = o.v;
-    };
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-        const long long row = b_first + 32 * (NB * wb + j) + (lane & 31);
-        const bool in = row < t.rows_b;  // (a lane and its partner have the same row)
-        if (KIND == kForward) {
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int f = a_first + 32 * wa + 16 * q;
-                float h[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) h[r] = activation(acc[0][j][8 * q + r], t.act) * acc[1][j][8 * q + r];
-                if (in) store(t.out0 + row * t.ld_out0, h, f);
-                if (t.pre && in) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int c = f + 8 * e + 4 * (lane >> 5);
-                        if (c >= t.rows_a) continue;
-                        f32x4 g, u;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            g[r] = acc[0][j][8 * q + 4 * e + r];
-                            u[r] = acc[1][j][8 * q + 4 * e + r];
-                        }
-                        *(f32x4*)(t.pre + row * t.rows_a + c) = g;
-                        *(f32x4*)(t.pre + (t.rows_b + row) * t.rows_a + c) = u;
-                    }
-                }
+            for (int i = 0; i < TOGETHER * 32 / ROWS; ++i) {
+                const int at = i * ROWS + lane / LANES;
+                const i32x4 x = *(__attribute__((address_space(3))) i32x4*)(size_t)(own + (unsigned)(at * PITCH + lane % LANES * 16));
+                const long long row = b_first + 32 * (NB * wb + j0) + at;
+                if (row < t.rows_b && c < t.rows_a) *(i32x4*)(to(row) + c) = x;
             }
-        } else if (in && t.parts) {
-            float* const out = t.parts + (blockIdx.y * t.rows_b + row) * t.rows_a;
+            asm volatile("" ::: "memory");
+        };
+        each_of<0, BLOCKS / TOGETHER>(some);
+    };
+    auto four_of = [&](auto i, auto j, auto g) INLINED {  // of block i of A and j of B
+        f32x4 x;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+        for (int r = 0; r < 4; ++r) x[r] = acc[i][j][4 * g + r];
+        return x;
+    };
+    if constexpr (KIND == kForward) {
+        const int first = a_first + 16 * NA * wa;
+        const Int<16 * NA> width{};
+        auto gate = [&](auto j, auto g) INLINED { return four_of(Int<g / 4 * 2>{}, j, Int<g % 4>{}); };
+        auto up_of = [&](auto j, auto g) INLINED { return four_of(Int<g / 4 * 2 + 1>{}, j, Int<g % 4>{}); };
+        auto hidden = [&](auto j, auto g) INLINED {
+            const f32x4 x = gate(j, g), y = up_of(j, g);
+            f32x4 h;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int c = a_first + 64 * wa + 32 * i + 8 * q + 4 * (lane >> 5);
-                    if (c < t.rows_a) *(f32x4*)(out + c) = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                }
-        } else if (in) {
-            const bool second = KIND == kWeightGrad && row >= t.rows_out0;
-            __bf16* const out = second ? t.out1 + (row - t.rows_out0) * t.ld_out1 : t.out0 + row * t.ld_out0;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float x[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) x[r] = acc[i][j][8 * q + r];
-                    store(out, x, a_first + 64 * wa + 32 * i + 16 * q);
-                }
-        }
+            for (int r = 0; r < 4; ++r) h[r] = activation(x[r], t.act) * y[r];
+            return h;
+        };
+        auto block = [&](auto j) INLINED {
+            const Int<j + 1> next{};
+            store((__bf16)0.f, width, j, next, first, hidden, [&](long long row) INLINED { return t.out0 + row * t.ld_out0; });
+            if (!t.pre) return;
+            store(0.f, width, j, next, first, gate, [&](long long row) INLINED { return t.pre + row * t.rows_a; });
+            store(0.f, width, j, next, first, up_of, [&](long long row) INLINED { return t.pre + (t.rows_b + row) * t.rows_a; });
+        };
+        each_of<0, NB>(block);
+    } else {
+        const int first = a_first + 32 * NA * wa;
+        const Int<32 * NA> width{};
+        auto sums = [&](auto j, auto g) INLINED { return four_of(Int<g / 4>{}, j, Int<g % 4>{}); };
+        if (t.parts)
+            store(0.f, width, Int<0>{}, Int<NB>{}, first, sums, [&](long long row) INLINED { return t.parts + (blockIdx.y * t.rows_b + row) * t.rows_a; });
+        else
+            store((__bf16)0.f, width, Int<0>{}, Int<NB>{}, first, sums, [&](long long row) INLINED {
+                return KIND == kWeightGrad && row >= t.rows_out0 ? t.out1 + (row - t.rows_out0) * t.ld_out1 : t.out0 + row * t.ld_out0;
+            });
     }
 }
 
@@ -528,10 +570,10 @@ struct LdsLimit {
     }
 };
 
-template <int KIND, int WA, int WB, int NB, int RING>
+template <int KIND, int WA, int WB, int NA, int NB, int STEP, int RING>
 hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
 {
-    typedef Shape<KIND, WA, WB, NB, RING> S;
+    typedef Shape<KIND, WA, WB, NA, NB, STEP, RING> S;
     const int a_rows = KIND == kForward ? S::TA / 2 : S::TA;
     t.tiles_a = (t.rows_a + a_rows - 1) / a_rows;
     const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB;
@@ -539,9 +581,9 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     t.tiles_b = (int)tiles_b;
     if (parts == 1) t.parts = nullptr;
     static LdsLimit limit;
-    const hipError_t allowed = limit.ensure((const void*)tile_kernel<KIND, WA, WB, NB, RING>, S::LDS);
+    const hipError_t allowed = limit.ensure((const void*)tile_kernel<KIND, WA, WB, NA, NB, STEP, RING>, S::LDS);
     if (allowed != hipSuccess) return allowed;
-    tile_kernel<KIND, WA, WB, NB, RING><<<dim3((unsigned)(tiles_b * t.tiles_a), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
+    tile_kernel<KIND, WA, WB, NA, NB, STEP, RING><<<dim3((unsigned)(tiles_b * t.tiles_a), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts == 1) return e;
     const long long n = t.rows_b * (t.rows_a / 8), blocks = (n + 255) / 256;
@@ -589,10 +631,15 @@ Plan weight_plan(long long tokens, int channels, int hidden) { return plan_of(kW
 template <int KIND>
 hipError_t launch_plan(const TileArgs& t, const Plan& p, hipStream_t stream)
 {
-    if (p.shape == kLarge) return launch_tiles<KIND, 4, 2, 4, 2>(t, p.parts, stream);
-    if constexpr (KIND != kWeightGrad)
-        if (p.shape == kMedium) return launch_tiles<KIND, 4, 2, 3, 2>(t, p.parts, stream);
-    return p.shape == kPair ? launch_tiles<KIND, 2, 2, 2, 2>(t, p.parts, stream) : launch_tiles<KIND, 2, 2, 2, 4>(t, p.parts, stream);
+    // Stages of 32, four in flight, instead of 64 and two: dX and dW at 4 608 x 2 432 x 6 528 8 and 4 % faster; forward, where then both operands would be read in
+    // halves of cache lines, 4 to 10 % slower.  256 x 192 has four waves there, as eight would not share its loads evenly.
+    constexpr int STEP = KIND == kForward ? 64 : 32, RING = 128 / STEP;
+    if (p.shape == kLarge) return launch_tiles<KIND, 4, 2, 2, 4, STEP, RING>(t, p.parts, stream);
+    if constexpr (KIND == kForward)
+        if (p.shape == kMedium) return launch_tiles<KIND, 4, 2, 2, 3, STEP, RING>(t, p.parts, stream);
+    if constexpr (KIND == kInputGrad)
+        if (p.shape == kMedium) return launch_tiles<KIND, 2, 2, 4, 3, STEP, RING>(t, p.parts, stream);
+    return p.shape == kPair ? launch_tiles<KIND, 2, 2, 2, 2, 64, 2>(t, p.parts, stream) : launch_tiles<KIND, 2, 2, 2, 2, 64, 4>(t, p.parts, stream);
 }
 
 // Whether the form for few tokens is the faster one: it reads X again for every 16 hidden channels, so its time grows with tokens and weights together (us at 25, 63 and 184 MB
