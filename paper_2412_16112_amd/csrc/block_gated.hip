@@ -594,9 +594,9 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
 
 // Tile shape and number of parts that the contraction is split into, by the time they are expected to take: rounds of workgroups over the 256 CUs, each of a
 // part's steps (64 of the contraction) and of what a tile costs beside (first loads, epilogue).  The constants, in us, were fitted to 1100 timings of the three products
-// in all shapes and 1 to 16 parts, at 100 to 8192 tokens and widths of 512 x 1024 to 4096 x 11264: the chosen form takes up to 4 % longer than the
-// best of them, 1 % on average.  (At 2432 x 6528 dX of 100 tokens takes 169 us in 256 x 256 tiles, 22 in deep ones with the contraction in 12 parts; of 4608 tokens 297 in
-// 256 x 256 tiles, which leave 76 CUs without one, 268 in 256 x 192 and 332 in small ones.)
+// in all shapes and 1 to 16 parts, at 100 to 8192 tokens and widths of 512 x 1024 to 4096 x 11264: the chosen form takes 0.3 % longer than the best of them on average, at most
+// 4 % (dW of the smallest width 11 %).  (At 2432 x 6528 dG, dU and dX of 100 tokens take 241 us in 256 x 256 tiles, 85 in deep ones, 26 in those with the
+// contraction in 8 parts; of 4608 tokens 362 in 256 x 256 tiles, which leave 76 CUs without one, 336 in 256 x 192 and 378 in small ones.)
 enum TileShape { kLarge, kMedium, kPair, kDeep };  // 256 x 256; 256 x 192; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
 struct Plan {
     TileShape shape;
@@ -613,10 +613,10 @@ Plan plan_of(int kind, long long rows_a, long long rows_b, long long depth)
         if (parts > 1 && steps < 8 * parts) break;
         const double each = (double)up(steps, parts);
         // (the parts are written and read once more)
-        const double join = parts == 1 ? 0 : 3.37 + (1.14 * parts + 0.5) * rows_a * rows_b * 4 / 4e6;
-        const double us[4] = {up(large * parts, 256) * (each * 1.42 + 9.26) + join, up(medium * parts, 256) * (each * 1.11 + 7.45) + join,
-                              (small * parts <= 256 ? each * 0.625 + 6.43 : up(small * parts, 512) * (each * 0.893 + 6.43)) + join,  // (a CU to itself where there are enough)
-                              up(small * parts, 256) * (each * 0.512 + 7.22) + join};
+        const double join = parts == 1 ? 0 : 2.01 + (1.8 * parts + 0.5) * rows_a * rows_b * 4 / 4e6;
+        const double us[4] = {up(large * parts, 256) * (each * 1.3 + 8.58) + join, up(medium * parts, 256) * (each * 1.07 + 8.22) + join,
+                              (small * parts <= 256 ? each * 0.625 + 7.29 : up(small * parts, 512) * (each * 0.89 + 7.29)) + join,  // (a CU to itself where there are enough)
+                              up(small * parts, 256) * (each * 0.468 + 7.71) + join};
         for (int s = 0; s < 4; ++s)
             if ((best_us == 0 || us[s] < best_us) && !(s == kMedium && kind == kWeightGrad)) {  // (stored across, 192 columns are no whole part of a load instruction)
                 best_us = us[s];
@@ -642,12 +642,14 @@ hipError_t launch_plan(const TileArgs& t, const Plan& p, hipStream_t stream)
     return p.shape == kPair ? launch_tiles<KIND, 2, 2, 2, 2, 64, 2>(t, p.parts, stream) : launch_tiles<KIND, 2, 2, 2, 2, 64, 4>(t, p.parts, stream);
 }
 
-// Whether the form for few tokens is the faster one: it reads X again for every 16 hidden channels, so its time grows with tokens and weights together (us at 25, 63 and 184 MB
-// of weights: 16 tokens 13, 16, 47; 32 tokens 13, 20, 56; 64 tokens 13, 28, 78), that of the tiles up to 128 tokens with the weights alone (17, 24, 44).
+// Whether the form for few tokens is the faster one, by the times, in us, that both are expected to take with weights from memory.  It reads X again for every 16 hidden
+// channels and is not faster for a CU that has less of them than others; the tiles take the same time up to 128 tokens.  Measured, 1, 16 and 32 tokens here, 16 in tiles:
+// 2 432 x 6 528 16, 19, 23 and 23; 3 200 x 8 640 28, 35, 40 and 31; 4 096 x 11 264 38, 46, 55 and 44; 5 120 x 13 824 63, 79, 97 and 52.
 bool few_tokens(const GatedArgs& a)
 {
-    const double megabytes = 4e-6 * a.channels * a.hidden;
-    return a.tokens <= 16 || (a.tokens <= 32 && megabytes <= 96) || (a.tokens <= 64 && megabytes <= 48);
+    if (a.tokens > 64) return false;
+    const double here = 3.1e-3 * a.channels * ((a.hidden + 4095) / 4096) * (1 + a.tokens / 64.), tiles = (9.4e-3 * a.channels + 2) * ((a.hidden + 16383) / 16384);
+    return here <= tiles;
 }
 
 }  // namespace
