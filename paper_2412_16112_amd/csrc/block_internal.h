@@ -76,24 +76,31 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
 
-// 8 consecutive elements, of which the first n (>= 8: all) exist; those that do not are 0 / are not written.
+// 8 elements as two fours, the second GAP elements behind the first (4: side by side); of the first 4 .. 8 the first n exist, of the second those that are then left
+// (n - GAP).  Elements that do not exist are 0 / are not written.
 template <typename T>
 struct Chunk8;
 template <>
 struct Chunk8<__bf16> {
     bf16x8 v;
+    template <int GAP = 4>
     __device__ __forceinline__ void load(const __bf16* p, int n)
     {
-        if (n >= 8) {
-            v = *(const bf16x8_any*)p;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (__bf16)0.f;
+        if constexpr (GAP == 4) {
+            if (n >= 8) {
+                v = *(const bf16x8_any*)p;
+                return;
+            }
         }
+        const bf16x4 lo = four(p, n), hi = four(p + GAP, n - GAP);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
     }
     __device__ __forceinline__ float get(int j) const { return (float)v[j]; }
+    template <int GAP = 4>
     static __device__ __forceinline__ void store(__bf16* p, int n, const float (&x)[8])
     {
+        static_assert(GAP == 4, "rows of bf16 are stored in eights");
         bf16x8 o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = (__bf16)x[j];
@@ -105,32 +112,52 @@ struct Chunk8<__bf16> {
                 if (j < n) p[j] = o[j];
         }
     }
+    static __device__ __forceinline__ bf16x4 four(const __bf16* p, int n)
+    {
+        bf16x4 x;
+        if (n >= 4) {
+            x = *(const bf16x4_any*)p;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = j < n ? p[j] : (__bf16)0.f;
+        }
+        return x;
+    }
 };
 template <>
 struct Chunk8<float> {
     f32x4 lo, hi;
+    template <int GAP = 4>
     __device__ __forceinline__ void load(const float* p, int n)
     {
-        if (n >= 8) {
-            lo = *(const f32x4_any*)p;
-            hi = *(const f32x4_any*)(p + 4);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                lo[j] = j < n ? p[j] : 0.f;
-                hi[j] = 4 + j < n ? p[4 + j] : 0.f;
-            }
-        }
+        lo = four(p, n);
+        hi = four(p + GAP, n - GAP);
     }
     __device__ __forceinline__ float get(int j) const { return j < 4 ? lo[j & 3] : hi[j & 3]; }
+    template <int GAP = 4>
     static __device__ __forceinline__ void store(float* p, int n, const float (&x)[8])
     {
-        if (n >= 8) {
-            *(f32x4_any*)p = f32x4{x[0], x[1], x[2], x[3]};
-            *(f32x4_any*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+        store_four(p, n, f32x4{x[0], x[1], x[2], x[3]});
+        store_four(p + GAP, n - GAP, f32x4{x[4], x[5], x[6], x[7]});
+    }
+    static __device__ __forceinline__ f32x4 four(const float* p, int n)
+    {
+        f32x4 x;
+        if (n >= 4) {
+            x = *(const f32x4_any*)p;
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < 4; ++j) x[j] = j < n ? p[j] : 0.f;
+        }
+        return x;
+    }
+    static __device__ __forceinline__ void store_four(float* p, int n, f32x4 x)
+    {
+        if (n >= 4) {
+            *(f32x4_any*)p = x;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
                 if (j < n) p[j] = x[j];
         }
     }

@@ -18,6 +18,15 @@ namespace {
 constexpr int kThreads = 512;
 __host__ __device__ constexpr int padded(int channels) { return (channels + 7) & ~7; }  // channels of a partial sum: whole chunks
 
+// Where the channels of chunk i of a lane are: element j at first(lane, i) + behind(j).
+template <typename T, int TEAM>
+struct Layout {
+    static constexpr bool FOURS = sizeof(T) == 4;
+    static constexpr int GAP = FOURS ? 256 * TEAM : 4;
+    static __device__ __forceinline__ int first(int lane, int i) { return (FOURS ? 4 : 8) * lane + 512 * TEAM * i; }
+    static __device__ __forceinline__ int behind(int j) { return j < 4 ? j : GAP + j - 4; }
+};
+
 // Sums over a team.  `slots`: N floats for each wave of the workgroup; every wave of the workgroup calls it.  With one barrier: the next call must be given other
 // slots, and the one after that may have these again.
 template <int TEAM, int N>
@@ -44,6 +53,7 @@ template <typename T, typename TW, int TEAM, int CH>
 __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
 {
     constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
+    typedef Layout<T, TEAM> L;
     __shared__ float slots[2][WAVES][1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM);
     const long long total = (long long)a.groups * a.rows;
@@ -56,17 +66,17 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
     Chunk8<T> v[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = 8 * (lane + 64 * TEAM * i);
-        v[i].load(x + c, C - c);
+        const int c = L::first(lane, i);
+        v[i].template load<L::GAP>(x + c, C - c);
     }
     const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)g * C : 0) : nullptr;
     const TW* const b = a.b ? (const TW*)a.b + (a.per_group ? (long long)g * C : 0) : nullptr;
     Chunk8<TW> cw[CH], cb[CH];  // (asked for here: they arrive while the sums are formed)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = 8 * (lane + 64 * TEAM * i);
-        if (w) cw[i].load(w + c, C - c);
-        if (b) cb[i].load(b + c, C - c);
+        const int c = L::first(lane, i);
+        if (w) cw[i].template load<L::GAP>(w + c, C - c);
+        if (b) cb[i].template load<L::GAP>(b + c, C - c);
     }
     float s[1] = {0.f};
 #pragma unroll
@@ -78,11 +88,11 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
     float q[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = 8 * (lane + 64 * TEAM * i);
+        const int c = L::first(lane, i);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float d = v[i].get(j) - mean;
-            q[0] += c + j < C ? d * d : 0.f;
+            q[0] += c + L::behind(j) < C ? d * d : 0.f;
         }
     }
     team_sum<TEAM>(q, slots[1], wave);
@@ -95,7 +105,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
     T* const y = (T*)a.y + g * a.st[2] + r * a.st[3];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = 8 * (lane + 64 * TEAM * i);
+        const int c = L::first(lane, i);
         if (c >= C) break;
         float o[8];
 #pragma unroll
@@ -104,7 +114,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
             if (w) o[j] *= a.offset + cw[i].get(j);
             if (b) o[j] += cb[i].get(j);
         }
-        Chunk8<T>::store(y + c, C - c, o);
+        Chunk8<T>::template store<L::GAP>(y + c, C - c, o);
     }
 }
 
@@ -114,6 +124,7 @@ template <typename T, typename TW, int TEAM, int CH>
 __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
 {
     constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
+    typedef Layout<T, TEAM> L;
     extern __shared__ __attribute__((aligned(16))) float lds[];  // [2][padded channels] where a workgroup has several teams
     __shared__ float slots[2][WAVES][2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM), team = wave / TEAM;
@@ -127,8 +138,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
     if (w) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int c = 8 * (lane + 64 * TEAM * i);
-            cw[i].load(w + c, C - c);
+            const int c = L::first(lane, i);
+            cw[i].template load<L::GAP>(w + c, C - c);
         }
     }
     float dw[CH][8], db[CH][8];
@@ -154,9 +165,9 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
         to->rstd = a.stats[total + row];
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int c = 8 * (lane + 64 * TEAM * i);
-            to->x[i].load(x + c, C - c);
-            to->dy[i].load(dy + c, to->live ? C - c : 0);
+            const int c = L::first(lane, i);
+            to->x[i].template load<L::GAP>(x + c, C - c);
+            to->dy[i].template load<L::GAP>(dy + c, to->live ? C - c : 0);
         }
     };
     constexpr bool AHEAD = CH < 4;  // the next row's loads are under way while a row is worked on; with 4 chunks a lane there are no registers for it
@@ -194,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
                 T* const dx = (T*)a.dx + now.g * a.st[4] + now.r * a.st[5];
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    const int c = 8 * (lane + 64 * TEAM * i);
+                    const int c = L::first(lane, i);
                     if (c >= C) break;
                     float o[8];
 #pragma unroll
@@ -202,7 +213,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
                         const float d = vd[i].get(j), h = (vx[i].get(j) - mean) * rstd;
                         o[j] = rstd * ((w ? d * (a.offset + cw[i].get(j)) : d) - s1 - h * s2);
                     }
-                    Chunk8<T>::store(dx + c, C - c, o);
+                    Chunk8<T>::template store<L::GAP>(dx + c, C - c, o);
                 }
             }
         }
@@ -215,17 +226,17 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
             float* const to = t + 1 < TEAMS ? lds : out;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int c = 8 * (lane + 64 * TEAM * i);
-                if (c < C) {
 #pragma unroll
-                    for (int h = 0; h < 8; h += 4) {
+                for (int h = 0; h < 8; h += 4) {
+                    const int c = L::first(lane, i) + L::behind(h);
+                    if (c < C) {
                         f32x4 sw = {dw[i][h], dw[i][h + 1], dw[i][h + 2], dw[i][h + 3]}, sb = {db[i][h], db[i][h + 1], db[i][h + 2], db[i][h + 3]};
                         if (t > 0) {
-                            sw += *(const f32x4*)(lds + c + h);
-                            sb += *(const f32x4*)(lds + wide + c + h);
+                            sw += *(const f32x4*)(lds + c);
+                            sb += *(const f32x4*)(lds + wide + c);
                         }
-                        *(f32x4_any*)(to + c + h) = sw;
-                        *(f32x4_any*)(to + wide + c + h) = sb;
+                        *(f32x4_any*)(to + c) = sw;
+                        *(f32x4_any*)(to + wide + c) = sb;
                     }
                 }
             }
