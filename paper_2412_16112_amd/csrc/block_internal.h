@@ -76,89 +76,130 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
 
-// 8 elements as two fours, the second GAP elements behind the first (4: side by side); of the first 4 .. 8 the first n exist, of the second those that are then left
-// (n - GAP).  Elements that do not exist are 0 / are not written.
+// How a row's chunks lie in it: `whole`: all lanes have all 8 elements of theirs; `tiny`: the row has less than 8.
+struct RowForm {
+    bool whole, tiny;
+};
+
+// 8 elements of a row, one piece of 8 (GAP 4) or two of 4, the second GAP elements behind the first.  From the chunk's place on, the row has n elements left.  A piece that
+// reaches past the end is taken further in front, so that it ends with the row; its elements that belong to the lane before are not the lane's own().  So a lane has one
+// load for a piece and no branch but for having none, and nothing waits for a load where it is asked for.
+template <int GAP>
+struct Piece {
+    static __device__ __forceinline__ int first(int j) { return GAP == 4 || j < 4 ? 0 : GAP; }                        // of element j's piece
+    static __device__ __forceinline__ int back(int j, int n) { return max((GAP == 4 ? 8 : 4) - (n - first(j)), 0); }  // how far it is taken in front
+    static __device__ __forceinline__ int in(int j) { return GAP == 4 ? j : j & 3; }                                  // element j's place in it
+    // Where element j is, from the chunk's place, and whether it is the lane's own.
+    static __device__ __forceinline__ int at(int j, int n, RowForm form) { return first(j) + in(j) - (form.whole || form.tiny ? 0 : back(j, n)); }
+    static __device__ __forceinline__ bool own(int j, int n, RowForm form)
+    {
+        if (form.whole) return true;
+        if (form.tiny) return first(j) + in(j) < n;
+        return n > first(j) && in(j) >= back(j, n);
+    }
+};
+
 template <typename T>
 struct Chunk8;
 template <>
 struct Chunk8<__bf16> {
     bf16x8 v;
-    template <int GAP = 4>
-    __device__ __forceinline__ void load(const __bf16* p, int n)
+    template <int GAP>
+    __device__ __forceinline__ void load(const __bf16* p, int n, RowForm form)
     {
-        if constexpr (GAP == 4) {
-            if (n >= 8) {
-                v = *(const bf16x8_any*)p;
-                return;
-            }
-        }
-        const bf16x4 lo = four(p, n), hi = four(p + GAP, n - GAP);
+        typedef Piece<GAP> P;
+        if (form.tiny) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+            for (int j = 0; j < 8; ++j) v[j] = P::own(j, n, form) ? p[P::at(j, n, form)] : (__bf16)0.f;
+        } else if (GAP == 4 && form.whole) {
+            v = *(const bf16x8_any*)p;
+        } else if (GAP == 4) {
+            v = bf16x8{};
+            if (n > 0) v = *(const bf16x8_any*)(p + P::at(0, n, form));
+        } else {
+            bf16x4 lo = {}, hi = {};
+            if (form.whole) {
+                lo = *(const bf16x4_any*)p;
+                hi = *(const bf16x4_any*)(p + GAP);
+            } else {
+                if (n > 0) lo = *(const bf16x4_any*)(p + P::at(0, n, form));
+                if (n > GAP) hi = *(const bf16x4_any*)(p + P::at(4, n, form));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+        }
+    }
+    template <int GAP>
+    __device__ __forceinline__ void clear_others(int n, RowForm form)  // elements that are not the lane's own: 0
+    {
+        if (form.whole) return;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = Piece<GAP>::own(j, n, form) ? v[j] : (__bf16)0.f;
     }
     __device__ __forceinline__ float get(int j) const { return (float)v[j]; }
-    template <int GAP = 4>
-    static __device__ __forceinline__ void store(__bf16* p, int n, const float (&x)[8])
+    template <int GAP>
+    static __device__ __forceinline__ void store(__bf16* p, int n, RowForm form, const float (&x)[8])
     {
         static_assert(GAP == 4, "rows of bf16 are stored in eights");
+        typedef Piece<GAP> P;
         bf16x8 o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = (__bf16)x[j];
-        if (n >= 8) {
+        if (form.whole || P::back(0, n) == 0) {
             *(bf16x8_any*)p = o;
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j < n) p[j] = o[j];
+                if (P::own(j, n, form)) p[P::at(j, n, form)] = o[j];
         }
-    }
-    static __device__ __forceinline__ bf16x4 four(const __bf16* p, int n)
-    {
-        bf16x4 x;
-        if (n >= 4) {
-            x = *(const bf16x4_any*)p;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = j < n ? p[j] : (__bf16)0.f;
-        }
-        return x;
     }
 };
 template <>
 struct Chunk8<float> {
     f32x4 lo, hi;
-    template <int GAP = 4>
-    __device__ __forceinline__ void load(const float* p, int n)
+    template <int GAP>
+    __device__ __forceinline__ void load(const float* p, int n, RowForm form)
     {
-        lo = four(p, n);
-        hi = four(p + GAP, n - GAP);
+        typedef Piece<GAP> P;
+        if (form.tiny) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lo[j] = P::own(j, n, form) ? p[P::at(j, n, form)] : 0.f;
+                hi[j] = P::own(4 + j, n, form) ? p[P::at(4 + j, n, form)] : 0.f;
+            }
+        } else if (form.whole) {
+            lo = *(const f32x4_any*)p;
+            hi = *(const f32x4_any*)(p + GAP);
+        } else {
+            lo = hi = f32x4{};
+            if (n > 0) lo = *(const f32x4_any*)(p + P::at(0, n, form));
+            if (n > P::first(4)) hi = *(const f32x4_any*)(p + P::at(4, n, form));
+        }
+    }
+    template <int GAP>
+    __device__ __forceinline__ void clear_others(int n, RowForm form)
+    {
+        if (form.whole) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = Piece<GAP>::own(j, n, form) ? lo[j] : 0.f;
+            hi[j] = Piece<GAP>::own(4 + j, n, form) ? hi[j] : 0.f;
+        }
     }
     __device__ __forceinline__ float get(int j) const { return j < 4 ? lo[j & 3] : hi[j & 3]; }
-    template <int GAP = 4>
-    static __device__ __forceinline__ void store(float* p, int n, const float (&x)[8])
+    template <int GAP>
+    static __device__ __forceinline__ void store(float* p, int n, RowForm form, const float (&x)[8])
     {
-        store_four(p, n, f32x4{x[0], x[1], x[2], x[3]});
-        store_four(p + GAP, n - GAP, f32x4{x[4], x[5], x[6], x[7]});
-    }
-    static __device__ __forceinline__ f32x4 four(const float* p, int n)
-    {
-        f32x4 x;
-        if (n >= 4) {
-            x = *(const f32x4_any*)p;
-        } else {
+        typedef Piece<GAP> P;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = j < n ? p[j] : 0.f;
-        }
-        return x;
-    }
-    static __device__ __forceinline__ void store_four(float* p, int n, f32x4 x)
-    {
-        if (n >= 4) {
-            *(f32x4_any*)p = x;
-        } else {
+        for (int h = 0; h < 8; h += 4) {
+            if (form.whole || P::back(h, n) == 0) {
+                *(f32x4_any*)(p + P::first(h) + P::in(h)) = f32x4{x[h], x[h + 1], x[h + 2], x[h + 3]};
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < n) p[j] = x[j];
+                for (int j = h; j < h + 4; ++j)
+                    if (P::own(j, n, form)) p[P::at(j, n, form)] = x[j];
+            }
         }
     }
 };

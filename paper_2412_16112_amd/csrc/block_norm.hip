@@ -16,15 +16,17 @@ namespace block {
 namespace {
 
 constexpr int kThreads = 512;
+__host__ __device__ constexpr int forward_threads(int team) { return team == 8 ? 512 : 256; }
 __host__ __device__ constexpr int padded(int channels) { return (channels + 7) & ~7; }  // channels of a partial sum: whole chunks
 
-// Where the channels of chunk i of a lane are: element j at first(lane, i) + behind(j).
-template <typename T, int TEAM>
+// Where chunk i of a lane is, and how its elements lie there.
+template <typename T, int TEAM, int CH, bool WHOLE>
 struct Layout {
     static constexpr bool FOURS = sizeof(T) == 4;
     static constexpr int GAP = FOURS ? 256 * TEAM : 4;
     static __device__ __forceinline__ int first(int lane, int i) { return (FOURS ? 4 : 8) * lane + 512 * TEAM * i; }
-    static __device__ __forceinline__ int behind(int j) { return j < 4 ? j : GAP + j - 4; }
+    typedef Piece<GAP> P;
+    static __device__ __forceinline__ RowForm form(int channels, int i) { return {WHOLE || i + 1 < CH, TEAM * CH == 1 && channels < 8}; }
 };
 
 // Sums over a team.  `slots`: N floats for each wave of the workgroup; every wave of the workgroup calls it.  With one barrier: the next call must be given other
@@ -49,11 +51,11 @@ __device__ __forceinline__ void team_sum(float (&x)[N], float (*slots)[N], int w
     }
 }
 
-template <typename T, typename TW, int TEAM, int CH>
-__global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
+template <typename T, typename TW, int TEAM, int CH, bool WHOLE>
+__global__ void __launch_bounds__(forward_threads(TEAM)) norm_forward_kernel(NormArgs a)
 {
-    constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
-    typedef Layout<T, TEAM> L;
+    constexpr int WAVES = forward_threads(TEAM) / 64, TEAMS = WAVES / TEAM;
+    typedef Layout<T, TEAM, CH, WHOLE> L;
     __shared__ float slots[2][WAVES][1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM);
     const long long total = (long long)a.groups * a.rows;
@@ -67,7 +69,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = L::first(lane, i);
-        v[i].template load<L::GAP>(x + c, C - c);
+        v[i].template load<L::GAP>(x + c, C - c, L::form(C, i));
     }
     const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)g * C : 0) : nullptr;
     const TW* const b = a.b ? (const TW*)a.b + (a.per_group ? (long long)g * C : 0) : nullptr;
@@ -75,26 +77,30 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = L::first(lane, i);
-        if (w) cw[i].template load<L::GAP>(w + c, C - c);
-        if (b) cb[i].template load<L::GAP>(b + c, C - c);
+        if (w) cw[i].template load<L::GAP>(w + c, C - c, L::form(C, i));
+        if (b) cb[i].template load<L::GAP>(b + c, C - c, L::form(C, i));
     }
+    const int last = C - L::first(lane, CH - 1);
+    const RowForm form = L::form(C, CH - 1);  // of the last chunks; the others are whole
+    v[CH - 1].template clear_others<L::GAP>(last, form);
     float s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += v[i].get(j);  // (channels past the end are 0)
+        for (int j = 0; j < 8; ++j) s[0] += v[i].get(j);
     team_sum<TEAM>(s, slots[0], wave);
     const float mean = s[0] / (float)C;
     float q[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int c = L::first(lane, i);
+    auto add_squares = [&](int i, auto all) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float d = v[i].get(j) - mean;
-            q[0] += c + L::behind(j) < C ? d * d : 0.f;
+            q[0] += all || L::P::own(j, last, form) ? d * d : 0.f;
         }
-    }
+    };
+#pragma unroll
+    for (int i = 0; i + 1 < CH; ++i) add_squares(i, std::true_type{});
+    add_squares(CH - 1, std::bool_constant<WHOLE>{});
     team_sum<TEAM>(q, slots[1], wave);
     const float rstd = 1.0f / sqrtf(q[0] / (float)C + a.eps);
     if (!live) return;
@@ -114,17 +120,17 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a)
             if (w) o[j] *= a.offset + cw[i].get(j);
             if (b) o[j] += cb[i].get(j);
         }
-        Chunk8<T>::template store<L::GAP>(y + c, C - c, o);
+        Chunk8<T>::template store<L::GAP>(y + c, C - c, L::form(C, i), o);
     }
 }
 
 // Workgroup (p, set) of the grid takes rows p TEAMS + team, then every gridDim.x TEAMS further ones, of the set (a group, or everything when the weight
 // is shared), writes their dX and adds up dy xhat and dy in registers; the teams' sums are added in order and become partial p of the set.
-template <typename T, typename TW, int TEAM, int CH>
+template <typename T, typename TW, int TEAM, int CH, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
 {
     constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
-    typedef Layout<T, TEAM> L;
+    typedef Layout<T, TEAM, CH, WHOLE> L;
     extern __shared__ __attribute__((aligned(16))) float lds[];  // [2][padded channels] where a workgroup has several teams
     __shared__ float slots[2][WAVES][2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM), team = wave / TEAM;
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = L::first(lane, i);
-            cw[i].template load<L::GAP>(w + c, C - c);
+            cw[i].template load<L::GAP>(w + c, C - c, L::form(C, i));
         }
     }
     float dw[CH][8], db[CH][8];
@@ -166,8 +172,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = L::first(lane, i);
-            to->x[i].template load<L::GAP>(x + c, C - c);
-            to->dy[i].template load<L::GAP>(dy + c, to->live ? C - c : 0);
+            to->x[i].template load<L::GAP>(x + c, C - c, L::form(C, i));
+            to->dy[i].template load<L::GAP>(dy + c, to->live ? C - c : 0, to->live ? L::form(C, i) : RowForm{false, false});
         }
     };
     constexpr bool AHEAD = CH < 4;  // the next row's loads are under way while a row is worked on; with 4 chunks a lane there are no registers for it
@@ -176,11 +182,13 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
     int turn = 0;
     for (long long base = (long long)blockIdx.x * TEAMS; base < in_set; base += step, turn ^= 1) {  // (the same number of turns for every wave)
         if (AHEAD) {
+            __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);  // vmcnt 0, here and not behind the next row's loads, where the compiler would put it for the first turn's sake
             now = next;
             if (base + step < in_set) fetch(base + step, &next);
         } else {
             fetch(base, &now);
         }
+        now.dy[CH - 1].template clear_others<L::GAP>(C - L::first(lane, CH - 1), L::form(C, CH - 1));
         const Chunk8<T>(&vx)[CH] = now.x, (&vd)[CH] = now.dy;
         const float mean = now.mean, rstd = now.rstd;
         const bool live = now.live;
@@ -213,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
                         const float d = vd[i].get(j), h = (vx[i].get(j) - mean) * rstd;
                         o[j] = rstd * ((w ? d * (a.offset + cw[i].get(j)) : d) - s1 - h * s2);
                     }
-                    Chunk8<T>::template store<L::GAP>(dx + c, C - c, o);
+                    Chunk8<T>::template store<L::GAP>(dx + c, C - c, L::form(C, i), o);
                 }
             }
         }
@@ -228,8 +236,9 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
             for (int i = 0; i < CH; ++i) {
 #pragma unroll
                 for (int h = 0; h < 8; h += 4) {
-                    const int c = L::first(lane, i) + L::behind(h);
-                    if (c < C) {
+                    const int n = C - L::first(lane, i), c = C - n + L::P::first(h) + L::P::in(h);
+                    const RowForm form = L::form(C, i);
+                    if (form.whole || L::P::back(h, n) == 0) {
                         f32x4 sw = {dw[i][h], dw[i][h + 1], dw[i][h + 2], dw[i][h + 3]}, sb = {db[i][h], db[i][h + 1], db[i][h + 2], db[i][h + 3]};
                         if (t > 0) {
                             sw += *(const f32x4*)(lds + c);
@@ -237,6 +246,14 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
                         }
                         *(f32x4_any*)(to + c) = sw;
                         *(f32x4_any*)(to + wide + c) = sb;
+                    } else {
+#pragma unroll
+                        for (int j = h; j < h + 4; ++j) {
+                            if (!L::P::own(j, n, form)) continue;
+                            const int at = C - n + L::P::at(j, n, form);
+                            to[at] = t > 0 ? dw[i][j] + lds[at] : dw[i][j];
+                            to[wide + at] = t > 0 ? db[i][j] + lds[wide + at] : db[i][j];
+                        }
                     }
                 }
             }
@@ -275,27 +292,32 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(NormArgs a, int partial
     }
 }
 
+// `whole`: rows fill their last chunks too; they have instances of their own, without masks.
 struct Form {
     int team, ch;
+    bool whole;
+    Form(int team, int channels) : team(team), ch((channels + 512 * team - 1) / (512 * team)), whole(channels == 512 * team * ch) {}
 };
-int chunks_a_lane(int channels, int team) { return (channels + 512 * team - 1) / (512 * team); }
 Form forward_form(int channels)
 {
-    const int team = channels <= 1536 ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
-    return {team, chunks_a_lane(channels, team)};
+    const int team = channels <= 1536 || (channels > 2048 && channels <= 2560) ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
+    return Form(team, channels);
 }
 Form backward_form(int channels)
 {
     const int team = channels <= 1536 ? 1 : channels <= 2 * 1536 ? 2 : channels <= 4 * 1536 ? 4 : 8;
-    return {team, chunks_a_lane(channels, team)};
+    return Form(team, channels);
 }
 
-// call(team, ch) with both as integral constants, if (TEAM, CH) is the form.
+// call(team, ch, whole) with all three as integral constants, if (TEAM, CH) is the form.
 template <int TEAM, int CH, typename F>
 bool try_form(const Form& f, F& call)
 {
     if (f.team != TEAM || f.ch != CH) return false;
-    call(std::integral_constant<int, TEAM>{}, std::integral_constant<int, CH>{});
+    if (f.whole)
+        call(std::integral_constant<int, TEAM>{}, std::integral_constant<int, CH>{}, std::true_type{});
+    else
+        call(std::integral_constant<int, TEAM>{}, std::integral_constant<int, CH>{}, std::false_type{});
     return true;
 }
 
@@ -303,12 +325,12 @@ template <typename T, typename TW>
 hipError_t forward(const NormArgs& a, hipStream_t stream)
 {
     const Form f = forward_form(a.channels);
-    auto call = [&](auto team, auto ch) {
-        constexpr int TEAM = team, CH = ch, teams = kThreads / 64 / TEAM;
+    auto call = [&](auto team, auto ch, auto whole) {
+        constexpr int TEAM = team, CH = ch, teams = forward_threads(TEAM) / 64 / TEAM;
         const long long rows = (long long)a.groups * a.rows;
-        norm_forward_kernel<T, TW, TEAM, CH><<<dim3((unsigned)((rows + teams - 1) / teams)), dim3(kThreads), 0, stream>>>(a);
+        norm_forward_kernel<T, TW, TEAM, CH, whole><<<dim3((unsigned)((rows + teams - 1) / teams)), dim3(forward_threads(TEAM)), 0, stream>>>(a);
     };
-    const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) ||
+    const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<1, 5>(f, call) || try_form<2, 2>(f, call) ||
                     try_form<2, 3>(f, call) || try_form<2, 4>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) || try_form<8, 3>(f, call) ||
                     try_form<8, 4>(f, call);
     return ok ? hipGetLastError() : hipErrorInvalidValue;
@@ -322,10 +344,10 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
     const int partials = norm_partials(a.groups, a.rows, a.channels, a.per_group);
     hipError_t e = hipSuccess;
     if (partials > 0) {
-        auto call = [&](auto team, auto ch) {
+        auto call = [&](auto team, auto ch, auto whole) {
             constexpr int TEAM = team, CH = ch, teams = kThreads / 64 / TEAM;
             const size_t lds = teams > 1 && (a.dw || a.db) ? (size_t)padded(a.channels) * 8 : 0;  // (at most 48 KB)
-            norm_backward_kernel<T, TW, TEAM, CH><<<dim3(partials, sets), dim3(kThreads), lds, stream>>>(a);
+            norm_backward_kernel<T, TW, TEAM, CH, whole><<<dim3(partials, sets), dim3(kThreads), lds, stream>>>(a);
         };
         const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
                         try_form<4, 2>(f, call) || try_form<4, 3>(f, call) || try_form<8, 2>(f, call) || try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
