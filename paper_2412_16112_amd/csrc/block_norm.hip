@@ -15,8 +15,9 @@ namespace clear {
 namespace block {
 namespace {
 
-constexpr int kThreads = 512;
 __host__ __device__ constexpr int forward_threads(int team) { return team == 8 ? 512 : 256; }
+// With one chunk a lane 16 waves (or as many whole teams) have the registers, else 8: fp32 rows of 256 channels 47 -> 40 us a 60000, bf16 of 512 27 -> 24 a 32768.
+__host__ __device__ constexpr int backward_threads(int team, int ch) { return ch == 1 ? 16 / team * team * 64 : 512; }
 __host__ __device__ constexpr int padded(int channels) { return (channels + 7) & ~7; }  // channels of a partial sum: whole chunks
 
 // Where chunk i of a lane is, and how its elements lie there.
@@ -28,6 +29,11 @@ struct Layout {
     typedef Piece<GAP> P;
     static __device__ __forceinline__ RowForm form(int channels, int i) { return {WHOLE || i + 1 < CH, TEAM * CH == 1 && channels < 8}; }
 };
+
+typedef __attribute__((address_space(3))) float* shared_float;
+typedef __attribute__((address_space(3))) f32x4* shared_f32x4;
+__device__ __forceinline__ void put_four(float* to, f32x4 x) { *(f32x4_any*)to = x; }
+__device__ __forceinline__ void put_four(shared_float to, f32x4 x) { *(shared_f32x4)to = x; }  // (at multiples of 16 bytes)
 
 // Sums over a team.  `slots`: N floats for each wave of the workgroup; every wave of the workgroup calls it.  With one barrier: the next call must be given other
 // slots, and the one after that may have these again.
@@ -127,9 +133,9 @@ __global__ void __launch_bounds__(forward_threads(TEAM)) norm_forward_kernel(Nor
 // Workgroup (p, set) of the grid takes rows p TEAMS + team, then every gridDim.x TEAMS further ones, of the set (a group, or everything when the weight
 // is shared), writes their dX and adds up dy xhat and dy in registers; the teams' sums are added in order and become partial p of the set.
 template <typename T, typename TW, int TEAM, int CH, bool WHOLE>
-__global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
+__global__ void __launch_bounds__(backward_threads(TEAM, CH)) norm_backward_kernel(NormArgs a)
 {
-    constexpr int WAVES = kThreads / 64, TEAMS = WAVES / TEAM;
+    constexpr int WAVES = backward_threads(TEAM, CH) / 64, TEAMS = WAVES / TEAM;
     typedef Layout<T, TEAM, CH, WHOLE> L;
     extern __shared__ __attribute__((aligned(16))) float lds[];  // [2][padded channels] where a workgroup has several teams
     __shared__ float slots[2][WAVES][2];
@@ -229,34 +235,42 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a)
     if (!sums) return;
     const int wide = padded(C);
     float* const out = a.ws + ((long long)set * gridDim.x + blockIdx.x) * 2 * wide;
-    for (int t = 0; t < TEAMS; ++t) {
-        if (team == t) {
-            float* const to = t + 1 < TEAMS ? lds : out;
+    // (LDS by pointers of its own address space: with one pointer to either, the stores become flat ones, whose base, taken in front of the first channel and led back by
+    // the instruction's offset, can lie outside LDS and is then an address in memory.)
+    const shared_float sum = (shared_float)lds;
+    auto give = [&](auto to, bool more) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
+        for (int i = 0; i < CH; ++i) {
 #pragma unroll
-                for (int h = 0; h < 8; h += 4) {
-                    const int n = C - L::first(lane, i), c = C - n + L::P::first(h) + L::P::in(h);
-                    const RowForm form = L::form(C, i);
-                    if (form.whole || L::P::back(h, n) == 0) {
-                        f32x4 sw = {dw[i][h], dw[i][h + 1], dw[i][h + 2], dw[i][h + 3]}, sb = {db[i][h], db[i][h + 1], db[i][h + 2], db[i][h + 3]};
-                        if (t > 0) {
-                            sw += *(const f32x4*)(lds + c);
-                            sb += *(const f32x4*)(lds + wide + c);
-                        }
-                        *(f32x4_any*)(to + c) = sw;
-                        *(f32x4_any*)(to + wide + c) = sb;
-                    } else {
+            for (int h = 0; h < 8; h += 4) {
+                const int n = C - L::first(lane, i), c = C - n + L::P::first(h) + L::P::in(h);
+                const RowForm form = L::form(C, i);
+                if (form.whole || L::P::back(h, n) == 0) {
+                    f32x4 sw = {dw[i][h], dw[i][h + 1], dw[i][h + 2], dw[i][h + 3]}, sb = {db[i][h], db[i][h + 1], db[i][h + 2], db[i][h + 3]};
+                    if (more) {
+                        sw += *(shared_f32x4)(sum + c);
+                        sb += *(shared_f32x4)(sum + wide + c);
+                    }
+                    put_four(to + c, sw);
+                    put_four(to + wide + c, sb);
+                } else {
 #pragma unroll
-                        for (int j = h; j < h + 4; ++j) {
-                            if (!L::P::own(j, n, form)) continue;
-                            const int at = C - n + L::P::at(j, n, form);
-                            to[at] = t > 0 ? dw[i][j] + lds[at] : dw[i][j];
-                            to[wide + at] = t > 0 ? db[i][j] + lds[wide + at] : db[i][j];
-                        }
+                    for (int j = h; j < h + 4; ++j) {
+                        if (!L::P::own(j, n, form)) continue;
+                        const int at = C - n + L::P::at(j, n, form);
+                        to[at] = more ? dw[i][j] + sum[at] : dw[i][j];
+                        to[wide + at] = more ? db[i][j] + sum[wide + at] : db[i][j];
                     }
                 }
             }
+        }
+    };
+    for (int t = 0; t < TEAMS; ++t) {
+        if (team == t) {
+            if (t + 1 < TEAMS)
+                give(sum, t > 0);
+            else
+                give(out, t > 0);
         }
         __syncthreads();
     }
@@ -303,9 +317,10 @@ Form forward_form(int channels)
     const int team = channels <= 1536 || (channels > 2048 && channels <= 2560) ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
     return Form(team, channels);
 }
-Form backward_form(int channels)
+Form backward_form(int channels, bool fp32)
 {
-    const int team = channels <= 1536 ? 1 : channels <= 2 * 1536 ? 2 : channels <= 4 * 1536 ? 4 : 8;
+    // (fp32 rows of 1025 to 1536 channels: three waves of one chunk, 15 waves a CU, instead of one of three, 8 a CU: 16717 x 1111 44 -> 39 us without the join)
+    const int team = channels <= 1536 ? (fp32 && channels > 1024 ? 3 : 1) : channels <= 2 * 1536 ? 2 : channels <= 4 * 1536 ? 4 : 8;
     return Form(team, channels);
 }
 
@@ -339,18 +354,19 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
 template <typename T, typename TW>
 hipError_t backward(const NormArgs& a, hipStream_t stream)
 {
-    const Form f = backward_form(a.channels);
+    const Form f = backward_form(a.channels, sizeof(T) == 4);
     const int sets = a.per_group ? a.groups : 1;
     const int partials = norm_partials(a.groups, a.rows, a.channels, a.per_group);
     hipError_t e = hipSuccess;
     if (partials > 0) {
         auto call = [&](auto team, auto ch, auto whole) {
-            constexpr int TEAM = team, CH = ch, teams = kThreads / 64 / TEAM;
+            constexpr int TEAM = team, CH = ch, threads = backward_threads(TEAM, CH), teams = threads / 64 / TEAM;
             const size_t lds = teams > 1 && (a.dw || a.db) ? (size_t)padded(a.channels) * 8 : 0;  // (at most 48 KB)
-            norm_backward_kernel<T, TW, TEAM, CH, whole><<<dim3(partials, sets), dim3(kThreads), lds, stream>>>(a);
+            norm_backward_kernel<T, TW, TEAM, CH, whole><<<dim3(partials, sets), dim3(threads), lds, stream>>>(a);
         };
-        const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
+        bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
                         try_form<4, 2>(f, call) || try_form<4, 3>(f, call) || try_form<8, 2>(f, call) || try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
+        if constexpr (sizeof(T) == 4) ok = ok || try_form<3, 1>(f, call);
         e = ok ? hipGetLastError() : hipErrorInvalidValue;
     }
     if (e == hipSuccess && (a.dw || a.db)) {
@@ -366,7 +382,8 @@ int norm_partials(long long groups, long long rows, int channels, int per_group)
 {
     // 256 workgroups, one for each CU, or as many as there are rows for; the sets share them.  (With two or four a CU at narrow widths the sums written and read back
     // cost more than the rows gained: 16896 x 1024 36 -> 47 us.)
-    const long long teams = kThreads / 64 / backward_form(channels).team, in_set = per_group ? rows : groups * rows, sets = per_group ? groups : 1;
+    const Form f = backward_form(channels, true);  // (at most as many teams a workgroup as for bf16)
+    const long long teams = backward_threads(f.team, f.ch) / 64 / f.team, in_set = per_group ? rows : groups * rows, sets = per_group ? groups : 1;
     if (in_set == 0 || sets == 0) return 0;
     return (int)std::min<long long>((in_set + teams - 1) / teams, std::max<long long>(1, 256 / sets));
 }

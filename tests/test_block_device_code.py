@@ -67,3 +67,15 @@ def test_no_packed_fp32(code_objects, text):  # noqa: F811
         for kernel, body in instructions(path):
             if "5clear5block" in kernel:
                 assert not any(line.startswith(text) for line in body), kernel
+
+
+def test_no_flat_memory_instructions(code_objects):  # noqa: F811
+    """A flat instruction takes its address for one in LDS or in memory by the base, before its own offset is added: a base in front of the first element of an array in LDS is
+    an address in memory.  Every pointer of these kernels is known to be one or the other."""
+    kernels = 0
+    for path in code_objects:
+        for kernel, body in instructions(path):
+            if "5clear5block" in kernel:
+                kernels += 1
+                assert not any(line.startswith("flat_") for line in body), kernel
+    assert kernels >= 100
