@@ -76,13 +76,14 @@ def _ptr(t):
 
 # Handle of torch's current stream of a device, without the Stream object around it (2 us a call) where torch offers that.
 _current = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (where there is a device tensor, the runtime has been started)
 
 
 def _call(name, device, stream, *args):
     """The C function on the tensors' device and on `stream` (a handle; None: torch's current stream of that device).  Returns the stream's handle."""
     s = _current(device.index) if stream is None else stream
     f = getattr(_lib or lib(), name)
-    if torch.cuda.current_device() == device.index:
+    if _current_device() == device.index:
         status = f(*args, s)
     else:
         with torch.cuda.device(device):
@@ -90,6 +91,11 @@ def _call(name, device, stream, *args):
     if status != CLEAR_OK:
         _check(status)
     return s
+
+
+def _new_like(t):
+    """A new contiguous tensor of t's shape, dtype and device (half the time of torch.empty, which is given all three)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _on_device(ref, *others):
@@ -190,8 +196,8 @@ def _norm_weights(x, weight, bias):
         if w.shape != some.shape or w.dtype != some.dtype:
             _refuse("weight and bias must agree in shape and dtype", CLEAR_ERR_MISMATCH)
     if some is None:
-        return 0, CLEAR_F32, torch.float32
-    return int(some.dim() == 2), ca._dtype_code(some), some.dtype
+        return 0, CLEAR_F32
+    return int(some.dim() == 2), ca._dtype_code(some)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, out=None, save_stats=False, stream=None):
@@ -201,8 +207,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, out=None,
     any stride; out=x works in place.  Returns y, or (y, stats) with save_stats (fp32 [2, ...]: mean and 1/sqrt(var + eps) of every row)."""
     dtype = ca._dtype_code(x)
     groups, rows, C = _rows(x)
-    per_group, wcode, _ = _norm_weights(x, weight, bias)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    per_group, wcode = _norm_weights(x, weight, bias)
+    y = _new_like(x) if out is None else out
     _on_device(x, weight, bias, y)
     if y.shape != x.shape or y.dtype != x.dtype:
         _refuse("out must have the shape and dtype of x", CLEAR_ERR_MISMATCH)
@@ -217,15 +223,15 @@ def layer_norm_backward(dy, x, weight, bias, stats, weight_offset=0.0, need=(Tru
     that is None and where `need` says so."""
     dtype = ca._dtype_code(x)
     groups, rows, C = _rows(x)
-    per_group, wcode, wdtype = _norm_weights(x, weight, bias)
+    per_group, wcode = _norm_weights(x, weight, bias)
     _on_device(x, dy, weight, bias, stats)
     if dy.shape != x.shape or dy.dtype != x.dtype:
         _refuse("dy must have the shape and dtype of x", CLEAR_ERR_MISMATCH)
     if stats.dtype != torch.float32 or not stats.is_contiguous() or tuple(stats.shape) != (2,) + tuple(x.shape[:-1]):
         _refuse("stats must be what layer_norm(..., save_stats=True) gave for x")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
-    dw = torch.empty(weight.shape, dtype=wdtype, device=x.device) if weight is not None and need[1] else None
-    db = torch.empty(bias.shape, dtype=wdtype, device=x.device) if bias is not None and need[2] else None
+    dx = _new_like(x) if need[0] else None
+    dw = _new_like(weight) if weight is not None and need[1] else None
+    db = _new_like(bias) if bias is not None and need[2] else None
     if dx is None and dw is None and db is None:
         return None, None, None
     ws = None
@@ -281,7 +287,7 @@ def gated_ff(x, w_gate, w_up, activation="silu", out=None, save_pre=False, strea
     M, ld_x = _matrix(x, "x", C)
     _, ld_g = _matrix(w_gate, "w_gate", C)
     _, ld_u = _matrix(w_up, "w_up", C)
-    h = torch.empty(tuple(x.shape[:-1]) + (F,), dtype=x.dtype, device=x.device) if out is None else out
+    h = x.new_empty(x.shape[:-1] + (F,)) if out is None else out
     rows, ld_h = _matrix(h, "out", F)
     if rows != M:
         _refuse("out must have a row for each of x", CLEAR_ERR_MISMATCH)
@@ -305,8 +311,8 @@ def gated_ff_backward(dh, x, w_gate, w_up, pre, activation="silu", need=(True, T
     if pre.dtype != torch.float32 or not pre.is_contiguous() or tuple(pre.shape) != (2, M, F):
         _refuse("pre must be what gated_ff(..., save_pre=True) gave for x")
     _on_device(x, dh, w_gate, w_up, pre)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
-    dw = torch.empty((2, F, C), dtype=x.dtype, device=x.device) if need[1] else (None, None)
+    dx = _new_like(x) if need[0] else None
+    dw = x.new_empty((2, F, C)) if need[1] else (None, None)
     if not need[0] and not need[1]:
         return None, None, None
     size = lib().clear_block_gated_ff_workspace(M, C, F)
