@@ -6,9 +6,10 @@
 // An operand is stored along the contraction ("rows": X and the weights forward, dG and dU for dX) or across it ("columns": the weights
 // for dX, everything for the weight gradients); the latter are read from LDS with the 16-bit transpose load.
 //
-// The largest tile is 256 x 256 for 8 waves of 64 x 128 (6 operand reads for 8 matrix instructions): at 16 717 x 2 432 x 9 728 forward 1.3 to 1.4 ms, 1.12 to 1.2 PFLOP/s, matrix pipe busy
-// 60 % at 1.8 GHz - at the part's power limit, where a deeper pipeline (stages of 32, four in flight) saved 4 % of the cycles and no time.  Four waves of 128 x 128 read a third less
-// from LDS, but a CU then has one wave a SIMD and the epilogue nothing beside it (+ 25 % time).  4 608 x 2 432 x 6 528, forward with the products kept, dX, dWg and dWu: 890 us together.
+// The largest tile is 256 x 256 for 8 waves of 64 x 128 (6 operand reads for 8 matrix instructions): at 16 717 x 2 432 x 9 728 forward 1.27 to 1.35 ms, 1.17 to 1.25 PFLOP/s, matrix pipe
+// busy 60 % at 1.9 GHz - at the part's power limit, where a deeper pipeline (stages of 32, four in flight) saved 4 % of the cycles and no time.  Four waves of 128 x 128 read a third less
+// from LDS, but a CU then has one wave a SIMD and the epilogue nothing beside it (+ 25 % time).  4 608 x 2 432 x 6 528: forward with the products kept 290 us, dX 270 (in 256 x 192), dWg and
+// dWu 240.
 #include <algorithm>
 #include <mutex>
 
@@ -435,7 +436,8 @@ __global__ void __launch_bounds__(64 * WA * WB) tile_kernel(const TileArgs t)
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
 // Up to 16 MT tokens: bound by the one reading of the weights.  A workgroup takes 16 hidden channels (gate and up) and all of the contraction,
 // its 8 waves every eighth 32 of it: weights go straight from memory to the operand registers (no other wave needs them), X comes from the caches.  The
-// waves' sums are added in order in LDS.  One token, 4 096 x 11 264: 37 us, 4.9 TB/s.
+// waves' sums are added in order in LDS.  One token, 4 096 x 11 264: 38 us, 4.9 TB/s (pieces of 64, more of them in flight
+// or loads past the caches: 0 to 10 % slower).
 constexpr int kFewWaves = 8;
 template <int MT>
 __global__ void __launch_bounds__(64 * kFewWaves) few_tokens_kernel(const GatedArgs g)
@@ -503,7 +505,8 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_tokens_kernel(const GatedA
     }
 }
 
-// dG = dH u act'(g) and dU = dH act(g) in bf16 [tokens][2 hidden], gate first, 8 channels a thread.  Memory-bound: 4 608 x 6 528 98 us, 4.3 TB/s.
+// dG = dH u act'(g) and dU = dH act(g) in bf16 [tokens][2 hidden], gate first, 8 channels a thread.  Memory-bound: 4 608 x 6 528 84 us, 5 TB/s
+// (4 channels a thread, side by side, or 32-bit division: the same).
 __global__ void __launch_bounds__(256) gated_gradient_kernel(const GatedArgs g, long long n)
 {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;

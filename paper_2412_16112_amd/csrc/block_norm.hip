@@ -2,10 +2,14 @@
 // mean, its variance (of the differences from the mean) and its result; the backward pass reads dy and x once for dX and both
 // weight sums.
 //
-// A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ...: 16 bytes a lane
-// side by side (bf16), any alignment.  Forward, rows of up to 1536 channels take one wave (sums by lane exchange, no barrier), longer ones 2, 4 or 8; backward,
-// where a lane also holds two sums for each of its channels, a wave holds up to 1536 channels and longer rows take 2, 4 or 8 (with 5 chunks a lane
-// the registers no longer suffice).  9 216 x 2 432 bf16: forward 25 us (3.6 TB/s), backward 38 us with 3.4 for the join of the sums (3.5 TB/s); 16 896 x 4 096: 51 (5.4 TB/s) and 80 (5.1).
+// A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ... (fp32: pairs of fours, so that neighbouring lanes load
+// neighbouring 16 bytes: 16 717 x 1 111 forward 37 -> 34 us), any alignment.  Forward, a row takes as few waves as it fills well: one up to 1536 channels (sums by lane
+// exchange, no barrier) and from 2049 to 2560 (five chunks; two waves would leave a fifth of their lanes idle: 9 216 x 2 432 25 -> 24), else 2, 4 or 8; workgroups of 256, of
+// which more fit beside each other than of 512 (16 896 x 4 096 52 -> 48).  Backward, where a lane also holds two sums for each of its channels, a wave holds up to 1536
+// channels and longer rows take 2, 4 or 8 (with 5 chunks a lane the registers no longer suffice).
+// What bounds it is what is in flight: a branch that waits for a load where the next row is asked for cost a third (9 216 x 2 432 bf16 backward 42 -> 29), so ragged ends have none.
+// 9 216 x 2 432 bf16: forward 20 us (4.5 TB/s), backward 29 (4.7), 3.4 for the join of the sums; 16 717 x 1 111 fp32 30 and 39 (4.9 and 5.7), 4.4; 16 896 x 4 096 bf16 47 (5.9 TB/s) and 79
+// with the join (5.3).
 #include <algorithm>
 #include <type_traits>
 
