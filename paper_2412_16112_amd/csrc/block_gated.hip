@@ -600,7 +600,7 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
 // in all shapes and 1 to 16 parts, at 100 to 8192 tokens and widths of 512 x 1024 to 4096 x 11264: the chosen form takes 0.3 % longer than the best of them on average, at most
 // 4 % (dW of the smallest width 11 %).  (At 2432 x 6528 dG, dU and dX of 100 tokens take 241 us in 256 x 256 tiles, 85 in deep ones, 26 in those with the
 // contraction in 8 parts; of 4608 tokens 362 in 256 x 256 tiles, which leave 76 CUs without one, 336 in 256 x 192 and 378 in small ones.)
-enum TileShape { kLarge, kMedium, kPair, kDeep };  // 256 x 256; 256 x 192; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
+enum TileShape { kLarge, kMedium, kPair, kDeep, kNarrow };  // 256 x 256; 256 x 192; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight; 64 x 128, one with six
 struct Plan {
     TileShape shape;
     int parts;
@@ -610,6 +610,10 @@ Plan plan_of(int kind, long long rows_a, long long rows_b, long long depth)
     const long long a = kind == kForward ? 2 * rows_a : rows_a, steps = (depth + kStep - 1) / kStep * (kind == kInputGrad ? 2 : 1);
     const auto up = [](long long x, long long by) { return (x + by - 1) / by; };
     const long long large = up(a, 256) * up(rows_b, 256), medium = up(a, 256) * up(rows_b, 192), small = up(a, 128) * up(rows_b, 128);
+    // Forward, where a CU each is enough for them, tiles of 32 hidden channels x 128 tokens: what few tokens wait for is the weights, and more CUs ask for them (33 and 128 tokens
+    // with weights from memory: 1536 x 4096 13 and 17 us, in 128 x 128 tiles 17 and 21; 2432 x 6528 19 and 24, 24 and 30; 4096 x 8192 31 and 37, 37 and 46; with tiles for two
+    // rounds 2048 x 8640 31 and 36, 23 and 27).
+    if (kind == kForward && up(a, 64) * up(rows_b, 128) <= 256) return {kNarrow, 1};
     Plan best = {kLarge, 1};
     double best_us = 0;
     for (int parts = 1; parts <= (kind == kForward ? 1 : 16); ++parts) {
@@ -638,20 +642,23 @@ hipError_t launch_plan(const TileArgs& t, const Plan& p, hipStream_t stream)
     // halves of cache lines, 4 to 10 % slower.  256 x 192 has four waves there, as eight would not share its loads evenly.
     constexpr int STEP = KIND == kForward ? 64 : 32, RING = 128 / STEP;
     if (p.shape == kLarge) return launch_tiles<KIND, 4, 2, 2, 4, STEP, RING>(t, p.parts, stream);
-    if constexpr (KIND == kForward)
+    if constexpr (KIND == kForward) {
+        if (p.shape == kNarrow) return launch_tiles<KIND, 1, 4, 2, 1, STEP, 6>(t, p.parts, stream);
         if (p.shape == kMedium) return launch_tiles<KIND, 4, 2, 2, 3, STEP, RING>(t, p.parts, stream);
+    }
     if constexpr (KIND == kInputGrad)
         if (p.shape == kMedium) return launch_tiles<KIND, 2, 2, 4, 3, STEP, RING>(t, p.parts, stream);
     return p.shape == kPair ? launch_tiles<KIND, 2, 2, 2, 2, 64, 2>(t, p.parts, stream) : launch_tiles<KIND, 2, 2, 2, 2, 64, 4>(t, p.parts, stream);
 }
 
 // Whether the form for few tokens is the faster one, by the times, in us, that both are expected to take with weights from memory.  It reads X again for every 16 hidden
-// channels and is not faster for a CU that has less of them than others; the tiles take the same time up to 128 tokens.  Measured, 1, 16 and 32 tokens here, 16 in tiles:
-// 2 432 x 6 528 16, 19, 23 and 23; 3 200 x 8 640 28, 35, 40 and 31; 4 096 x 11 264 38, 46, 55 and 44; 5 120 x 13 824 63, 79, 97 and 52.
+// channels and is not faster for a CU that has less of them than others; the tiles take nearly the same time up to 64 tokens.  Measured, 1, 16 and 32 tokens here, 16 in
+// tiles: 1 536 x 4 096 11, 11, 11 and 13; 2 432 x 6 528 16, 19, 23 and 19; 3 200 x 8 640 28, 35, 40 and 31; 4 096 x 11 264 38, 46, 55 and 44; 5 120 x 13 824 63, 79, 97 and 52.
 bool few_tokens(const GatedArgs& a)
 {
     if (a.tokens > 64) return false;
-    const double here = 3.1e-3 * a.channels * ((a.hidden + 4095) / 4096) * (1 + a.tokens / 64.), tiles = (9.4e-3 * a.channels + 2) * ((a.hidden + 16383) / 16384);
+    const double here = 3.1e-3 * a.channels * ((a.hidden + 4095) / 4096) * (1 + a.tokens / 64.);
+    const double tiles = a.hidden <= 8192 ? 6.7e-3 * a.channels + 2.3 : (9.4e-3 * a.channels + 2) * ((a.hidden + 16383) / 16384);
     return here <= tiles;
 }
 
