@@ -340,7 +340,7 @@ def adamw_state(param, state_bits=32):
 
 
 _dtype_of = operator.attrgetter("dtype")
-_device_of, _ptr_of, _numel, _contiguous = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous
+_device_of, _ptr_of, _numel, _contiguous, _same_size = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.is_same_size
 
 
 def _alike(tensors, dtype, device):
@@ -383,7 +383,7 @@ def _set_grads(table, params, grads):
         table[:, 1] = 0
         return
     of = params if len(have) == len(grads) else [p for p, g in zip(params, grads) if g is not None]
-    if not (_alike(have, of[0].dtype, of[0].get_device()) and all(g.shape == p.shape for g, p in zip(have, of))):
+    if not (_alike(have, of[0].dtype, of[0].get_device()) and all(map(_same_size, have, of))):
         _refuse("a gradient must be contiguous and have its parameter's shape, dtype and device")
     table[:, 1] = list(map(_ptr_of, have)) if len(have) == len(grads) else [0 if g is None else g.data_ptr() for g in grads]
 
