@@ -15,6 +15,7 @@ SIZES = [  # tokens, channels, hidden, with the tiles that the costs choose for 
     (600, 72, 8200), (3001, 4104, 264), (600, 1000, 4104),  # forward, dX and dW in 256 x 256; dW in 128 x 128, two a CU, in the first
     (2500, 136, 8200), (4609, 136, 4104), (6001, 264, 2056),  # dW in parts of 256 x 256 and of 128 x 128 two a CU, dX in parts of the latter
     (4609, 136, 8200),  # dX in parts of 256 x 192
+    (1500, 2432, 6536), (997, 4096, 11272),  # forward in two launches: full rounds of 256 x 256, the rest in 128 x 128
 ]
 
 
