@@ -41,7 +41,9 @@ const char* clear_block_last_error(void);
  * a position (clear_block_rotary_frequencies).  Angles are formed and reduced to a turn in fp64, so a far position costs no precision.
  *
  * strides: 12 values, (batch, head, token) of Q, Q_out, K, K_out.  An output is either its input itself (same pointer and strides:
- * in place) or its address range must not overlap either input's; its strides must be > 0 where the axis has more than one entry.
+ * in place) or its address range must not overlap either input's; its rows must not overlap: a stride of an axis with more than one
+ * entry steps over all that the smaller ones reach.  Where Q or K is turned in place they must share no element: their address ranges
+ * are apart, or they have strides in common and lie apart within each of their steps (slices of one projection's output).
  * K = K_out = NULL with Hk = 0: Q alone.  2 <= rot_dim <= head_dim <= 1024, rot_dim even.  dtype CLEAR_BF16 or CLEAR_F32.
  * B = 0 or N = 0 does nothing. */
 int clear_block_rotary(const void* Q, void* Q_out, int Hq, const void* K, void* K_out, int Hk, const long long* strides, long long B,

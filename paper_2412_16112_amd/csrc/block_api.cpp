@@ -48,6 +48,67 @@ Span span_of(const void* p, const long long* extent, const long long* stride, in
 bool overlap(const Span& a, const Span& b) { return a.first < b.last && b.first < a.last; }
 bool too_long(const Span& a) { return a.last > ((__int128)1 << 62); }
 
+// Axes of one or two tensors by falling stride, without those on which nobody has a second entry.
+struct Axes {
+    int n = 0;
+    long long stride[3], ep[3], eq[3];
+    // (two tensors need to agree on a stride only where both step along it); false if they do not
+    bool gather(const long long* p_extent, const long long* p_stride, const long long* q_extent, const long long* q_stride)
+    {
+        for (int i = 0; i < 3; ++i) {
+            if (p_extent[i] <= 1 && q_extent[i] <= 1) continue;
+            if (p_extent[i] > 1 && q_extent[i] > 1 && p_stride[i] != q_stride[i]) return false;
+            const long long s = p_extent[i] > 1 ? p_stride[i] : q_stride[i];
+            int at = n++;
+            for (; at > 0 && stride[at - 1] < s; --at) stride[at] = stride[at - 1], ep[at] = ep[at - 1], eq[at] = eq[at - 1];
+            stride[at] = s, ep[at] = p_extent[i], eq[at] = q_extent[i];
+        }
+        return true;
+    }
+    // Elements from the first to behind the last over the axes from `from` on.
+    __int128 span(const long long* extent, int from, long long row) const
+    {
+        __int128 s = row;
+        for (int i = from; i < n; ++i) s += (__int128)(extent[i] - 1) * stride[i];
+        return s;
+    }
+};
+// Whether no two rows of a tensor share an element, by strides that step over all that the smaller ones reach.
+bool rows_are_own(const long long* extent, const long long* stride, long long row)
+{
+    Axes a;
+    a.gather(extent, stride, extent, stride);
+    for (int i = 0; i < a.n; ++i)
+        if (a.stride[i] < a.span(a.ep, i + 1, row)) return false;
+    return true;
+}
+// Whether two tensors share no element: their ranges are apart, or they are slices of one tensor, which lie apart within every step of the strides that they have in
+// common.  (What cannot be told in this way counts as shared.)
+bool elements_apart(const void* P, const long long* p_extent, const long long* p_stride, const void* Q, const long long* q_extent, const long long* q_stride, long long row, int size)
+{
+    if (!overlap(span_of(P, p_extent, p_stride, 3, row, size), span_of(Q, q_extent, q_stride, 3, row, size))) return true;
+    __int128 d = (__int128)(uintptr_t)Q - (__int128)(uintptr_t)P;  // from P to Q
+    if (d % size) return false;
+    d /= size;
+    Axes a;
+    if (!a.gather(p_extent, p_stride, q_extent, q_stride)) return false;
+    for (int i = 0;; ++i) {
+        if (d >= a.span(a.ep, i, row) || -d >= a.span(a.eq, i, row)) return true;
+        if (i == a.n || a.stride[i] == 0) return false;
+        const __int128 s = a.stride[i], p = a.span(a.ep, i + 1, row), q = a.span(a.eq, i + 1, row);
+        __int128 k = d / s, off = d % s;  // Q's entry j on this axis lies `off` behind P's entry j + k
+        if (off < 0) off += s, --k;
+        if (p <= s && off + q <= s) {
+            d = off;
+        } else if (q <= s && p <= off) {  // P's entry j + k + 1 lies s - off behind Q's entry j, and within its step
+            d = off - s, ++k;
+        } else {
+            return false;
+        }
+        if (k >= a.ep[i] || -k >= a.eq[i]) return true;  // no two entries in one step
+    }
+}
+
 }  // namespace
 
 const char* clear_block_last_error(void) { return g_error.c_str(); }
@@ -84,6 +145,7 @@ int clear_block_rotary(const void* Q, void* Q_out, int Hq, const void* K, void* 
     }
     const Span q = span_of(Q, eq, strides, 3, head_dim, size), qo = span_of(Q_out, eq, strides + 3, 3, head_dim, size);
     if (too_long(q) || too_long(qo)) return unsupported("tensor of more than 2^62 bytes");
+    if (!rows_are_own(eq, strides + 3, head_dim)) return invalid("the rows of Q_out must not overlap");
     const bool q_in_place = Q == Q_out && std::equal(strides, strides + 3, strides + 3);
     bool k_in_place = true;
     if (!q_in_place && overlap(q, qo)) return invalid("Q_out must be Q itself or must not overlap it");
@@ -91,11 +153,12 @@ int clear_block_rotary(const void* Q, void* Q_out, int Hq, const void* K, void* 
         const Span k = span_of(K, ek, strides + 6, 3, head_dim, size), ko = span_of(K_out, ek, strides + 9, 3, head_dim, size);
         if (too_long(k) || too_long(ko)) return unsupported("tensor of more than 2^62 bytes");
         k_in_place = K == K_out && std::equal(strides + 6, strides + 9, strides + 9);
+        if (!rows_are_own(ek, strides + 9, head_dim)) return invalid("the rows of K_out must not overlap");
         if (!k_in_place && overlap(k, ko)) return invalid("K_out must be K itself or must not overlap it");
-        // (in place, Q and K may be interleaved slices of one tensor; they may not be the same elements)
         if (!q_in_place && (overlap(qo, k) || overlap(qo, ko))) return invalid("Q_out must not overlap K or K_out");
         if (!k_in_place && overlap(ko, q)) return invalid("K_out must not overlap Q");
-        if (q_in_place && k_in_place && Q == K) return invalid("Q and K must not be the same tensor in place");
+        // (what is turned in place is written while the other is read; they may be slices of one tensor)
+        if ((q_in_place || k_in_place) && !elements_apart(Q, eq, strides, K, ek, strides + 6, head_dim, size)) return invalid("Q and K must not share elements where one is turned in place");
     }
     RotaryArgs a = {};
     a.q = Q, a.k = K, a.q_out = Q_out, a.k_out = K_out;
