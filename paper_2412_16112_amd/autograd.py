@@ -8,8 +8,10 @@ Contexts (tile schedule, mask table, workspaces) are cached per (device, shape, 
 `MAX_CACHED_CONTEXTS` most recently used ones (an evicted context is destroyed once no pending backward holds it) and
 `clear_context_cache()` empties it.  Gradients need bf16 tensors: the backward kernels are built for bf16 only, and
 a call that asks for gradients of fp32 tensors is refused in the forward pass, not later inside `loss.backward()`.
+Gradients are first-order: a gradient of a gradient (create_graph=True and a loss on it) raises.
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import clear_attn as ca
 from . import clear_block as cb
@@ -63,6 +65,7 @@ class ClearAttentionFunction(torch.autograd.Function):
         return O
 
     @staticmethod
+    @once_differentiable
     def backward(fctx, dO):
         Q, K, V, O, lse = fctx.saved_tensors
         dO = dO.to(Q.dtype)
@@ -91,6 +94,7 @@ class RotaryFunction(torch.autograd.Function):
         return cb.rotary(q, k, positions, freqs, interleaved=interleaved, scale=scale)
 
     @staticmethod
+    @once_differentiable
     def backward(fctx, dq, dk):
         positions, freqs = fctx.saved_tensors
         interleaved, scale = fctx.how
@@ -117,6 +121,7 @@ class LayerNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(fctx, dy):
         x, weight, bias, stats = fctx.saved_tensors
         dx, dw, db = cb.layer_norm_backward(_rows_ok(dy), x, weight, bias, stats, weight_offset=fctx.weight_offset, need=fctx.needs_input_grad[:3])
@@ -145,6 +150,7 @@ class GatedFFFunction(torch.autograd.Function):
         return h
 
     @staticmethod
+    @once_differentiable
     def backward(fctx, dh):
         x, w_gate, w_up, pre = fctx.saved_tensors
         need = fctx.needs_input_grad

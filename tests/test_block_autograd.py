@@ -1,0 +1,72 @@
+"""The differentiable entry points without a GPU: what they hand to the library (replaced here by plain operations on the CPU) and when."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2412_16112_amd import autograd as ag
+from paper_2412_16112_amd import clear_block as cb
+from tests import block_util as ref
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Plain stand-ins for the library's calls; the list of what was called."""
+    made = []
+
+    def rotary(q, k, positions, freqs, interleaved=True, scale=1.0, inverse=False):
+        made.append("rotary")
+        return tuple(None if t is None else ref.rotary(t, positions, freqs, interleaved, scale, inverse).to(t.dtype) for t in (q, k))
+
+    def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, save_stats=False):
+        made.append("layer_norm, statistics kept" if save_stats else "layer_norm")
+        y = ref.layer_norm(x, weight, bias, eps, weight_offset)
+        return (y, torch.zeros((2,) + x.shape[:-1])) if save_stats else y
+
+    def gated_ff(x, w_gate, w_up, activation="silu", save_pre=False):
+        made.append("gated_ff, products kept" if save_pre else "gated_ff")
+        h = ref.activation(x @ w_gate.T, activation) * (x @ w_up.T)
+        return (h, torch.zeros(2, x.shape[0], w_gate.shape[0])) if save_pre else h
+    monkeypatch.setattr(cb, "rotary", rotary)
+    monkeypatch.setattr(cb, "layer_norm", layer_norm)
+    monkeypatch.setattr(cb, "gated_ff", gated_ff)
+    monkeypatch.setattr(cb, "layer_norm_backward", lambda dy, x, w, b, stats, weight_offset=0.0, need=None: (dy * 2, None if w is None else w * 2, None if b is None else b * 2))
+    monkeypatch.setattr(cb, "gated_ff_backward", lambda dh, x, wg, wu, pre, activation="silu", need=None: (x * 2, wg * 2, wu * 2))
+    return made
+
+
+X = torch.randn(6, 8, generator=torch.Generator().manual_seed(0))
+W = torch.randn(16, 8, generator=torch.Generator().manual_seed(1))
+PLACES = (torch.arange(6).view(1, 1, 6), torch.ones(1, 4, dtype=torch.float64))
+ENTRIES = {  # of one tensor that wants gradients
+    "rotary": lambda x: ag.rotary(x.view(1, 1, 6, 8), None, *PLACES)[0],
+    "rotary, keys too": lambda x: torch.cat(ag.rotary(x.view(1, 1, 6, 8), 2 * x.view(1, 1, 6, 8), *PLACES), 1),
+    "layer_norm": lambda x: ag.layer_norm(x, torch.ones(8), torch.zeros(8)),
+    "gated_ff": lambda x: ag.gated_ff(x, W, W),
+}
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+def test_a_gradient_of_a_gradient_is_refused(calls, entry):
+    """The backward passes are kernels, which have no derivative here: a penalty on a gradient must raise, not lose its term."""
+    x = X.clone().requires_grad_()
+    y = ENTRIES[entry](x)
+    grad, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (y.sum() + grad.square().sum()).backward()
+    x.grad = None
+    ENTRIES[entry](x).square().sum().backward()
+    assert x.grad is not None
+
+
+def test_the_attention_refuses_it_too(monkeypatch):
+    class Context:
+        forward_strided = staticmethod(lambda Q, K, V, lse=None: Q * V)
+        backward_strided = staticmethod(lambda Q, K, V, O, dO, lse: (dO * V, torch.zeros_like(K), dO * Q))
+    monkeypatch.setattr(ag, "_context", lambda *a: Context)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    x = torch.randn(1, 1, 4, 64).bfloat16().requires_grad_()
+    y = ag.clear_attention(x, x.detach(), x.detach(), 0, 2, 2, 1)
+    grad, = torch.autograd.grad(y.float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        grad.sum().backward()
