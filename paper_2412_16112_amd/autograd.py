@@ -85,6 +85,12 @@ def clear_attention(Q, K, V, n_text, gridH, gridW, r, mask_kind=ca.CLEAR_MASK_DI
 
 # ---- the operators around the attention (clear_block) -------------------------------------------------------------------------
 
+def _no_gradients(*tensors):
+    """Whether a call on these tensors (None skipped) needs no backward pass.  To be asked outside the Function: inside its forward gradients are off, and needs_input_grad
+    says what the tensors want, whatever the caller's mode."""
+    return not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors))
+
+
 class RotaryFunction(torch.autograd.Function):
     @staticmethod
     def forward(fctx, q, k, positions, freqs, interleaved, scale):
@@ -113,8 +119,6 @@ def rotary(q, k, positions, freqs, interleaved=True, scale=1.0):
 class LayerNormFunction(torch.autograd.Function):
     @staticmethod
     def forward(fctx, x, weight, bias, eps, weight_offset):
-        if not any(fctx.needs_input_grad[:3]):
-            return cb.layer_norm(x, weight, bias, eps=eps, weight_offset=weight_offset)
         y, stats = cb.layer_norm(x, weight, bias, eps=eps, weight_offset=weight_offset, save_stats=True)
         fctx.save_for_backward(x, weight, bias, stats)
         fctx.weight_offset = weight_offset
@@ -136,14 +140,15 @@ def _rows_ok(t):
 def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0):
     """clear_block.layer_norm, differentiable in x, weight and bias."""
     own = lambda t: t if t is None else t.contiguous()
-    return LayerNormFunction.apply(_rows_ok(x), own(weight), own(bias), eps, weight_offset)
+    x, weight, bias = _rows_ok(x), own(weight), own(bias)
+    if _no_gradients(x, weight, bias):
+        return cb.layer_norm(x, weight, bias, eps=eps, weight_offset=weight_offset)
+    return LayerNormFunction.apply(x, weight, bias, eps, weight_offset)
 
 
 class GatedFFFunction(torch.autograd.Function):
     @staticmethod
     def forward(fctx, x, w_gate, w_up, activation):
-        if not any(fctx.needs_input_grad[:3]):
-            return cb.gated_ff(x, w_gate, w_up, activation=activation)
         h, pre = cb.gated_ff(x, w_gate, w_up, activation=activation, save_pre=True)
         fctx.save_for_backward(x, w_gate, w_up, pre)
         fctx.activation = activation
@@ -160,4 +165,7 @@ class GatedFFFunction(torch.autograd.Function):
 
 def gated_ff(x, w_gate, w_up, activation="silu"):
     """clear_block.gated_ff, differentiable in x, w_gate and w_up."""
-    return GatedFFFunction.apply(x if x.dim() == 2 and x.stride(1) == 1 else x.contiguous(), w_gate, w_up, activation)
+    x = x if x.dim() == 2 and x.stride(1) == 1 else x.contiguous()
+    if _no_gradients(x, w_gate, w_up):
+        return cb.gated_ff(x, w_gate, w_up, activation=activation)
+    return GatedFFFunction.apply(x, w_gate, w_up, activation)

@@ -70,3 +70,17 @@ def test_the_attention_refuses_it_too(monkeypatch):
     grad, = torch.autograd.grad(y.float().square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         grad.sum().backward()
+
+
+@pytest.mark.parametrize("quiet", [torch.no_grad, torch.inference_mode])
+def test_nothing_is_kept_without_gradients(calls, quiet):
+    """Trainable weights under no_grad: the two products (8 bytes for each output) and the statistics are for a backward pass that never comes."""
+    weights = [W.clone().requires_grad_() for _ in range(2)]
+    scale = torch.ones(8).requires_grad_()
+    with quiet():
+        assert not ag.gated_ff(X, *weights).requires_grad and not ag.layer_norm(X, scale).requires_grad
+    assert calls == ["gated_ff", "layer_norm"]
+    assert not ag.gated_ff(X, W, W).requires_grad and not ag.layer_norm(X, scale.detach()).requires_grad  # nobody wants gradients
+    assert calls[2:] == ["gated_ff", "layer_norm"]
+    assert ag.gated_ff(X, *weights).requires_grad and ag.layer_norm(X, scale).requires_grad
+    assert calls[4:] == ["gated_ff, products kept", "layer_norm, statistics kept"]
