@@ -62,14 +62,14 @@ __device__ __forceinline__ void team_sum(float (&x)[N], float (*slots)[N], int w
 }
 
 template <typename T, typename TW, int TEAM, int CH, bool WHOLE>
-__global__ void __launch_bounds__(forward_threads(TEAM)) norm_forward_kernel(NormArgs a)
+__global__ void __launch_bounds__(forward_threads(TEAM)) norm_forward_kernel(NormArgs a, long long row_first)
 {
     constexpr int WAVES = forward_threads(TEAM) / 64, TEAMS = WAVES / TEAM;
     typedef Layout<T, TEAM, CH, WHOLE> L;
     __shared__ float slots[2][WAVES][1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x % (64 * TEAM);
     const long long total = (long long)a.groups * a.rows;
-    const long long row = (long long)blockIdx.x * TEAMS + wave / TEAM;
+    const long long row = row_first + (long long)blockIdx.x * TEAMS + wave / TEAM;
     const bool live = row < total;
     const int at = live ? (int)row : 0;
     const int g = at / a.rows, r = at - g * a.rows;
@@ -344,15 +344,21 @@ template <typename T, typename TW>
 hipError_t forward(const NormArgs& a, hipStream_t stream)
 {
     const Form f = forward_form(a.channels);
+    hipError_t e = hipSuccess;
     auto call = [&](auto team, auto ch, auto whole) {
-        constexpr int TEAM = team, CH = ch, teams = forward_threads(TEAM) / 64 / TEAM;
+        constexpr int TEAM = team, CH = ch, threads = forward_threads(TEAM), teams = threads / 64 / TEAM;
+        constexpr long long most = 0xffffffffLL / threads;  // workgroups a launch can have
         const long long rows = (long long)a.groups * a.rows;
-        norm_forward_kernel<T, TW, TEAM, CH, whole><<<dim3((unsigned)((rows + teams - 1) / teams)), dim3(forward_threads(TEAM)), 0, stream>>>(a);
+        for (long long first = 0; first < rows && e == hipSuccess; first += most * teams) {  // (one launch up to 2^23 rows and more)
+            const long long blocks = std::min(most, (rows - first + teams - 1) / teams);
+            norm_forward_kernel<T, TW, TEAM, CH, whole><<<dim3((unsigned)blocks), dim3(threads), 0, stream>>>(a, first);
+            e = hipGetLastError();
+        }
     };
     const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<1, 5>(f, call) || try_form<2, 2>(f, call) ||
                     try_form<2, 3>(f, call) || try_form<2, 4>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) || try_form<8, 3>(f, call) ||
                     try_form<8, 4>(f, call);
-    return ok ? hipGetLastError() : hipErrorInvalidValue;
+    return ok ? e : hipErrorInvalidValue;
 }
 
 template <typename T, typename TW>

@@ -1,0 +1,39 @@
+"""What the operators around the attention launch, recorded instead of run (no GPU; pointers are numbers that nothing follows)."""
+import ctypes
+import shutil
+
+import pytest
+
+from paper_2412_16112_amd import clear_attn as ca
+from tests import fake_launch
+
+pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None, reason="hipcc not found")
+MOST_THREADS = 2 ** 32 - 1  # of a launch, along an axis of its grid
+f32, i64, ptr = ctypes.c_float, ctypes.c_longlong, ctypes.c_void_p
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    return fake_launch.build(str(tmp_path_factory.mktemp("fake_launch")))
+
+
+def ll(*v):
+    return (i64 * len(v))(*v)
+
+
+@pytest.mark.parametrize("dtype", [ca.CLEAR_BF16, ca.CLEAR_F32])
+@pytest.mark.parametrize("channels", [1, 64, 512, 1024, 1111, 1536, 1537, 2048, 2432, 3100, 4096, 4097, 8192, 8193, 16384])
+@pytest.mark.parametrize("groups,rows", [(1, 77), (2, 9216), (1, 2 ** 23 - 1), (1, 2 ** 23), (1, 2 ** 24), (4, 2 ** 24 + 3), (1, 2 ** 26), (1, 2 ** 31 - 1), (2 ** 31 - 1, 1), (46340, 46340)])
+def test_layer_norm_of_any_number_of_rows(lib, groups, rows, channels, dtype):
+    """Every row once, in launches that the device can make."""
+    rc = lib.clear_block_layer_norm(ptr(1 << 50), None, None, ptr(1 << 50), None, i64(groups), i64(rows), channels, ll(rows * channels, channels, rows * channels, channels), 0,
+                                    f32(1e-6), f32(0), dtype, dtype, None)
+    made = fake_launch.launches(lib)
+    assert rc == ca.CLEAR_OK and made
+    done = 0
+    for launch in made:
+        assert launch.kernel.startswith("norm_forward_kernel<") and launch.grid_x * launch.block <= MOST_THREADS and launch.grid_y == 1 and launch.first == done
+        team = int(launch.kernel.split(",")[2])
+        done += launch.grid_x * (launch.block // 64 // team)
+    assert done - launch.block // 64 // team < groups * rows <= done
+    assert len(made) == -(-groups * rows // (MOST_THREADS // launch.block * (launch.block // 64 // team)))
