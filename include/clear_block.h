@@ -76,7 +76,7 @@ int clear_block_layer_norm(const void* X, const void* weight, const void* bias, 
                            int channels, const long long* strides, int per_group, float eps, float weight_offset, int dtype,
                            int weight_dtype, void* stream);
 
-/* Backward pass.  dY the gradient of Y, X and stats as the forward pass had and gave them; writes (each may be NULL, not all)
+/* Backward pass.  dY the gradient of Y, X and stats as the forward pass had and gave them; writes (each may be NULL, but not all where there are rows)
  *     dX = (dyw - mean(dyw) - xhat * mean(dyw * xhat)) / sqrt(var + eps),  dyw = dy * (weight_offset + weight),
  *     d_weight = sum dy * xhat,  d_bias = sum dy   over the rows (of a group with per_group, else of all groups; 0 for no rows),
  * the latter two laid out and typed like weight.  strides: (group, row) of dY, X, dX, 6 values; dX may be dY itself (same strides).
@@ -102,7 +102,7 @@ typedef enum {
 int clear_block_gated_ff(const void* X, const void* Wg, const void* Wu, void* H, float* pre, long long tokens, int channels, int hidden,
                          long long ld_x, long long ld_gate, long long ld_up, long long ld_h, int activation, void* stream);
 
-/* Backward pass.  dH [tokens, hidden] the gradient of H, pre as the forward pass wrote it; writes (dX may be NULL; dWg and dWu both or neither)
+/* Backward pass.  dH [tokens, hidden] the gradient of H, pre as the forward pass wrote it; writes (dX may be NULL; dWg and dWu both or neither; one of them where there are tokens)
  *     dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X   with  dG = dH * u * act'(g),  dU = dH * act(g)
  * in bf16 (dG and dU are rounded to bf16 as operands of the products; 0 for no tokens).  ld: the row strides of dH, X, Wg, Wu, dX, dWg, dWu, 7 values
  * under the rules above.  workspace: clear_block_gated_ff_workspace bytes, 16-byte aligned. */

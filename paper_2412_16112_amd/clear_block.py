@@ -136,7 +136,7 @@ def rotary(q, k, positions, freqs, interleaved=True, scale=1.0, inverse=False, o
     out_k = None if k is None else torch.empty_like(k) if out_k is None else out_k
     _on_device(q, k, out_q, out_k, positions, freqs)
     for x, y in ((q, out_q), (k, out_k)):
-        if x is not None and not (y.shape == x.shape and y.dtype == x.dtype and x.stride(3) == 1 and y.stride(3) == 1):
+        if x is not None and not (y.shape == x.shape and y.dtype == x.dtype and (x.stride(3) == 1 and y.stride(3) == 1 or x.numel() == 0)):
             _refuse("an output must have its input's shape and dtype, and channels must be contiguous")
     if freqs.dim() == 1:
         freqs = freqs[None]
@@ -172,6 +172,8 @@ def _rows(x):
 
 
 def _row_strides(t, name):
+    if t.numel() == 0:  # (whatever its strides, it counts as contiguous)
+        return [0, t.shape[-1]]
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         _refuse("%s: channels must be contiguous" % name)
     if t.dim() == 3:
@@ -266,6 +268,8 @@ def _matrix(t, name, width):
         if not t.is_contiguous():
             _refuse("%s: a tensor of %d axes must be contiguous" % (name, t.dim()))
         t = t.reshape(-1, width)
+    if t.shape[0] == 0:  # (whatever its strides)
+        return 0, width
     if t.stride(1) != 1:
         _refuse("%s: the last axis must be contiguous" % name)
     return t.shape[0], max(t.stride(0), width) if t.shape[0] <= 1 else t.stride(0)

@@ -263,8 +263,8 @@ int clear_block_layer_norm_backward(const void* dY, const void* X, const void* w
     const int rc = check_norm(groups, rows, channels, strides, 6, dtype, weight_dtype);
     if (rc != CLEAR_OK) return rc;
     if (!std::isfinite(weight_offset)) return invalid("weight_offset must be finite");
-    if (!dX && !d_weight && !d_bias) return invalid("one of dX, d_weight, d_bias must be non-NULL");
-    const bool some = groups > 0 && rows > 0;
+    const bool some = groups > 0 && rows > 0;  // (without rows dX has no elements, and may have no address)
+    if (some && !dX && !d_weight && !d_bias) return invalid("one of dX, d_weight, d_bias must be non-NULL");
     if (some && (!dY || !X || !stats)) return invalid("dY, X and stats must be non-NULL");
     if (some && (d_weight || d_bias) && !workspace) return invalid("d_weight and d_bias need a workspace");
     if (per_group && groups > 65535) return unsupported("at most 65535 groups with a weight each");
@@ -391,7 +391,7 @@ int clear_block_gated_ff_backward(const void* dH, const void* X, const void* Wg,
     if (rc != CLEAR_OK) return rc;
     if (activation < CLEAR_ACT_SILU || activation > CLEAR_ACT_GELU_ERF) return invalid("unknown activation");
     if ((dWg == nullptr) != (dWu == nullptr)) return invalid("dWg and dWu go together: both or neither");
-    if (!dX && !dWg) return invalid("one of dX and dWg, dWu must be non-NULL");
+    if (!dX && !dWg) return tokens > 0 ? invalid("one of dX and dWg, dWu must be non-NULL") : CLEAR_OK;  // (without tokens dX has no elements, and may have no address)
     if (tokens > 0 && (!dH || !X || !Wg || !Wu || !pre || !workspace)) return invalid("dH, X, Wg, Wu, pre and workspace must be non-NULL");
     if (!aligned(dH, 16) || !aligned(X, 16) || !aligned(Wg, 16) || !aligned(Wu, 16) || !aligned(pre, 16) || !aligned(dX, 16) || !aligned(dWg, 16) || !aligned(dWu, 16) ||
         !aligned(workspace, 16))
