@@ -92,7 +92,7 @@ long long clear_block_layer_norm_workspace(long long groups, long long rows, int
  * H = act(X Wg^T) * (X Wu^T) for X [tokens, channels] and the weights Wg, Wu [hidden, channels]: both products, the activation
  * and the product in one pass.  bf16, fp32 accumulation, one rounding on output.  pre: NULL, or fp32 [2, tokens, hidden], which receives
  * the two products (gate first) for the backward pass.  ld_x, ld_gate, ld_up, ld_h: elements from one row to the next.  Pointers 16-byte
- * aligned; channels, hidden and the row strides multiples of 8; row strides < 2^20 and tokens < 2^31.  A few tokens take a form that
+ * aligned; channels, hidden and the row strides multiples of 8; row strides < 2^20 (those of a single token are not looked at) and tokens < 2^31.  A few tokens take a form that
  * streams the weights once. */
 typedef enum {
     CLEAR_ACT_SILU = 0,      /* g / (1 + e^-g) */

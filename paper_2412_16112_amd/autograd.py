@@ -159,13 +159,20 @@ class GatedFFFunction(torch.autograd.Function):
     def backward(fctx, dh):
         x, w_gate, w_up, pre = fctx.saved_tensors
         need = fctx.needs_input_grad
-        dx, dg, du = cb.gated_ff_backward(dh.contiguous(), x, w_gate, w_up, pre, activation=fctx.activation, need=(need[0], need[1] or need[2]))
+        dx, dg, du = cb.gated_ff_backward(_tokens_ok(dh), x, w_gate, w_up, pre, activation=fctx.activation, need=(need[0], need[1] or need[2]))
         return dx, dg if need[1] else None, du if need[2] else None, None
 
 
+def _tokens_ok(t):
+    """t, or a copy where the projection would not take its layout: rows 16-byte aligned, a multiple of 8 elements and under 2^20 apart (a single row anywhere)."""
+    if t.dim() != 2 or t.stride(1) != 1 or (t.shape[0] > 1 and not (t.shape[1] <= t.stride(0) < 1 << 20 and t.stride(0) % 8 == 0)):
+        t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
 def gated_ff(x, w_gate, w_up, activation="silu"):
-    """clear_block.gated_ff, differentiable in x, w_gate and w_up."""
-    x = x if x.dim() == 2 and x.stride(1) == 1 else x.contiguous()
+    """clear_block.gated_ff, differentiable in x, w_gate and w_up.  x may lie in any way (it is copied where the projection needs it)."""
+    x = _tokens_ok(x)
     if _no_gradients(x, w_gate, w_up):
         return cb.gated_ff(x, w_gate, w_up, activation=activation)
     return GatedFFFunction.apply(x, w_gate, w_up, activation)

@@ -272,7 +272,7 @@ def _matrix(t, name, width):
         return 0, width
     if t.stride(1) != 1:
         _refuse("%s: the last axis must be contiguous" % name)
-    return t.shape[0], max(t.stride(0), width) if t.shape[0] <= 1 else t.stride(0)
+    return t.shape[0], width if t.shape[0] <= 1 else t.stride(0)
 
 
 def _activation(name):

@@ -342,6 +342,8 @@ int clear_block_adamw_decode(const void* m, const float* m_scale, const void* v,
 
 namespace {
 
+// A single row has no stride: what its tensor says is not looked at.
+long long row_stride(long long rows, long long ld, int width) { return rows == 1 ? width : ld; }
 // Sizes and row strides of the gated projection.
 int check_gated(long long tokens, int channels, int hidden, const long long* ld, const int* width, int n_ld)
 {
@@ -364,6 +366,7 @@ Span rows_of(const void* p, long long rows, long long ld, int width, int size)
 int clear_block_gated_ff(const void* X, const void* Wg, const void* Wu, void* H, float* pre, long long tokens, int channels, int hidden, long long ld_x,
                          long long ld_gate, long long ld_up, long long ld_h, int activation, void* stream)
 {
+    ld_x = row_stride(tokens, ld_x, channels), ld_h = row_stride(tokens, ld_h, hidden);
     const long long ld[4] = {ld_x, ld_gate, ld_up, ld_h};
     const int width[4] = {channels, channels, channels, hidden};
     const int rc = check_gated(tokens, channels, hidden, ld, width, 4);
@@ -383,10 +386,12 @@ int clear_block_gated_ff(const void* X, const void* Wg, const void* Wu, void* H,
 }
 
 int clear_block_gated_ff_backward(const void* dH, const void* X, const void* Wg, const void* Wu, const float* pre, void* dX, void* dWg, void* dWu, long long tokens,
-                                  int channels, int hidden, const long long* ld, int activation, void* workspace, void* stream)
+                                  int channels, int hidden, const long long* strides, int activation, void* workspace, void* stream)
 {
-    if (!ld) return invalid("ld is NULL");
+    if (!strides) return invalid("ld is NULL");
     const int width[7] = {hidden, channels, channels, channels, channels, channels, channels};
+    long long ld[7];
+    for (int i = 0; i < 7; ++i) ld[i] = i == 2 || i == 3 || i > 4 ? strides[i] : row_stride(tokens, strides[i], width[i]);  // dH, X and dX have a row for each token
     const int rc = check_gated(tokens, channels, hidden, ld, width, 7);
     if (rc != CLEAR_OK) return rc;
     if (activation < CLEAR_ACT_SILU || activation > CLEAR_ACT_GELU_ERF) return invalid("unknown activation");

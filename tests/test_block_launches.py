@@ -37,3 +37,25 @@ def test_layer_norm_of_any_number_of_rows(lib, groups, rows, channels, dtype):
         done += launch.grid_x * (launch.block // 64 // team)
     assert done - launch.block // 64 // team < groups * rows <= done
     assert len(made) == -(-groups * rows // (MOST_THREADS // launch.block * (launch.block // 64 // team)))
+
+
+def gated(lib, tokens, ld_x, ld_h):
+    rc = lib.clear_block_gated_ff(ptr(1 << 40), ptr(2 << 40), ptr(3 << 40), ptr(4 << 40), None, i64(tokens), 64, 128, i64(ld_x), i64(64), i64(64), i64(ld_h), 0, None)
+    return rc, fake_launch.launches(lib)
+
+
+def gated_backward(lib, tokens, ld):
+    rc = lib.clear_block_gated_ff_backward(ptr(1 << 40), ptr(2 << 40), ptr(3 << 40), ptr(4 << 40), ptr(5 << 40), ptr(6 << 40), ptr(7 << 40), ptr(8 << 40), i64(tokens), 64, 128,
+                                           ll(*ld), 0, ptr(9 << 40), None)
+    return rc, fake_launch.launches(lib)
+
+
+@pytest.mark.parametrize("stride", [1 << 20, 512 * 2432, (1 << 40) + 4, 100, 8, 0])
+def test_the_row_stride_of_a_single_token_means_nothing(lib, stride):
+    """The last token of a sequence is a row whose stride is the sequence's length."""
+    plain = gated(lib, 1, 64, 128)
+    assert plain[0] == ca.CLEAR_OK and plain[1] and gated(lib, 1, stride, stride) == plain
+    plain = gated_backward(lib, 1, (128, 64, 64, 64, 64, 64, 64))
+    assert plain[0] == ca.CLEAR_OK and gated_backward(lib, 1, (stride, stride, 64, 64, stride, 64, 64)) == plain
+    assert gated(lib, 2, stride, 128)[0] != ca.CLEAR_OK and gated(lib, 2, 64, stride)[0] != ca.CLEAR_OK
+    assert gated_backward(lib, 1, (128, 64, stride, 64, 64, 64, 64))[0] != ca.CLEAR_OK  # (a weight has rows)
