@@ -18,12 +18,12 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ca.ClearAttnError(ca.CLEAR_ERR_INVALID_ARG, "state_bits must be 32 or 8")
         self.hyper = dict(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
-        self.state_bits, self.steps = state_bits, 0
+        self.state_bits = state_bits
         self.masters = [p.detach().float().clone() for p in self.params] if masters else None
         states = [cb.adamw_state(p.detach(), state_bits) for p in self.params]
         self.exp_avgs, self.exp_avg_sqs = [s[0] for s in states], [s[1] for s in states]
         self.scales = [s[2] for s in states] if state_bits == 8 else None
-        # one table of descriptors for each (device, dtype)
+        # one table of descriptors for each (device, dtype), with the number of updates that each of its parameters has had
         self._tables = []
         places = {}
         for i, p in enumerate(self.params):
@@ -32,22 +32,34 @@ class AdamW:
             of = lambda kept: None if kept is None else [kept[i] for i in members]
             params = [self.params[i].detach() for i in members]
             ca._dtype_code(params[0])
-            self._tables.append((members, params, cb._table(params, of(self.exp_avgs), of(self.exp_avg_sqs), of(self.masters), of(self.scales))))
+            self._tables.append((members, params, cb._table(params, of(self.exp_avgs), of(self.exp_avg_sqs), of(self.masters), of(self.scales)), [0] * len(members)))
+
+    @property
+    def steps(self):
+        """The updates of the parameter that has had most of them.  Set, it holds for all."""
+        return max((max(counts) for _, _, _, counts in self._tables), default=0)
+
+    @steps.setter
+    def steps(self, n):
+        for _, _, _, counts in self._tables:
+            counts[:] = [n] * len(counts)
 
     def step(self, grads=None, grad_scale=None, stream=None, **hyper):
-        """One step with the parameters' .grad, or with `grads` (a list in their order); entries that are None are skipped.  Keyword arguments
+        """One step with the parameters' .grad, or with `grads` (a list in their order); entries that are None are skipped: a parameter counts its own updates.  Keyword arguments
         (lr, ...) hold for this step only.  grad_scale: an fp32 device scalar that the gradients are multiplied by."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
         h = dict(self.hyper, **hyper)
-        for members, params, table in self._tables:  # (everything is checked before anything is updated)
+        for members, params, table, _ in self._tables:  # (everything is checked before anything is updated)
             if any(self.params[i].data_ptr() != p.data_ptr() for i, p in zip(members, params)):
                 raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "a parameter has moved since the optimizer was made")
             cb._set_grads(table, params, [grads[i] for i in members])
-        self.steps += 1
-        for members, params, table in self._tables:
-            cb._launch(table, params[0], self.state_bits == 8, self.steps, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], grad_scale, stream)
+        for _, params, table, counts in self._tables:
+            for n in sorted(set(counts)):  # (parameters that have had as many updates go together: all of them, unless gradients were missing; those without one are skipped)
+                some = table if counts.count(n) == len(counts) else table[[c == n for c in counts]]
+                cb._launch(some, params[0], self.state_bits == 8, n + 1, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], grad_scale, stream)
+            counts[:] = [c + (grad != 0) for c, grad in zip(counts, table[:, 1].tolist())]
 
     def zero_grad(self):
         for p in self.params:
