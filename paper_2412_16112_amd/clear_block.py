@@ -392,9 +392,12 @@ def _set_grads(table, params, grads):
     table[:, 1] = list(map(_ptr_of, have)) if len(have) == len(grads) else [0 if g is None else g.data_ptr() for g in grads]
 
 
-def _launch(table, first, eight, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream):
-    if grad_scale is not None and not (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == first.device):
+def _check_scale(grad_scale, device):
+    if grad_scale is not None and not (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == device):
         _refuse("grad_scale must be one fp32 value on the parameters' device")
+
+
+def _launch(table, first, eight, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream):
     _call("clear_block_adamw", first.device, stream, len(table), table.ctypes.data, ca._dtype_code(first), 8 if eight else 32, lr, beta1, beta2, eps, weight_decay, step, _ptr(grad_scale))
 
 
@@ -410,6 +413,7 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1=0.9, beta2=
         return
     table = _table(params, exp_avgs, exp_avg_sqs, masters, scales)
     _set_grads(table, params, grads)
+    _check_scale(grad_scale, params[0].device)
     _launch(table, params[0], scales is not None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream)
 
 

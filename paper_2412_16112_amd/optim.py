@@ -51,9 +51,10 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
         h = dict(self.hyper, **hyper)
-        for members, params, table, _ in self._tables:  # (everything is checked before anything is updated)
+        for members, params, table, _ in self._tables:  # (everything is checked before anything is updated; the numbers, which are everybody's, with the first launch)
             if any(self.params[i].data_ptr() != p.data_ptr() for i, p in zip(members, params)):
                 raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "a parameter has moved since the optimizer was made")
+            cb._check_scale(grad_scale, params[0].device)
             cb._set_grads(table, params, [grads[i] for i in members])
         for _, params, table, counts in self._tables:
             for n in sorted(set(counts)):  # (parameters that have had as many updates go together: all of them, unless gradients were missing; those without one are skipped)

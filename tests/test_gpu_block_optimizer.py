@@ -1,7 +1,10 @@
 """The optimizer class: what it counts, checks and keeps.  The step itself is test_gpu_block_adamw's; here it is the oracle, called with each parameter's own numbers."""
+import types
+
 import pytest
 import torch
 
+from paper_2412_16112_amd import clear_attn as ca
 from paper_2412_16112_amd import clear_block as cb
 from paper_2412_16112_amd.optim import AdamW
 from tests.test_gpu_block_adamw import HYPER, tensors
@@ -36,3 +39,40 @@ def test_a_parameter_counts_its_own_updates(bits):
     late.step([torch.full((300,), 7.0, device="cuda"), None])
     # m / (1 - beta1) = g and sqrt(v / (1 - beta2)) = |g|, to a few roundings of fp32: a first step is lr
     assert bool(((late.params[0] + 0.25).abs() <= 8 * 2.0 ** -24).all())
+
+
+def test_a_refused_step_changes_nothing():
+    params, grads = tensors(torch.float32, seed=3, sizes=[100, 300])
+    params.append(torch.randn(50, device="cuda").bfloat16())
+    grads.append(torch.randn(50, device="cuda").bfloat16())
+    opt = AdamW(params, **HYPER)
+    opt.step(grads)
+    before = moved(opt)
+    bad = [dict(lr=float("nan")), dict(lr=-1.0), dict(beta1=1.0), dict(eps=float("inf")), dict(weight_decay=-1.0), dict(grad_scale=torch.ones(())), dict(grad_scale=torch.ones(2, device="cuda")),
+           dict(grad_scale=torch.ones((), device="cuda", dtype=torch.bfloat16)), dict(grads=grads[:2]), dict(grads=[grads[0], grads[1].bfloat16(), grads[2]]), dict(grads=[*grads[:2], grads[2].float()])]
+    for change in bad:
+        with pytest.raises(ca.ClearAttnError):
+            opt.step(**dict(dict(grads=grads), **change))
+        assert opt.steps == 1 and all(torch.equal(a, b) for a, b in zip(moved(opt), before)), change
+    same = AdamW([p.clone() for p in params], **HYPER)
+    with pytest.raises(ca.ClearAttnError):
+        same.step(grads, lr=float("nan"))
+    assert same.steps == 0
+    opt.step(grads)
+    assert opt.steps == 2
+
+
+def test_a_scale_that_is_not_everybodys_is_refused_before_anybody_is_updated(monkeypatch):
+    """Parameters on several devices: a scale on one of them is no use to the others.  (The second device is played by a table whose parameters say so.)"""
+    params, grads = tensors(torch.float32, seed=3, sizes=[100])
+    params.append(torch.randn(50, device="cuda").bfloat16())
+    grads.append(torch.randn(50, device="cuda").bfloat16())
+    opt = AdamW(params, **HYPER)
+    before = moved(opt)
+    opt._tables[1][1][0] = types.SimpleNamespace(device=torch.device("cuda", 1), dtype=torch.bfloat16, data_ptr=params[1].data_ptr)
+    monkeypatch.setattr(cb, "_set_grads", lambda *a: None)
+    opt._tables[0][2][:, 1] = grads[0].data_ptr()
+    with pytest.raises(ca.ClearAttnError):
+        opt.step(grads, grad_scale=torch.ones((), device="cuda"))
+    torch.cuda.synchronize()
+    assert opt.steps == 0 and all(torch.equal(a, b) for a, b in zip(moved(opt), before))
