@@ -76,3 +76,47 @@ def test_a_scale_that_is_not_everybodys_is_refused_before_anybody_is_updated(mon
         opt.step(grads, grad_scale=torch.ones((), device="cuda"))
     torch.cuda.synchronize()
     assert opt.steps == 0 and all(torch.equal(a, b) for a, b in zip(moved(opt), before))
+
+
+@pytest.mark.parametrize("masters", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_resumed_optimizer_goes_on_bit_for_bit(bits, masters, tmp_path):
+    params, grads = tensors(torch.bfloat16, seed=31)
+    opt = AdamW(params, state_bits=bits, masters=masters, **HYPER)
+    some = lambda turn: [None if i == 2 and turn < 2 else g.roll(turn) for i, g in enumerate(grads)]
+    for turn in range(3):
+        opt.step(some(turn))
+    torch.save({"opt": opt.state_dict(), "params": params}, tmp_path / "kept")
+    loaded = torch.load(tmp_path / "kept", weights_only=True)
+    other = [p.cuda() for p in loaded["params"]]
+    again = AdamW(other, lr=0.5, state_bits=bits, masters=masters)
+    again.load_state_dict(loaded["opt"])
+    assert again.hyper == opt.hyper and again.steps == opt.steps == 3
+    for turn in range(3, 5):
+        opt.step(some(turn))
+        again.step(some(turn))
+    assert all(torch.equal(a, b) for a, b in zip(moved(opt), moved(again)))
+
+
+def test_a_state_that_does_not_fit_is_refused_whole():
+    params, grads = tensors(torch.float32, seed=33, sizes=[300, 20])
+    opt = AdamW(params, state_bits=8, **HYPER)
+    opt.step(grads)
+    before, good = moved(opt), opt.state_dict()
+    for change in (dict(state_bits=32), dict(updates=[1]), dict(updates=[1, -1]), dict(exp_avgs=good["exp_avgs"][:1]), dict(exp_avg_sqs=[t.float() for t in good["exp_avg_sqs"]]),
+                   dict(exp_avgs=[good["exp_avgs"][0], torch.zeros(21, dtype=torch.int8)]), dict(scales=None), dict(scales=[good["scales"][0]]), dict(masters=[p.clone() for p in params])):
+        with pytest.raises(ca.ClearAttnError):
+            opt.load_state_dict(dict(good, **change))
+        assert all(torch.equal(a, b) for a, b in zip(moved(opt), before)) and opt.steps == 1, change
+    with pytest.raises(ca.ClearAttnError):
+        opt.load_state_dict({"exp_avgs": []})
+
+
+def test_states_are_not_replaced_in_silence():
+    """A step works on the tensors that were written down: others in their place would be ignored."""
+    opt = AdamW([torch.zeros(10, device="cuda")], masters=True, state_bits=8)
+    for name in ("exp_avgs", "exp_avg_sqs", "scales", "masters"):
+        with pytest.raises(AttributeError):
+            setattr(opt, name, [None])
+        with pytest.raises(TypeError):
+            getattr(opt, name)[0] = None
