@@ -364,7 +364,10 @@ def _table(params, exp_avgs, exp_avg_sqs, masters, scales):
     if not (_alike(exp_avgs, m_type, device) and _alike(exp_avg_sqs, v_type, device) and list(map(_numel, exp_avgs)) == n and list(map(_numel, exp_avg_sqs)) == n):
         _refuse("states must be contiguous, on the parameters' device, of their sizes, and fp32, or int8 and uint8 with scales")
     table = np.zeros((len(n), 8), dtype=np.int64)
-    table[:, 0] = list(map(_ptr_of, params))
+    places = list(map(_ptr_of, params))
+    if len(set(places)) != len(places) and len(set(full := [p for p, k in zip(places, n) if k])) != len(full):
+        _refuse("a parameter is there twice: it would be updated by two descriptors at once")
+    table[:, 0] = places
     if masters is not None:
         if not (_alike(masters, torch.float32, device) and list(map(_numel, masters)) == n):
             _refuse("masters must be contiguous fp32, of their parameters' sizes and on their device")

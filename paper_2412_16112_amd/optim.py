@@ -36,6 +36,10 @@ class AdamW:
             ca._dtype_code(params[0])
             self._tables.append((members, params, cb._table(params, of(self.exp_avgs), of(self.exp_avg_sqs), of(self.masters), of(self.scales)), [0] * len(members)))
 
+        spans = sorted((p.device.index, p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
+        if any(a[0] == b[0] and b[1] < a[2] for a, b in zip(spans, spans[1:])):
+            raise ca.ClearAttnError(ca.CLEAR_ERR_INVALID_ARG, "parameters share memory")
+
     exp_avgs = property(lambda self: self._exp_avgs)
     exp_avg_sqs = property(lambda self: self._exp_avg_sqs)
     scales = property(lambda self: self._scales)

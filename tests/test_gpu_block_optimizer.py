@@ -120,3 +120,19 @@ def test_states_are_not_replaced_in_silence():
             setattr(opt, name, [None])
         with pytest.raises(TypeError):
             getattr(opt, name)[0] = None
+
+
+def test_a_parameter_given_twice_is_refused():
+    """Two descriptors of one tensor would be updated side by side, each reading what the other writes."""
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    other, empty = torch.ones(10, device="cuda"), torch.ones(0, device="cuda")
+    for params in ([p, other, p], [p, p.view(3, 100)], [p, p[:100]], [p[200:], p], [p, p[299:]]):
+        with pytest.raises(ca.ClearAttnError) as e:
+            AdamW(params)
+        assert e.value.status == ca.CLEAR_ERR_INVALID_ARG
+    states = [cb.adamw_state(p) for _ in range(2)]
+    with pytest.raises(ca.ClearAttnError):
+        cb.adamw_step([p, p], [g, g], [s[0] for s in states], [s[1] for s in states], step=1, lr=0.1)
+    assert bool((p == 1).all()) and bool((other == 1).all())
+    AdamW([p[:150], p[150:], empty, empty.clone(), empty]).step([g[:150], g[150:], empty, None, empty])  # neighbours, and nothing several times
+    assert bool((p < 1).all())
