@@ -3,7 +3,8 @@ positions, layer norm, gated feed-forward projection, AdamW step.  Argument mars
 device memory, workspaces and streams; every step runs in the HIP kernels, and there is no fallback.
 
 Refusals raise ClearAttnError, as in clear_attn.  Each call enqueues on `stream` (default: torch's current stream of the tensors' device); with another
-one the caller orders it with torch's, before the call (results are allocated for torch's stream) and after it."""
+one the caller orders it with torch's, before the call (results are allocated for torch's stream) and after it.  These calls are not differentiable (autograd.py has
+the forms that are); the tensors that a caller gives them to write into - outputs, parameters, masters - count as changed for autograd afterwards."""
 import ctypes
 import operator
 
@@ -93,6 +94,10 @@ def _call(name, device, stream, *args):
     return s
 
 
+# A tensor that was written into counts as changed for autograd, as after one of torch's own in-place operations.
+_changed = torch.autograd.graph.increment_version
+
+
 def _new_like(t):
     """A new contiguous tensor of t's shape, dtype and device (half the time of torch.empty, which is given all three)."""
     return torch.empty_like(t, memory_format=torch.contiguous_format)
@@ -132,6 +137,7 @@ def rotary(q, k, positions, freqs, interleaved=True, scale=1.0, inverse=False, o
         _refuse("q and k must agree in batch, tokens, head_dim and dtype", CLEAR_ERR_MISMATCH)
     dtype = ca._dtype_code(q)
     # (a new tensor keeps the order of a dense one's strides)
+    given = [t for t in (out_q, out_k if k is not None else None) if t is not None]
     out_q = torch.empty_like(q) if out_q is None else out_q
     out_k = None if k is None else torch.empty_like(k) if out_k is None else out_k
     _on_device(q, k, out_q, out_k, positions, freqs)
@@ -154,6 +160,8 @@ def rotary(q, k, positions, freqs, interleaved=True, scale=1.0, inverse=False, o
     _call("clear_block_rotary", q.device, stream, q.data_ptr(), out_q.data_ptr(), Hq, _ptr(k), _ptr(out_k), 0 if k is None else k.shape[1], strides, B, N, d,
           2 * half, int(bool(interleaved)), positions.data_ptr(), 64 if positions.dtype == torch.int64 else 32, _Strides3(*ps), axes, freqs.data_ptr(), scale,
           int(bool(inverse)), dtype)
+    if given:
+        _changed(given)
     return out_q, out_k
 
 
@@ -217,6 +225,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, out=None,
     stats = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if save_stats else None
     _call("clear_block_layer_norm", x.device, stream, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(stats), groups, rows, C,
           _Strides4(*_row_strides(x, "x"), *_row_strides(y, "out")), per_group, eps, weight_offset, dtype, wcode)
+    if out is not None:
+        _changed(out)
     return (y, stats) if save_stats else y
 
 
@@ -298,6 +308,8 @@ def gated_ff(x, w_gate, w_up, activation="silu", out=None, save_pre=False, strea
     _on_device(x, w_gate, w_up, h)
     pre = torch.empty((2, M, F), dtype=torch.float32, device=x.device) if save_pre else None
     _call("clear_block_gated_ff", x.device, stream, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(pre), M, C, F, ld_x, ld_g, ld_u, ld_h, act)
+    if out is not None:
+        _changed(out)
     return (h, pre) if save_pre else h
 
 
@@ -385,14 +397,26 @@ def _table(params, exp_avgs, exp_avg_sqs, masters, scales):
 
 
 def _set_grads(table, params, grads):
+    """Writes the gradients into a table; the numbers of the parameters that have one, or None for all of them."""
     have = [g for g in grads if g is not None]
     if not have:
         table[:, 1] = 0
-        return
+        return []
     of = params if len(have) == len(grads) else [p for p, g in zip(params, grads) if g is not None]
     if not (_alike(have, of[0].dtype, of[0].get_device()) and all(map(_same_size, have, of))):
         _refuse("a gradient must be contiguous and have its parameter's shape, dtype and device")
-    table[:, 1] = list(map(_ptr_of, have)) if len(have) == len(grads) else [0 if g is None else g.data_ptr() for g in grads]
+    if len(have) == len(grads):
+        table[:, 1] = list(map(_ptr_of, have))
+        return None
+    table[:, 1] = [0 if g is None else g.data_ptr() for g in grads]
+    return [i for i, g in enumerate(grads) if g is not None]
+
+
+def _updated(some, *lists):
+    """The parameters and masters of a call (None skipped), all or `some` of each, have been written.  (The states are in no graph.)"""
+    for tensors in lists:
+        if tensors is not None:
+            _changed(tensors if some is None else [tensors[i] for i in some])
 
 
 def _check_scale(grad_scale, device):
@@ -415,9 +439,10 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1=0.9, beta2=
     if count == 0:
         return
     table = _table(params, exp_avgs, exp_avg_sqs, masters, scales)
-    _set_grads(table, params, grads)
+    some = _set_grads(table, params, grads)
     _check_scale(grad_scale, params[0].device)
     _launch(table, params[0], scales is not None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream)
+    _updated(some, params, masters)
 
 
 def adamw_decode(m, m_scale, v, v_scale, stream=None):

@@ -34,7 +34,8 @@ class AdamW:
             of = lambda kept: None if kept is None else [kept[i] for i in members]
             params = [self.params[i].detach() for i in members]
             ca._dtype_code(params[0])
-            self._tables.append((members, params, cb._table(params, of(self.exp_avgs), of(self.exp_avg_sqs), of(self.masters), of(self.scales)), [0] * len(members)))
+            table = cb._table(params, of(self.exp_avgs), of(self.exp_avg_sqs), of(self.masters), of(self.scales))
+            self._tables.append((members, params, table, [0] * len(members), of(self.masters)))
 
         spans = sorted((p.device.index, p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
         if any(a[0] == b[0] and b[1] < a[2] for a, b in zip(spans, spans[1:])):
@@ -48,11 +49,11 @@ class AdamW:
     @property
     def steps(self):
         """The updates of the parameter that has had most of them.  Set, it holds for all."""
-        return max((max(counts) for _, _, _, counts in self._tables), default=0)
+        return max((max(counts) for _, _, _, counts, _ in self._tables), default=0)
 
     @steps.setter
     def steps(self, n):
-        for _, _, _, counts in self._tables:
+        for _, _, _, counts, _ in self._tables:
             counts[:] = [n] * len(counts)
 
     def step(self, grads=None, grad_scale=None, stream=None, **hyper):
@@ -62,21 +63,23 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
         h = dict(self.hyper, **hyper)
-        for members, params, table, _ in self._tables:  # (everything is checked before anything is updated; the numbers, which are everybody's, with the first launch)
+        given = []
+        for members, params, table, _, _ in self._tables:  # (everything is checked before anything is updated; the numbers, which are everybody's, with the first launch)
             if any(self.params[i].data_ptr() != p.data_ptr() for i, p in zip(members, params)):
                 raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "a parameter has moved since the optimizer was made")
             cb._check_scale(grad_scale, params[0].device)
-            cb._set_grads(table, params, [grads[i] for i in members])
-        for _, params, table, counts in self._tables:
+            given.append(cb._set_grads(table, params, [grads[i] for i in members]))
+        for (_, params, table, counts, masters), some in zip(self._tables, given):
             for n in sorted(set(counts)):  # (parameters that have had as many updates go together: all of them, unless gradients were missing; those without one are skipped)
-                some = table if counts.count(n) == len(counts) else table[[c == n for c in counts]]
-                cb._launch(some, params[0], self.state_bits == 8, n + 1, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], grad_scale, stream)
-            counts[:] = [c + (grad != 0) for c, grad in zip(counts, table[:, 1].tolist())]
+                rows = table if counts.count(n) == len(counts) else table[[c == n for c in counts]]
+                cb._launch(rows, params[0], self.state_bits == 8, n + 1, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], grad_scale, stream)
+            counts[:] = [c + 1 for c in counts] if some is None else [c + (i in some) for i, c in enumerate(counts)]
+            cb._updated(some, params, masters)
 
     def state_dict(self):
         """What load_state_dict takes: the states themselves (not copies), the masters, each parameter's number of updates and the numbers of a step."""
         updates = [0] * len(self.params)
-        for members, _, _, counts in self._tables:
+        for members, _, _, counts, _ in self._tables:
             for i, n in zip(members, counts):
                 updates[i] = n
         lists = {name: None if kept is None else list(kept) for name, kept in self._kept()}
@@ -107,7 +110,7 @@ class AdamW:
                     copies.append((a, b))
         for a, b in copies:
             a.copy_(b)
-        for members, _, _, counts in self._tables:
+        for members, _, _, counts, _ in self._tables:
             counts[:] = [state["updates"][i] for i in members]
         self.hyper = dict(state["hyper"])
 
