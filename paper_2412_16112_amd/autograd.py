@@ -91,6 +91,11 @@ def _no_gradients(*tensors):
     return not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors))
 
 
+def _channels_ok(t):
+    """t (or None), or a contiguous copy where its channels are not."""
+    return t if t is None or (t.dim() > 0 and t.stride(-1) == 1) else t.contiguous()
+
+
 class RotaryFunction(torch.autograd.Function):
     @staticmethod
     def forward(fctx, q, k, positions, freqs, interleaved, scale):
@@ -104,16 +109,14 @@ class RotaryFunction(torch.autograd.Function):
     def backward(fctx, dq, dk):
         positions, freqs = fctx.saved_tensors
         interleaved, scale = fctx.how
-        fix = lambda t: t if t is None or t.stride(-1) == 1 else t.contiguous()
         # (the transposed map: the negative angle, the same scale)
-        dq, dk = cb.rotary(fix(dq), fix(dk) if fctx.has_k else None, positions, freqs, interleaved=interleaved, scale=scale, inverse=True)
+        dq, dk = cb.rotary(_channels_ok(dq), _channels_ok(dk) if fctx.has_k else None, positions, freqs, interleaved=interleaved, scale=scale, inverse=True)
         return dq, dk, None, None, None, None
 
 
 def rotary(q, k, positions, freqs, interleaved=True, scale=1.0):
     """clear_block.rotary, differentiable in q and k (k may be None)."""
-    fix = lambda t: t if t is None or t.stride(-1) == 1 else t.contiguous()
-    return RotaryFunction.apply(fix(q), fix(k), positions, freqs, interleaved, scale)
+    return RotaryFunction.apply(_channels_ok(q), _channels_ok(k), positions, freqs, interleaved, scale)
 
 
 class LayerNormFunction(torch.autograd.Function):
@@ -134,7 +137,7 @@ class LayerNormFunction(torch.autograd.Function):
 
 def _rows_ok(t):
     """t, or a contiguous copy where its rows are not evenly spaced or its channels not contiguous (an expanded gradient, say)."""
-    return t if t.stride(-1) == 1 and t.dim() in (2, 3) else t.contiguous()
+    return t if t.dim() in (2, 3) and t.stride(-1) == 1 else t.contiguous()
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0):

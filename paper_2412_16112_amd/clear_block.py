@@ -291,13 +291,17 @@ def _activation(name):
     return ACTIVATIONS[name]
 
 
+def _gated_weights(w_gate, w_up):
+    if w_gate.dim() != 2 or w_up.shape != w_gate.shape:
+        _refuse("w_gate and w_up must be [F, C], of one shape", CLEAR_ERR_MISMATCH)
+    return w_gate.shape
+
+
 def gated_ff(x, w_gate, w_up, activation="silu", out=None, save_pre=False, stream=None):
     """clear_block_gated_ff: act(x w_gate^T) * (x w_up^T) for bf16 x [..., C] and weights [F, C] (rows at any stride: halves of one packed
     [2 F, C] weight will do).  activation: "silu", "gelu_tanh", "gelu_erf".  Returns h [..., F], or (h, pre) with save_pre (fp32 [2, rows, F]: both products)."""
     act = _activation(activation)
-    if w_gate.dim() != 2 or w_up.shape != w_gate.shape:
-        _refuse("w_gate and w_up must be [F, C], of one shape", CLEAR_ERR_MISMATCH)
-    F, C = w_gate.shape
+    F, C = _gated_weights(w_gate, w_up)
     M, ld_x = _matrix(x, "x", C)
     _, ld_g = _matrix(w_gate, "w_gate", C)
     _, ld_u = _matrix(w_up, "w_up", C)
@@ -317,13 +321,13 @@ def gated_ff_backward(dh, x, w_gate, w_up, pre, activation="silu", need=(True, T
     """clear_block_gated_ff_backward: (dx, d_w_gate, d_w_up) for what gated_ff(..., save_pre=True) was called with.  need: whether dx, and whether
     the weights' gradients are wanted (None otherwise)."""
     act = _activation(activation)
-    F, C = w_gate.shape
+    F, C = _gated_weights(w_gate, w_up)
     M, ld_x = _matrix(x, "x", C)
     rows, ld_dh = _matrix(dh, "dh", F)
     _, ld_g = _matrix(w_gate, "w_gate", C)
     _, ld_u = _matrix(w_up, "w_up", C)
-    if rows != M or w_up.shape != w_gate.shape:
-        _refuse("dh must have a row for each of x, and the weights one shape", CLEAR_ERR_MISMATCH)
+    if rows != M:
+        _refuse("dh must have a row for each of x", CLEAR_ERR_MISMATCH)
     if pre.dtype != torch.float32 or not pre.is_contiguous() or tuple(pre.shape) != (2, M, F):
         _refuse("pre must be what gated_ff(..., save_pre=True) gave for x")
     _on_device(x, dh, w_gate, w_up, pre)
