@@ -4,8 +4,9 @@
 //
 // A team of TEAM waves holds a row in chunks of 8 channels a lane: lane l of the team owns chunks l, l + 64 TEAM, ... (fp32: pairs of fours, so that neighbouring lanes load
 // neighbouring 16 bytes: 16 717 x 1 111 forward 37 -> 34 us), any alignment.  Forward, a row takes as few waves as it fills well: one up to 1536 channels (sums by lane
-// exchange, no barrier) and from 2049 to 2560 (five chunks; two waves would leave a fifth of their lanes idle: 9 216 x 2 432 25 -> 24), else 2, 4 or 8; workgroups of 256, of
-// which more fit beside each other than of 512 (16 896 x 4 096 52 -> 48).  Backward, where a lane also holds two sums for each of its channels, a wave holds up to 1536
+// exchange, no barrier) and for bf16 from 2049 to 2560 (five chunks; two waves would leave a fifth of their lanes idle: 9 216 rows of 2 056, 2 304, 2 560 channels 17.7, 19.5,
+// 18.6 us, in two waves 18.5, 19.8, 20.7; in fp32 28.2, 30.4, 32.1 and 26.7, 28.5, 31.3), else 2, 4 or 8; workgroups of 256, of which more fit beside each other than of 512
+// (16 896 x 4 096 52 -> 48).  Backward, where a lane also holds two sums for each of its channels, a wave holds up to 1536
 // channels and longer rows take 2, 4 or 8 (with 5 chunks a lane the registers no longer suffice).
 // What bounds it is what is in flight: a branch that waits for a load where the next row is asked for cost a third (9 216 x 2 432 bf16 backward 42 -> 29), so ragged ends have none.
 // 9 216 x 2 432 bf16: forward 20 us (4.5 TB/s), backward 29 (4.7), 3.4 for the join of the sums; 16 717 x 1 111 fp32 30 and 39 (4.9 and 5.7), 4.4; 16 896 x 4 096 bf16 47 (5.9 TB/s) and 79
@@ -316,14 +317,15 @@ struct Form {
     bool whole;
     Form(int team, int channels) : team(team), ch((channels + 512 * team - 1) / (512 * team)), whole(channels == 512 * team * ch) {}
 };
-Form forward_form(int channels)
+Form forward_form(int channels, bool fp32)
 {
-    const int team = channels <= 1536 || (channels > 2048 && channels <= 2560) ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
+    const int team = channels <= 1536 || (!fp32 && channels > 2048 && channels <= 2560) ? 1 : channels <= 4096 ? 2 : channels <= 8192 ? 4 : 8;
     return Form(team, channels);
 }
 Form backward_form(int channels, bool fp32)
 {
-    // (fp32 rows of 1025 to 1536 channels: three waves of one chunk, 15 waves a CU, instead of one of three, 8 a CU: 16717 x 1111 44 -> 39 us without the join)
+    // (fp32 rows of 1025 to 1536 channels: three waves of one chunk, 15 waves a CU, instead of one of three, 8 a CU: 16717 rows of 1032, 1111, 1280, 1536 channels 40.5, 42.9, 46.9,
+    // 58.4 us with the join, in one wave 43.8, 47.4, 50.7, 61.5)
     const int team = channels <= 1536 ? (fp32 && channels > 1024 ? 3 : 1) : channels <= 2 * 1536 ? 2 : channels <= 4 * 1536 ? 4 : 8;
     return Form(team, channels);
 }
@@ -343,7 +345,7 @@ bool try_form(const Form& f, F& call)
 template <typename T, typename TW>
 hipError_t forward(const NormArgs& a, hipStream_t stream)
 {
-    const Form f = forward_form(a.channels);
+    const Form f = forward_form(a.channels, sizeof(T) == 4);
     hipError_t e = hipSuccess;
     auto call = [&](auto team, auto ch, auto whole) {
         constexpr int TEAM = team, CH = ch, threads = forward_threads(TEAM), teams = threads / 64 / TEAM;
@@ -355,9 +357,9 @@ hipError_t forward(const NormArgs& a, hipStream_t stream)
             e = hipGetLastError();
         }
     };
-    const bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<1, 5>(f, call) || try_form<2, 2>(f, call) ||
-                    try_form<2, 3>(f, call) || try_form<2, 4>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) || try_form<8, 3>(f, call) ||
-                    try_form<8, 4>(f, call);
+    bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
+              try_form<2, 4>(f, call) || try_form<4, 3>(f, call) || try_form<4, 4>(f, call) || try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
+    if constexpr (sizeof(T) == 2) ok = ok || try_form<1, 5>(f, call);
     return ok ? e : hipErrorInvalidValue;
 }
 
@@ -374,9 +376,12 @@ hipError_t backward(const NormArgs& a, hipStream_t stream)
             const size_t lds = teams > 1 && (a.dw || a.db) ? (size_t)padded(a.channels) * 8 : 0;  // (at most 48 KB)
             norm_backward_kernel<T, TW, TEAM, CH, whole><<<dim3(partials, sets), dim3(threads), lds, stream>>>(a);
         };
-        bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<1, 3>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) ||
-                        try_form<4, 2>(f, call) || try_form<4, 3>(f, call) || try_form<8, 2>(f, call) || try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
-        if constexpr (sizeof(T) == 4) ok = ok || try_form<3, 1>(f, call);
+        bool ok = try_form<1, 1>(f, call) || try_form<1, 2>(f, call) || try_form<2, 2>(f, call) || try_form<2, 3>(f, call) || try_form<4, 2>(f, call) ||
+                  try_form<4, 3>(f, call) || try_form<8, 2>(f, call) || try_form<8, 3>(f, call) || try_form<8, 4>(f, call);
+        if constexpr (sizeof(T) == 4)
+            ok = ok || try_form<3, 1>(f, call);
+        else
+            ok = ok || try_form<1, 3>(f, call);
         e = ok ? hipGetLastError() : hipErrorInvalidValue;
     }
     if (e == hipSuccess && (a.dw || a.db)) {
