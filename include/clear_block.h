@@ -126,7 +126,7 @@ long long clear_block_gated_ff_workspace(long long tokens, int channels, int hid
  *     v is uint8 c:  v = scale * t^4,   t = c / 255     (the nearest of the fourth root; a v > 0 is not stored as 0)
  * with ceil(n / 256) fp32 scales each in m_scale and v_scale.  The step itself uses the new m and v before they are stored.  A state that is not
  * finite makes its block's stored states NaN (both codes 0, scales NaN).
- * `tensors` is a HOST array, read before the call returns, as are the numbers of the step: a captured graph repeats them.  No two tensors may share memory. */
+ * `tensors` is a HOST array, read before the call returns, as are the numbers of the step: a captured graph repeats them.  No two tensors may share memory.  n <= 2^35. */
 typedef struct {
     void* param;
     const void* grad;

@@ -278,8 +278,8 @@ __global__ void __launch_bounds__(kThreads) adamw_decode_kernel(const signed cha
 
 hipError_t launch_adamw(int n, const clear_block_adamw_tensor* tensors, const AdamHyper& h, int dtype, int state_bits, hipStream_t stream)
 {
-    // A launch takes as many tensors as its arguments hold and 2^24 workgroups (68 G elements).
-    constexpr unsigned kMostBlocks = 1u << 24;
+    // A launch takes as many tensors as its arguments hold, and 2^32 - 1 threads; a tensor has at most half of them.
+    constexpr unsigned kMostBlocks = 0xffffffffu / kThreads;
     auto kernel = dtype == CLEAR_BF16 ? (state_bits == 8 ? adamw_kernel<__bf16, true> : adamw_kernel<__bf16, false>)
                                       : (state_bits == 8 ? adamw_kernel<float, true> : adamw_kernel<float, false>);
     Launch l;
@@ -297,7 +297,6 @@ hipError_t launch_adamw(int n, const clear_block_adamw_tensor* tensors, const Ad
     for (int i = 0; i < n; ++i) {
         if (!tensors[i].grad || tensors[i].n == 0) continue;
         const long long need = (tensors[i].n + kChunk - 1) / kChunk;
-        if (need > kMostBlocks) return hipErrorInvalidValue;
         if (l.n == kAdamTensors || blocks + need > kMostBlocks) {
             const hipError_t e = flush();
             if (e != hipSuccess) return e;

@@ -35,7 +35,7 @@ bool known_dtype(int dtype) { return dtype == CLEAR_BF16 || dtype == CLEAR_F32; 
 int size_of(int dtype) { return dtype == CLEAR_BF16 ? 2 : 4; }
 bool aligned(const void* p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
 
-// Byte range [first, last) that a strided tensor spans; false if it does not fit 62 bits.
+// Byte range [first, last) that a strided tensor spans.
 struct Span {
     __int128 first, last;
 };
@@ -312,7 +312,7 @@ int clear_block_adamw(int n_tensors, const clear_block_adamw_tensor* tensors, in
     for (int i = 0; i < n_tensors; ++i) {
         const clear_block_adamw_tensor& t = tensors[i];
         if (t.n < 0) return invalid("a tensor has a negative number of elements");
-        if (t.n > (1LL << 36)) return unsupported("a tensor has more than 2^36 elements");
+        if (t.n > (1LL << 35)) return unsupported("a tensor has more than 2^35 elements");
         if (t.n == 0 || !t.grad) continue;
         if (!t.param || !t.m || !t.v) return invalid("param, m and v of a tensor must be non-NULL");
         if (state_bits == 8 && (!t.m_scale || !t.v_scale)) return invalid("states of 8 bits need m_scale and v_scale");

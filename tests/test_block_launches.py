@@ -5,11 +5,12 @@ import shutil
 import pytest
 
 from paper_2412_16112_amd import clear_attn as ca
+from paper_2412_16112_amd import clear_block as cb
 from tests import fake_launch
 
 pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None, reason="hipcc not found")
 MOST_THREADS = 2 ** 32 - 1  # of a launch, along an axis of its grid
-f32, i64, ptr = ctypes.c_float, ctypes.c_longlong, ctypes.c_void_p
+f32, f64, i64, ptr = ctypes.c_float, ctypes.c_double, ctypes.c_longlong, ctypes.c_void_p
 
 
 @pytest.fixture(scope="module")
@@ -59,3 +60,18 @@ def test_the_row_stride_of_a_single_token_means_nothing(lib, stride):
     assert plain[0] == ca.CLEAR_OK and gated_backward(lib, 1, (stride, stride, 64, 64, stride, 64, 64)) == plain
     assert gated(lib, 2, stride, 128)[0] != ca.CLEAR_OK and gated(lib, 2, 64, stride)[0] != ca.CLEAR_OK
     assert gated_backward(lib, 1, (128, 64, stride, 64, 64, 64, 64))[0] != ca.CLEAR_OK  # (a weight has rows)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [ca.CLEAR_BF16, ca.CLEAR_F32])
+def test_adamw_of_any_number_of_elements(lib, dtype, bits):
+    """Every element's workgroup once, in launches that the device can make; what has more elements than that is refused."""
+    chunk = 4096  # elements of a workgroup
+    for sizes in ([1], [2 ** 35], [2 ** 35, 2 ** 35], [2 ** 34 + 1, 2 ** 35 - 1, 7, 2 ** 35], [0, 5, 0], [2 ** 35 - 4096, 2 ** 34, 2 ** 34], list(range(1, 200)), [2 ** 34] * 70):
+        table = (cb.AdamWTensor * len(sizes))(*[cb.AdamWTensor(1 << 40, 1 << 41, None, 1 << 42, 1 << 43, 1 << 44, 1 << 45, n) for n in sizes])
+        rc = lib.clear_block_adamw(len(sizes), table, dtype, bits, f64(1e-3), f64(0.9), f64(0.99), f64(1e-8), f64(0), i64(1), None, None)
+        made = fake_launch.launches(lib)
+        assert rc == ca.CLEAR_OK and all(x.grid_x * x.block <= MOST_THREADS and x.grid_x > 0 for x in made)
+        assert sum(x.grid_x for x in made) == sum(-(-n // chunk) for n in sizes)
+    table = (cb.AdamWTensor * 1)(cb.AdamWTensor(1 << 40, 1 << 41, None, 1 << 42, 1 << 43, 1 << 44, 1 << 45, 2 ** 35 + 1))
+    assert lib.clear_block_adamw(1, table, dtype, bits, f64(1e-3), f64(0.9), f64(0.99), f64(1e-8), f64(0), i64(1), None, None) == ca.CLEAR_ERR_UNSUPPORTED
