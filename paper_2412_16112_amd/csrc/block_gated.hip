@@ -507,7 +507,8 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_tokens_kernel(const GatedA
 }
 
 // dG = dH u act'(g) and dU = dH act(g) in bf16 [tokens][2 hidden], gate first, 8 channels a thread.  Memory-bound: 4 608 x 6 528 84 us, 5 TB/s
-// (4 channels a thread, side by side, or 32-bit division: the same).
+// (4 channels a thread, side by side, or 32-bit division: the same).  The rounding to bf16 is what the matrix instructions take: it adds 0.0017 of their norm to the error of dX, dWg
+// and dWu, whose own rounding is as much, independently (0.0023 together); two terms each would take it out and double both products.
 __global__ void __launch_bounds__(256) gated_gradient_kernel(const GatedArgs g, long long n)
 {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
