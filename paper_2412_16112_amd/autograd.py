@@ -38,6 +38,12 @@ def clear_context_cache():
     _contexts.clear()
 
 
+def _no_gradients(*tensors):
+    """Whether a call on these tensors (None skipped) needs no backward pass.  To be asked outside the Function: inside its forward gradients are off, and needs_input_grad
+    says what the tensors want, whatever the caller's mode."""
+    return not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors))
+
+
 class ClearAttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(fctx, Q, K, V, n_text, gridH, gridW, r, mask_kind=ca.CLEAR_MASK_DISC, shift=0):
@@ -80,16 +86,12 @@ class ClearAttentionFunction(torch.autograd.Function):
 def clear_attention(Q, K, V, n_text, gridH, gridW, r, mask_kind=ca.CLEAR_MASK_DISC, shift=0):
     """softmax(Q K^T / sqrt(d) under the CLEAR mask) V for [B, H, n_text + gridH*gridW, d] device tensors.
     mask_kind / shift select one of the compared local masks instead of the disc (clear_attn_create_masked)."""
+    if _no_gradients(Q, K, V):
+        Q, K, V = Q.detach(), K.detach(), V.detach()
     return ClearAttentionFunction.apply(Q, K, V, n_text, gridH, gridW, r, mask_kind, shift)
 
 
 # ---- the operators around the attention (clear_block) -------------------------------------------------------------------------
-
-def _no_gradients(*tensors):
-    """Whether a call on these tensors (None skipped) needs no backward pass.  To be asked outside the Function: inside its forward gradients are off, and needs_input_grad
-    says what the tensors want, whatever the caller's mode."""
-    return not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors))
-
 
 def _channels_ok(t):
     """t (or None), or a contiguous copy where its channels are not."""

@@ -84,3 +84,27 @@ def test_nothing_is_kept_without_gradients(calls, quiet):
     assert calls[2:] == ["gated_ff", "layer_norm"]
     assert ag.gated_ff(X, *weights).requires_grad and ag.layer_norm(X, scale).requires_grad
     assert calls[4:] == ["gated_ff, products kept", "layer_norm, statistics kept"]
+
+
+def test_the_attention_without_gradients(monkeypatch):
+    """Under no_grad nothing is kept for a backward pass, and fp32 tensors, which have none, are not refused because they want gradients elsewhere."""
+    kept = []
+
+    class Context:
+        forward = staticmethod(lambda Q, K, V: Q * V)
+        forward_lse = staticmethod(lambda Q, K, V: kept.append("lse"))
+
+        @staticmethod
+        def forward_strided(Q, K, V, lse=None):
+            kept.append("nothing" if lse is None else "lse")
+            return Q * V
+    monkeypatch.setattr(ag, "_context", lambda *a: Context)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn(1, 1, 4, 64).to(dtype).requires_grad_()
+        with torch.no_grad():
+            assert not ag.clear_attention(x, x, x, 0, 2, 2, 1).requires_grad
+    assert kept == ["nothing"]
+    assert ag.clear_attention(x, x, x, 0, 2, 2, 1).requires_grad and kept == ["nothing", "lse"]
+    with pytest.raises(ag.ca.ClearAttnError):
+        ag.clear_attention(x.detach().float().requires_grad_(), x.float(), x.float(), 0, 2, 2, 1)
