@@ -148,6 +148,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0):
     x, weight, bias = _rows_ok(x), own(weight), own(bias)
     if _no_gradients(x, weight, bias):
         return cb.layer_norm(x, weight, bias, eps=eps, weight_offset=weight_offset)
+    if any(w is not None and w.dim() == 2 and w.shape[0] > 65535 for w in (weight, bias)):
+        raise ca.ClearAttnError(ca.CLEAR_ERR_UNSUPPORTED, "gradients: at most 65535 items with a weight each")
     return LayerNormFunction.apply(x, weight, bias, eps, weight_offset)
 
 

@@ -108,3 +108,18 @@ def test_the_attention_without_gradients(monkeypatch):
     assert ag.clear_attention(x, x, x, 0, 2, 2, 1).requires_grad and kept == ["nothing", "lse"]
     with pytest.raises(ag.ca.ClearAttnError):
         ag.clear_attention(x.detach().float().requires_grad_(), x.float(), x.float(), 0, 2, 2, 1)
+
+
+def test_weights_of_more_items_than_a_backward_pass_takes(calls):
+    """What the backward pass would refuse is refused forward, where gradients are wanted."""
+    many, scale = torch.zeros(65536, 1, 8), torch.ones(65536, 8)
+    with pytest.raises(ag.ca.ClearAttnError) as e:
+        ag.layer_norm(many.clone().requires_grad_(), scale)
+    assert e.value.status == ag.ca.CLEAR_ERR_UNSUPPORTED
+    with pytest.raises(ag.ca.ClearAttnError):
+        ag.layer_norm(many, None, scale.clone().requires_grad_())
+    assert calls == []
+    ag.layer_norm(many, scale)
+    ag.layer_norm(many.clone().requires_grad_(), scale[0])
+    ag.layer_norm(many[1:].clone().requires_grad_(), scale[1:])
+    assert len(calls) == 3
