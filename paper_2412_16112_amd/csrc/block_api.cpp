@@ -8,16 +8,14 @@
 #include <cstdint>
 #include <string>
 
+#include "block_checks.h"
 #include "block_internal.h"
 
 using namespace clear::block;
 
-namespace {
+static thread_local std::string g_error;
 
-thread_local std::string g_error;
-
-// Nothing leaves a C entry point as an exception: a message that cannot be stored is dropped.
-int fail(int code, const char* what, const char* why = "") noexcept
+int clear::block::fail(int code, const char* what, const char* why) noexcept
 {
     try {
         g_error.assign(what);
@@ -27,26 +25,8 @@ int fail(int code, const char* what, const char* why = "") noexcept
     }
     return code;
 }
-int invalid(const char* what) noexcept { return fail(CLEAR_ERR_INVALID_ARG, what); }
-int unsupported(const char* what) noexcept { return fail(CLEAR_ERR_UNSUPPORTED, what); }
-int launched(hipError_t e, const char* what) noexcept { return e == hipSuccess ? CLEAR_OK : fail(CLEAR_ERR_HIP, what, hipGetErrorString(e)); }
 
-bool known_dtype(int dtype) { return dtype == CLEAR_BF16 || dtype == CLEAR_F32; }
-int size_of(int dtype) { return dtype == CLEAR_BF16 ? 2 : 4; }
-bool aligned(const void* p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
-
-// Byte range [first, last) that a strided tensor spans.
-struct Span {
-    __int128 first, last;
-};
-Span span_of(const void* p, const long long* extent, const long long* stride, int axes, long long row, int size)
-{
-    __int128 last = row;
-    for (int i = 0; i < axes; ++i) last += (__int128)(extent[i] - 1) * stride[i];
-    return {(__int128)(uintptr_t)p, (__int128)(uintptr_t)p + last * size};
-}
-bool overlap(const Span& a, const Span& b) { return a.first < b.last && b.first < a.last; }
-bool too_long(const Span& a) { return a.last > ((__int128)1 << 62); }
+namespace {
 
 // Axes of one or two tensors by falling stride, without those on which nobody has a second entry.
 struct Axes {
@@ -215,21 +195,6 @@ int check_norm(long long groups, long long rows, int channels, const long long* 
         if (strides[i] > (1LL << 48)) return unsupported("strides must be <= 2^48");
     }
     return CLEAR_OK;
-}
-
-// An output may be `in` itself; else their ranges must be apart.  A row of an output is its own.
-bool out_apart(const void* out, const long long* out_strides, const void* in, const long long* in_strides, const long long* extent, int channels, int size, bool may_be_same)
-{
-    if (may_be_same && out == in && out_strides[0] == in_strides[0] && out_strides[1] == in_strides[1]) return true;
-    return !overlap(span_of(out, extent, out_strides, 2, channels, size), span_of(in, extent, in_strides, 2, channels, size));
-}
-bool rows_apart(const long long* strides, const long long* extent, int channels)
-{
-    if (extent[1] > 1 && strides[1] < channels) return false;
-    if (extent[0] <= 1) return true;
-    // groups one after the other, or interleaved with the rows (a transposed view)
-    const __int128 rows = (__int128)(extent[1] - 1) * strides[1] + channels;
-    return strides[0] >= rows || (strides[0] >= channels && (extent[1] == 1 || strides[1] >= (__int128)(extent[0] - 1) * strides[0] + channels));
 }
 
 }  // namespace
