@@ -143,6 +143,88 @@ int clear_block_adamw(int n_tensors, const clear_block_adamw_tensor* tensors, in
 int clear_block_adamw_decode(const void* m, const float* m_scale, const void* v, const float* v_scale, float* m_out, float* v_out,
                              long long n, void* stream);
 
+/* ---- Gated residual with its norms ---------------------------------------------------------------------------------------
+ *
+ * What lies between two sublayers of a block.  X the residual stream, Y a sublayer's output, [groups, rows, channels] both:
+ *     z = post(y) * (post_offset + post_weight)      (post CLEAR_NORM_NONE: z = y)
+ *     r = residual_scale * x + gate * z,   h = norm(r) * (weight_offset + weight) + bias
+ * where norm and post take each row's size off, CLEAR_NORM_LAYER (v - mean) / sqrt(var + eps), CLEAR_NORM_RMS v / sqrt(mean(v^2) + eps): R is the stream from here on, H what
+ * the next sublayer is given.  r goes into its norm before it is rounded to R's type.
+ * gate: NULL (1), [channels] or, with gate_per_group != 0, [groups, channels]; weight and bias: each NULL (weight: 1), [channels] or, with per_group != 0, [groups, channels];
+ * post_weight: NULL (1) or [channels]; all contiguous, of weight_dtype.  dtype: of Y and H; stream_dtype: of X and R: CLEAR_BF16 or CLEAR_F32, not fp32 beside a
+ * stream in bf16.  stats: NULL, or fp32 [2, groups, rows], with a post norm [4, groups, rows], which receives mean (0 for CLEAR_NORM_RMS) and 1 / size of r, then of y, for the
+ * backward pass.  strides: (group, row) of X, Y, R, H, 8 values, in elements; R may be X itself and H may be Y itself (same strides), else no output overlaps anything.
+ * 1 <= channels <= 8192; groups * rows < 2^31; eps >= 0. */
+typedef enum {
+    CLEAR_NORM_NONE = 0,
+    CLEAR_NORM_LAYER = 1,
+    CLEAR_NORM_RMS = 2
+} clear_norm_kind;
+int clear_block_residual_norm(const void* X, const void* Y, const void* gate, const void* weight, const void* bias, const void* post_weight, void* R, void* H, float* stats,
+                              long long groups, long long rows, int channels, const long long* strides, int gate_per_group, int per_group, int kind, int post, float eps,
+                              float residual_scale, float weight_offset, float post_offset, int dtype, int stream_dtype, int weight_dtype, void* stream);
+
+/* Backward pass.  dR (NULL: 0) and dH the gradients of R and H, typed like these; X, Y, the vectors and stats as the forward pass had and gave them; writes (each may be NULL, but not
+ * all where there are rows), with rhat = norm(r), yhat = post(y), dn the gradient of r through its norm,
+ *     dr + dn = d,   dX = residual_scale * d,   dY = the gradient of y through its norm from gate * d * (post_offset + post_weight)   (gate * d without a post norm),
+ *     d_gate = sum d * z,   d_weight = sum dh * rhat,   d_bias = sum dh,   d_post_weight = sum gate * d * yhat
+ * the sums over the rows (of a group where the vector is a group's own, else of all groups; 0 for no rows), laid out and typed like the vectors.  strides: (group, row) of dR, dH, X, Y,
+ * dX, dY, 12 values; dX may be dR itself and dY may be dH itself (same strides).  workspace: fp32, clear_block_residual_norm_workspace floats, needed for the
+ * vectors' gradients.  At most 65535 groups where a vector is a group's own. */
+int clear_block_residual_norm_backward(const void* dR, const void* dH, const void* X, const void* Y, const void* gate, const void* weight, const void* post_weight, const float* stats,
+                                       void* dX, void* dY, void* d_gate, void* d_weight, void* d_bias, void* d_post_weight, long long groups, long long rows, int channels,
+                                       const long long* strides, int gate_per_group, int per_group, int kind, int post, float residual_scale, float weight_offset,
+                                       float post_offset, int dtype, int stream_dtype, int weight_dtype, float* workspace, void* stream);
+/* Floats of that workspace (host only); -1 for sizes that the calls refuse. */
+long long clear_block_residual_norm_workspace(long long groups, long long rows, int channels, int gate_per_group, int per_group);
+
+/* ---- Norm of gradients, clipping -----------------------------------------------------------------------------------------
+ *
+ * Over n_tensors tensors together, of any types and sizes (data NULL or n = 0: not there):
+ *     norm = |u| sqrt(sum g^2)  (CLEAR_GRAD_NORM_2)  or  |u| max |g|  (CLEAR_GRAD_NORM_MAX),   factor = u * min(1, max_norm / norm)
+ * with u = *unscale, a device fp32 scalar (NULL: 1; the inverse of a loss's scale), to the device fp32 scalars norm and factor (either may be NULL; max_norm >= 0 counts for factor alone).
+ * The factor is what clear_block_adamw takes as grad_scale, and clear_block_grad_scale.  Squares and sums are fp64: no gradient is too large or too small to be squared.  A NaN among the
+ * gradients makes norm and factor NaN; an infinity makes norm infinite and factor 0.  workspace: clear_block_grad_norm_workspace bytes, 8-byte aligned.
+ * `tensors` is a HOST array, read before the call returns; a captured graph repeats its tensors.  n <= 2^35. */
+typedef enum {
+    CLEAR_GRAD_NORM_2 = 0,
+    CLEAR_GRAD_NORM_MAX = 1
+} clear_grad_norm_kind;
+typedef struct {
+    void* data;
+    long long n;
+    int dtype;
+} clear_block_grad;
+int clear_block_grad_norm(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, const float* unscale, float* norm, float* factor, void* workspace,
+                          void* stream);
+/* Bytes of that workspace (host only); -1 for tensors that the calls refuse. */
+long long clear_block_grad_norm_workspace(int n_tensors, const clear_block_grad* tensors);
+/* Every element of every tensor times *factor, in fp32, rounded once, in place.  A factor of 1 leaves everything as it is and reads nothing.  No two tensors may share memory. */
+int clear_block_grad_scale(int n_tensors, const clear_block_grad* tensors, const float* factor, void* stream);
+
+/* ---- Operands in 4 bits -----------------------------------------------------------------------------------------------------
+ *
+ * A matrix [rows, channels] (channels a multiple of 32) as codes of 4 bits with a scale for every 32 channels of a row (the microscaled format e2m1 with scales e8m0):
+ *     codes  [rows][channels / 2] bytes: channel 2i in the low, 2i + 1 in the high half of byte i; a code is a sign (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 .. 7);
+ *     scales [ceil(channels / 256)][rows][8] bytes: block b of a row (channels 32 b .. 32 b + 31) has byte [b / 8][row][b % 8], which stands for 2^(byte - 127), 255 for NaN
+ * ld_codes bytes from one row of codes to the next, ld_scales bytes from one group of scales to the next, so that a range of rows of a matrix is one too.  Codes 16-byte aligned, ld_codes a
+ * multiple of 16 and <= 2^20; scales 8-byte aligned, ld_scales a multiple of 8.  Strides of a single row, or of a single group, are not looked at, nor are bytes behind a row's last scale (written as 0).
+ *
+ * Quantise: a block's scale is 2^e, e = max(floor(log2 of its largest magnitude) - 2, -127); a code is the nearest to x / 2^e, halfway the one of even number, 6 for what is over 6.  A
+ * block that holds a NaN or an infinity becomes NaN (scale 255, codes 0).  X of dtype (CLEAR_BF16 or CLEAR_F32), rows of ld_x elements.  Dequantise: the values that the codes stand
+ * for, rounded to dtype (exact but for bf16's and fp32's smallest numbers). */
+int clear_block_mx_quantize(const void* X, void* codes, void* scales, long long rows, int channels, long long ld_x, long long ld_codes, long long ld_scales, int dtype, void* stream);
+int clear_block_mx_dequantize(const void* codes, const void* scales, void* Y, long long rows, int channels, long long ld_codes, long long ld_scales, long long ld_y, int dtype,
+                              void* stream);
+/* Y = X W^T + bias for W [outputs, channels] in 4 bits and X [tokens, channels] in 4 bits (X_scales non-NULL: X are its codes) or of x_dtype, which the call takes to 4 bits first, as clear_block_mx_quantize
+ * does.  fp32 accumulation, one rounding on output.  bias: NULL or [outputs] of bias_dtype; Y of out_dtype, any outputs, rows of any stride >= outputs.  strides, 5 values: of X (elements, or bytes of codes),
+ * X_scales, W codes, W_scales (bytes), Y (elements).  workspace: clear_block_mx_linear_workspace bytes, 16-byte aligned.  channels, outputs <= 2^20; tokens < 2^31.  A few tokens
+ * take a form that streams the weights once. */
+int clear_block_mx_linear(const void* X, const void* X_scales, const void* W, const void* W_scales, const void* bias, void* Y, long long tokens, int channels, int outputs,
+                          const long long* strides, int x_dtype, int bias_dtype, int out_dtype, void* workspace, void* stream);
+/* Bytes of that workspace (host only), quantized: X comes in 4 bits; -1 for sizes that the call refuses. */
+long long clear_block_mx_linear_workspace(long long tokens, int channels, int outputs, int quantized);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,11 +1,14 @@
 """Thin ctypes binding of the operators around the attention (include/clear_block.h, same library as clear_attn): rotary
-positions, layer norm, gated feed-forward projection, AdamW step.  Argument marshalling only: PyTorch tensors are used for
+positions, layer norm, gated residual with its norms, gated feed-forward projection, products of operands in 4 bits, AdamW
+step, norm and clipping of gradients.  Argument marshalling only: PyTorch tensors are used for
 device memory, workspaces and streams; every step runs in the HIP kernels, and there is no fallback.
 
 Refusals raise ClearAttnError, as in clear_attn.  Each call enqueues on `stream` (default: torch's current stream of the tensors' device); with another
 one the caller orders it with torch's, before the call (results are allocated for torch's stream) and after it.  These calls are not differentiable (autograd.py has
 the forms that are); the tensors that a caller gives them to write into - outputs, parameters, masters - count as changed for autograd afterwards."""
+import collections
 import ctypes
+import math
 import operator
 
 import numpy as np
@@ -18,12 +21,18 @@ CLEAR_ROPE_PLAIN, CLEAR_ROPE_LINEAR, CLEAR_ROPE_BASE, CLEAR_ROPE_PARTS = range(4
 CLEAR_ACT_SILU, CLEAR_ACT_GELU_TANH, CLEAR_ACT_GELU_ERF = range(3)
 ACTIVATIONS = {"silu": CLEAR_ACT_SILU, "gelu_tanh": CLEAR_ACT_GELU_TANH, "gelu_erf": CLEAR_ACT_GELU_ERF}
 SCALINGS = {"plain": CLEAR_ROPE_PLAIN, "linear": CLEAR_ROPE_LINEAR, "base": CLEAR_ROPE_BASE, "parts": CLEAR_ROPE_PARTS}
+CLEAR_NORM_NONE, CLEAR_NORM_LAYER, CLEAR_NORM_RMS = range(3)
+NORMS = {None: CLEAR_NORM_NONE, "layer": CLEAR_NORM_LAYER, "rms": CLEAR_NORM_RMS}
+CLEAR_GRAD_NORM_2, CLEAR_GRAD_NORM_MAX = range(2)
+MX_BLOCK, MX_GROUP = 32, 256  # channels that share a scale where a matrix is in 4 bits, and channels of a group of scales
 STATE_BLOCK = 256  # elements that share a scale where AdamW's states have 8 bits
 
 EXPORTS = [
     "clear_block_last_error", "clear_block_rotary", "clear_block_rotary_frequencies", "clear_block_layer_norm",
     "clear_block_layer_norm_backward", "clear_block_layer_norm_workspace", "clear_block_gated_ff", "clear_block_gated_ff_backward",
-    "clear_block_gated_ff_workspace", "clear_block_adamw", "clear_block_adamw_decode",
+    "clear_block_gated_ff_workspace", "clear_block_adamw", "clear_block_adamw_decode", "clear_block_residual_norm",
+    "clear_block_residual_norm_backward", "clear_block_residual_norm_workspace", "clear_block_grad_norm", "clear_block_grad_norm_workspace",
+    "clear_block_grad_scale", "clear_block_mx_quantize", "clear_block_mx_dequantize", "clear_block_mx_linear", "clear_block_mx_linear_workspace",
 ]
 
 
@@ -32,7 +41,11 @@ class AdamWTensor(ctypes.Structure):
                 ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n", ctypes.c_longlong)]
 
 
-_Strides3, _Strides4, _Strides6, _Strides7, _Strides12 = (ctypes.c_longlong * n for n in (3, 4, 6, 7, 12))
+class Grad(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_longlong), ("dtype", ctypes.c_int)]
+
+
+_Strides3, _Strides4, _Strides5, _Strides6, _Strides7, _Strides8, _Strides12 = (ctypes.c_longlong * n for n in (3, 4, 5, 6, 7, 8, 12))
 _lib = None
 
 
@@ -53,11 +66,22 @@ def lib():
         L.clear_block_gated_ff_workspace.argtypes = [ll, i, i]
         L.clear_block_adamw.argtypes = [i, vp, i, i, d, d, d, d, d, ll, vp, vp]
         L.clear_block_adamw_decode.argtypes = [vp, vp, vp, vp, vp, vp, ll, vp]
+        L.clear_block_residual_norm.argtypes = [vp] * 9 + [ll, ll, i, vp, i, i, i, i, f, f, f, f, i, i, i, vp]
+        L.clear_block_residual_norm_backward.argtypes = [vp] * 14 + [ll, ll, i, vp, i, i, i, i, f, f, f, i, i, i, vp, vp]
+        L.clear_block_residual_norm_workspace.argtypes = [ll, ll, i, i, i]
+        L.clear_block_grad_norm.argtypes = [i, vp, i, d, vp, vp, vp, vp, vp]
+        L.clear_block_grad_norm_workspace.argtypes = [i, vp]
+        L.clear_block_grad_scale.argtypes = [i, vp, vp, vp]
+        L.clear_block_mx_quantize.argtypes = [vp, vp, vp, ll, i, ll, ll, ll, i, vp]
+        L.clear_block_mx_dequantize.argtypes = [vp, vp, vp, ll, i, ll, ll, ll, i, vp]
+        L.clear_block_mx_linear.argtypes = [vp, vp, vp, vp, vp, vp, ll, i, i, vp, i, i, i, vp, vp]
+        L.clear_block_mx_linear_workspace.argtypes = [ll, i, i, i]
         for name in EXPORTS:
             getattr(L, name).restype = i
         L.clear_block_last_error.restype = ctypes.c_char_p
-        L.clear_block_layer_norm_workspace.restype = ll
-        L.clear_block_gated_ff_workspace.restype = ll
+        for name in EXPORTS:
+            if name.endswith("_workspace"):
+                getattr(L, name).restype = ll
         _lib = L
     return _lib
 
@@ -266,6 +290,96 @@ def _record(t, stream):
         t.record_stream(torch.cuda.ExternalStream(stream, device=t.device))
 
 
+# ---- gated residual with its norms -----------------------------------------------------------------------------------------
+
+def _norm_kinds(kind, post):
+    if kind not in NORMS or kind is None:
+        _refuse("kind must be 'layer' or 'rms'")
+    if post not in NORMS:
+        _refuse("post must be None, 'layer' or 'rms'")
+    return NORMS[kind], NORMS[post]
+
+
+def _residual_vectors(x, gate, weight, bias, post_weight, post):
+    """(gate_per_group, per_group, weight dtype code): gate, weight and bias are [C], or [B, C] for x [B, N, C]; post_weight is [C]."""
+    per_group, code = _norm_weights(x, weight, bias)
+    gate_per_group, _ = _norm_weights(x, gate, None)
+    if post_weight is not None:
+        if post is None:
+            _refuse("post_weight without a post norm")
+        if post_weight.dim() != 1:
+            _refuse("post_weight must be [C]")
+        _norm_weights(x, post_weight, None)
+    given = [v for v in (gate, weight, bias, post_weight) if v is not None]
+    if any(v.dtype != given[0].dtype for v in given):
+        _refuse("gate, weight, bias and post_weight must have one dtype", CLEAR_ERR_MISMATCH)
+    return gate_per_group, per_group, ca._dtype_code(given[0]) if given else CLEAR_F32
+
+
+def _residual_tensors(x, y):
+    if y.shape != x.shape:
+        _refuse("x and y must have one shape", CLEAR_ERR_MISMATCH)
+    return ca._dtype_code(y), ca._dtype_code(x)
+
+
+def residual_norm(x, y, gate=None, weight=None, bias=None, post_weight=None, kind="layer", post=None, eps=1e-6, residual_scale=1.0, weight_offset=0.0, post_offset=0.0,
+                  out=None, save_stats=False, stream=None):
+    """clear_block_residual_norm: what lies between two sublayers, x the residual stream and y a sublayer's output:
+        r = residual_scale * x + gate * post(y) * (post_offset + post_weight),   h = norm(r) * (weight_offset + weight) + bias
+
+    kind: the norm of r, post: the norm of y, "layer" or "rms" (post None: none).  gate, weight, bias: [C], or [B, C] for x [B, N, C], post_weight [C], of one dtype; each may be
+    None.  x (and r) and y (and h): bf16 or fp32, rows at any stride, not x in bf16 beside y in fp32.  out: (r, h) to write to; r may be x and h may be y.  Returns (r, h), or (r, h, stats)
+    with save_stats (for residual_norm_backward)."""
+    kind_code, post_code = _norm_kinds(kind, post)
+    dtype, stream_dtype = _residual_tensors(x, y)
+    groups, rows, C = _rows(x)
+    gate_per_group, per_group, wcode = _residual_vectors(x, gate, weight, bias, post_weight, post)
+    r, h = (_new_like(x), _new_like(y)) if out is None else out
+    _on_device(x, y, gate, weight, bias, post_weight, r, h)
+    if r.shape != x.shape or r.dtype != x.dtype or h.shape != y.shape or h.dtype != y.dtype:
+        _refuse("out must have the shapes and dtypes of x and y", CLEAR_ERR_MISMATCH)
+    stats = torch.empty((4 if post_code else 2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if save_stats else None
+    strides = _Strides8(*_row_strides(x, "x"), *_row_strides(y, "y"), *_row_strides(r, "r"), *_row_strides(h, "h"))
+    _call("clear_block_residual_norm", x.device, stream, x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(weight), _ptr(bias), _ptr(post_weight), r.data_ptr(), h.data_ptr(), _ptr(stats),
+          groups, rows, C, strides, gate_per_group, per_group, kind_code, post_code, eps, residual_scale, weight_offset, post_offset, dtype, stream_dtype, wcode)
+    if out is not None:
+        _changed(list(out))
+    return (r, h, stats) if save_stats else (r, h)
+
+
+def residual_norm_backward(dr, dh, x, y, gate, weight, bias, post_weight, stats, kind="layer", post=None, residual_scale=1.0, weight_offset=0.0, post_offset=0.0,
+                           need=(True,) * 6, stream=None):
+    """clear_block_residual_norm_backward: (dx, dy, d_gate, d_weight, d_bias, d_post_weight) for what residual_norm(..., save_stats=True) was called with; None for a vector that is
+    None and where `need` says so.  dr: the gradient of r, or None where nothing came back through it."""
+    kind_code, post_code = _norm_kinds(kind, post)
+    dtype, stream_dtype = _residual_tensors(x, y)
+    groups, rows, C = _rows(x)
+    gate_per_group, per_group, wcode = _residual_vectors(x, gate, weight, bias, post_weight, post)
+    _on_device(x, y, dr, dh, gate, weight, bias, post_weight, stats)
+    if dh.shape != y.shape or dh.dtype != y.dtype or (dr is not None and (dr.shape != x.shape or dr.dtype != x.dtype)):
+        _refuse("dr and dh must have the shapes and dtypes of x and y", CLEAR_ERR_MISMATCH)
+    if stats.dtype != torch.float32 or not stats.is_contiguous() or tuple(stats.shape) != (4 if post_code else 2,) + tuple(x.shape[:-1]):
+        _refuse("stats must be what residual_norm(..., save_stats=True) gave for x and y")
+    grads = [_new_like(v) if v is not None and n else None for v, n in zip((x, y, gate, weight, bias, post_weight), need)]
+    if all(g is None for g in grads):
+        return tuple(grads)
+    ws = None
+    if any(g is not None for g in grads[2:]):
+        floats = lib().clear_block_residual_norm_workspace(groups, rows, C, gate_per_group, per_group)
+        if floats < 0:
+            _check(CLEAR_ERR_UNSUPPORTED)
+        ws = torch.empty(max(1, floats), dtype=torch.float32, device=x.device)
+    strides = []
+    for t, name in ((dr, "dr"), (dh, "dh"), (x, "x"), (y, "y"), (grads[0], "dx"), (grads[1], "dy")):
+        strides += _row_strides(t, name) if t is not None else (0, 0)
+    s = _call("clear_block_residual_norm_backward", x.device, stream, _ptr(dr), dh.data_ptr(), x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(weight), _ptr(post_weight),
+              stats.data_ptr(), *map(_ptr, grads), groups, rows, C, _Strides12(*strides), gate_per_group, per_group, kind_code, post_code, residual_scale, weight_offset,
+              post_offset, dtype, stream_dtype, wcode, _ptr(ws))
+    if ws is not None and stream is not None:
+        _record(ws, s)
+    return tuple(grads)
+
+
 # ---- gated feed-forward projection ----------------------------------------------------------------------------------------
 
 def _matrix(t, name, width):
@@ -461,3 +575,209 @@ def adamw_decode(m, m_scale, v, v_scale, stream=None):
     out = [torch.empty(m.shape, dtype=torch.float32, device=m.device) for _ in range(2)]
     _call("clear_block_adamw_decode", m.device, stream, m.data_ptr(), m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), n)
     return out[0], out[1]
+
+
+# ---- norm and clipping of gradients ---------------------------------------------------------------------------------------------
+
+def _grad_table(grads):
+    """Descriptors (rows of clear_block_grad's three words) of the gradients that are there, with the device they are on."""
+    have = [g for g in grads if g is not None]
+    if not have:
+        _refuse("there must be a gradient")
+    device = have[0].device
+    if not have[0].is_cuda:
+        _refuse("tensors must be device tensors")
+    if set(map(_device_of, have)) != {device.index}:
+        _refuse("gradients must be on one device")
+    if not all(map(_contiguous, have)):
+        _refuse("gradients must be contiguous")
+    dtypes = set(map(_dtype_of, have))
+    codes = {t: ca._dtype_code(next(g for g in have if g.dtype == t)) for t in dtypes}
+    table = np.zeros((len(have), 3), dtype=np.int64)
+    table[:, 0] = list(map(_ptr_of, have))
+    table[:, 1] = list(map(_numel, have))
+    table[:, 2] = next(iter(codes.values())) if len(codes) == 1 else [codes[g.dtype] for g in have]
+    return table, have, device
+
+
+def _grad_kind(norm_type):
+    if norm_type not in (2, math.inf):
+        _refuse("norm_type must be 2 or infinity", CLEAR_ERR_UNSUPPORTED)
+    return CLEAR_GRAD_NORM_2 if norm_type == 2 else CLEAR_GRAD_NORM_MAX
+
+
+def _launch_norm(table, device, kind, max_norm, grad_scale, stream):
+    """(norm, factor), both fp32 scalars on the device; factor None without a max_norm."""
+    L = _lib or lib()
+    size = L.clear_block_grad_norm_workspace(len(table), table.ctypes.data)
+    if size < 0:
+        _check(CLEAR_ERR_UNSUPPORTED)
+    out = torch.empty(2, dtype=torch.float32, device=device)
+    ws = torch.empty(max(1, size // 8), dtype=torch.float64, device=device)
+    norm, factor = out.unbind(0)
+    s = _call("clear_block_grad_norm", device, stream, len(table), table.ctypes.data, kind, 0.0 if max_norm is None else max_norm, _ptr(grad_scale), norm.data_ptr(),
+              None if max_norm is None else factor.data_ptr(), ws.data_ptr())
+    if stream is not None:
+        _record(ws, s)
+    return norm, None if max_norm is None else factor
+
+
+def grad_norm(grads, norm_type=2.0, max_norm=None, grad_scale=None, stream=None):
+    """clear_block_grad_norm: the norm of all gradients together (a list of contiguous bf16 and fp32 tensors; None is skipped), as an fp32 scalar on their device: nothing waits for
+    it.  norm_type: 2 or math.inf.  grad_scale: an fp32 device scalar that the gradients are multiplied by (the inverse of a loss's scale).  With max_norm: (norm, factor), the factor
+    grad_scale * min(1, max_norm / norm) being what adamw_step takes as its grad_scale."""
+    kind = _grad_kind(norm_type)
+    table, _, device = _grad_table(grads)
+    _check_scale(grad_scale, device)
+    norm, factor = _launch_norm(table, device, kind, max_norm, grad_scale, stream)
+    return norm if max_norm is None else (norm, factor)
+
+
+def _refuse_shared(table):
+    size = np.where(table[:, 2] == CLEAR_F32, 4, 2) * table[:, 1]
+    at = table[size > 0, 0]
+    order = np.argsort(at)
+    ends = at[order] + size[size > 0][order]
+    if np.any(ends[:-1] > at[order][1:]):
+        _refuse("gradients share memory")
+
+
+def clip_grads(grads, max_norm, norm_type=2.0, grad_scale=None, stream=None):
+    """Scales all gradients in place by grad_scale * min(1, max_norm / norm) and returns their norm, that of grad_scale times them (an fp32 scalar on their device): grad_norm, then clear_block_grad_scale."""
+    kind = _grad_kind(norm_type)
+    table, have, device = _grad_table(grads)
+    _refuse_shared(table)
+    _check_scale(grad_scale, device)
+    norm, factor = _launch_norm(table, device, kind, max_norm, grad_scale, stream)
+    _call("clear_block_grad_scale", device, stream, len(table), table.ctypes.data, factor.data_ptr())
+    _changed(have)
+    return norm
+
+
+def scale_grads(grads, factor, stream=None):
+    """clear_block_grad_scale: every gradient times an fp32 device scalar, in place."""
+    table, have, device = _grad_table(grads)
+    _refuse_shared(table)
+    if factor is None:
+        _refuse("a factor is needed")
+    _check_scale(factor, device)
+    _call("clear_block_grad_scale", device, stream, len(table), table.ctypes.data, factor.data_ptr())
+    _changed(have)
+
+
+# ---- operands in 4 bits -----------------------------------------------------------------------------------------------------------
+
+class MX4(collections.namedtuple("MX4", "codes scales")):
+    """A matrix [..., C] in 4 bits: codes uint8 [..., C / 2], channel 2i in the low half of byte i, and scales uint8 [ceil(C / 256), rows, 8], byte [k, row, j] of channels 256 k + 32 j to + 31, standing for
+    2^(byte - 127).  rows() is a range of rows, without copying."""
+    __slots__ = ()
+
+    def rows(self, first, last):
+        return MX4(self.codes[first:last], self.scales[:, first:last])
+
+
+def _mx_sizes(rows, C):
+    if C % MX_BLOCK or C == 0:
+        _refuse("channels must be a multiple of %d" % MX_BLOCK, CLEAR_ERR_UNSUPPORTED)
+    return -(-C // MX_GROUP)
+
+
+def _mx_operand(t, name):
+    """(rows, channels, bytes from row to row of codes, bytes from group to group of scales)."""
+    if not isinstance(t, tuple) or len(t) != 2:
+        _refuse("%s must be an MX4" % name)
+    codes, scales = t
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() < 1:
+        _refuse("%s: codes and scales must be uint8" % name)
+    C = 2 * codes.shape[-1]
+    if codes.dim() == 2 and (codes.shape[0] <= 1 or codes.stride(1) == 1):
+        rows, ld = codes.shape[0], codes.stride(0)
+        if rows == 1 and C > 2 and codes.stride(1) != 1:
+            _refuse("%s: the last axis of codes must be contiguous" % name)
+    elif codes.is_contiguous():
+        rows, ld = codes.numel() // max(1, C // 2), C // 2
+    else:
+        _refuse("%s: the last axis of codes must be contiguous, and more than two axes altogether" % name)
+    groups = _mx_sizes(rows, C)
+    if tuple(scales.shape) != (groups, rows, 8):
+        _refuse("%s: scales must be [%d, %d, 8]" % (name, groups, rows), CLEAR_ERR_MISMATCH)
+    if rows > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 8)):
+        _refuse("%s: scales must be contiguous within a group" % name)
+    return rows, C, ld, scales.stride(0)
+
+
+def _any_rows(t, name):
+    """(rows, row stride) of a tensor [..., C] whose leading axes are one axis of evenly spaced rows."""
+    if t.dim() < 1:
+        _refuse("%s: a tensor of at least one axis is needed" % name)
+    if t.dim() != 2:
+        if not t.is_contiguous():
+            _refuse("%s: a tensor of %d axes must be contiguous" % (name, t.dim()))
+        t = t.reshape(-1, t.shape[-1])
+    if t.shape[0] == 0:
+        return 0, t.shape[1]
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse("%s: the last axis must be contiguous" % name)
+    return t.shape[0], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def mx_quantize(x, stream=None):
+    """clear_block_mx_quantize: x [..., C] (bf16 or fp32, C a multiple of 32) to 4 bits with a scale for every 32 channels of a row: an MX4."""
+    dtype = ca._dtype_code(x)
+    _on_device(x)
+    rows, ld = _any_rows(x, "x")
+    C = x.shape[-1]
+    groups = _mx_sizes(rows, C)
+    codes = torch.empty(x.shape[:-1] + (C // 2,), dtype=torch.uint8, device=x.device)
+    scales = torch.empty((groups, rows, 8), dtype=torch.uint8, device=x.device)
+    _call("clear_block_mx_quantize", x.device, stream, x.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, C, ld, C // 2, 8 * rows, dtype)
+    return MX4(codes, scales)
+
+
+def mx_dequantize(t, dtype=torch.bfloat16, stream=None):
+    """clear_block_mx_dequantize: the numbers that an MX4 stands for, in bf16 or fp32."""
+    rows, C, ld, ld_scales = _mx_operand(t, "t")
+    _on_device(*t)
+    y = torch.empty(t[0].shape[:-1] + (C,), dtype=dtype, device=t[0].device)
+    _call("clear_block_mx_dequantize", y.device, stream, t[0].data_ptr(), t[1].data_ptr(), y.data_ptr(), rows, C, ld, ld_scales, C, ca._dtype_code(y))
+    return y
+
+
+def mx_linear(x, w, bias=None, dtype=None, out=None, stream=None):
+    """clear_block_mx_linear: x w^T + bias for w [F, C] in 4 bits (an MX4) and x [..., C]: an MX4, or bf16 or fp32, which the call takes to 4 bits first.  bias: [F], bf16 or fp32, or None.
+    Returns [..., F] of `dtype` (bf16 by default), or out."""
+    F, C, ld_w, ld_ws = _mx_operand(w, "w")
+    if w[0].dim() != 2 or F < 1:
+        _refuse("w must be [F, C], F >= 1")
+    quantized = isinstance(x, tuple)
+    if quantized:
+        M, Cx, ld_x, ld_xs = _mx_operand(x, "x")
+        lead, x_code, xp, xsp = x[0].shape[:-1], 0, x[0].data_ptr(), x[1].data_ptr()
+    else:
+        M, ld_x = _any_rows(x, "x")
+        Cx, ld_xs, lead, x_code, xp, xsp = x.shape[-1], 0, x.shape[:-1], ca._dtype_code(x), x.data_ptr(), None
+    if Cx != C:
+        _refuse("x must be [..., %d]" % C, CLEAR_ERR_MISMATCH)
+    if bias is not None and (tuple(bias.shape) != (F,) or not bias.is_contiguous()):
+        _refuse("bias must be contiguous, [%d]" % F, CLEAR_ERR_MISMATCH)
+    device = w[0].device
+    if out is None:
+        y = torch.empty(tuple(lead) + (F,), dtype=torch.bfloat16 if dtype is None else dtype, device=device)
+    else:
+        y = out
+        if tuple(y.shape) != tuple(lead) + (F,) or (dtype is not None and y.dtype != dtype):
+            _refuse("out must be %s, of the dtype asked for" % (list(lead) + [F],), CLEAR_ERR_MISMATCH)
+    _on_device(w[0], w[1], bias, y, *(x if quantized else (x,)))
+    _, ld_y = _any_rows(y, "out")
+    out_code = ca._dtype_code(y)
+    size = (_lib or lib()).clear_block_mx_linear_workspace(M, C, F, int(quantized))
+    if size < 0:
+        _check(CLEAR_ERR_UNSUPPORTED)
+    ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    s = _call("clear_block_mx_linear", device, stream, xp, xsp, w[0].data_ptr(), w[1].data_ptr(), _ptr(bias), y.data_ptr(), M, C, F, _Strides5(ld_x, ld_xs, ld_w, ld_ws, ld_y),
+              x_code, 0 if bias is None else ca._dtype_code(bias), out_code, _ptr(ws))
+    if ws is not None and stream is not None:
+        _record(ws, s)
+    if out is not None:
+        _changed(out)
+    return y

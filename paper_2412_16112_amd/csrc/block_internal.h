@@ -66,6 +66,53 @@ hipError_t launch_adamw(int n, const clear_block_adamw_tensor* tensors, const Ad
 hipError_t launch_adamw_decode(const void* m, const float* ms, const void* v, const float* vs, float* m_out, float* v_out, long long n,
                                hipStream_t stream);
 
+// ---- gated residual with its norms
+constexpr int kResidualMaxChannels = 8192;
+struct ResidualArgs {
+    const void *x, *y, *gate, *w, *b, *pw, *dr, *dh;
+    void *r, *h, *dx, *dy, *dgate, *dw, *db, *dpw;
+    float *stats, *ws;
+    int groups, rows, channels;
+    long long st[12];  // forward: (group, row) of x, y, r, h; backward: of dr, dh, x, y, dx, dy
+    int per_group, gate_per_group, kind, post;
+    float eps, offset, post_offset, scale;
+    int rows_out, sums;  // (backward, set by the launcher: whether more than weight's and bias's gradients are wanted; how many sums are)
+};
+hipError_t launch_residual_forward(const ResidualArgs& a, int dtype, int stream_dtype, int weight_dtype, hipStream_t stream);
+hipError_t launch_residual_backward(const ResidualArgs& a, int dtype, int stream_dtype, int weight_dtype, hipStream_t stream);
+int residual_partials(long long groups, long long rows, int channels, long long sets);  // workgroups whose sums a set is joined from
+
+// ---- norm of gradients
+struct GradFactor {
+    int kind;  // CLEAR_GRAD_NORM_2 or CLEAR_GRAD_NORM_MAX
+    double max_norm;
+    const float* unscale;
+    float *norm, *factor;
+};
+hipError_t launch_grad_norm(int n, const clear_block_grad* tensors, const GradFactor& f, void* workspace, hipStream_t stream);
+hipError_t launch_grad_scale(int n, const clear_block_grad* tensors, const float* factor, hipStream_t stream);
+long long grad_norm_partials(int n, const clear_block_grad* tensors);
+
+// ---- operands in 4 bits
+struct MxArgs {
+    const void *x, *codes, *scales;
+    void *y, *codes_out, *scales_out;
+    long long rows, ld_x, ld_codes, ld_scales, ld_y;
+    int channels;
+};
+hipError_t launch_mx_quantize(const MxArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_mx_dequantize(const MxArgs& a, int dtype, hipStream_t stream);
+struct MxLinearArgs {
+    const void *x, *xs, *w, *ws, *bias;
+    void* y;
+    long long tokens, ld_x, ld_xs, ld_w, ld_ws, ld_y;
+    int channels, outputs;
+    int x_dtype, bias_dtype, out_dtype;  // (x_dtype where xs is null)
+    void* workspace;
+};
+hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream);
+size_t mx_linear_workspace_bytes(long long tokens, int channels, int outputs, bool quantized);
+
 // ---- device types.  Callers' tensors need the alignment of their elements only: global memory takes a wide access at any
 // address, and the types say so to the compiler.
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;

@@ -1,0 +1,646 @@
+// Operands in 4 bits: rows of numbers to codes of 4 bits with a scale for every 32 channels, back, and the product of two such matrices on the scaled matrix instructions.
+//
+// A code is a sign, two bits of exponent and one of fraction: 0, 0.5, 1, 1.5, 2, 3, 4, 6.  A block of 32 channels of a row shares a scale, the power of two at which its largest
+// magnitude lies in [4, 8): 2^e, e = max(floor(log2 max |x|) - 2, -127), stored as e + 127; a code is the nearest to x / 2^e, halfway the one whose fraction is 0, and over 6 it is 6.  Scales lie in
+// groups of 8 blocks (256 channels, a stage of the product's contraction): [groups][rows][8], so that a tile's scales of a stage are one piece of memory.
+#include <algorithm>
+
+#include "block_tiles.h"
+
+namespace clear {
+namespace block {
+namespace {
+
+constexpr int kGroup = 256;  // channels of a group of scales, and of a stage of the contraction
+typedef __attribute__((ext_vector_type(4), aligned(2))) int i32x4_any2;
+typedef __attribute__((ext_vector_type(4), aligned(4))) int i32x4_any4;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+int groups_of(int channels) { return (channels + kGroup - 1) / kGroup; }
+
+// ---- to 4 bits and back ---------------------------------------------------------------------------------------------------
+// Memory-bound.  A lane has 8 channels (4 lanes a block, half a wave a group), kQuantRows rows one after the other; a workgroup the same group of kQuantRows x 8 rows, whose scales are
+// one piece.
+constexpr int kQuantRows = 4;
+
+__device__ __forceinline__ unsigned top_of_block(unsigned bits)  // the largest of 4 neighbouring lanes
+{
+    bits = max(bits, (unsigned)__builtin_amdgcn_update_dpp(0, (int)bits, 0xb1, 0xf, 0xf, true));
+    return max(bits, (unsigned)__builtin_amdgcn_update_dpp(0, (int)bits, 0x4e, 0xf, 0xf, true));
+}
+// Stored exponent of a block by the bits of its largest magnitude (a NaN's or an infinity's make it 255, which stands for NaN).
+__device__ __forceinline__ int exponent_of(unsigned top) { return top >= 0x7f800000u ? 255 : max((int)(top >> 23) - 2, 0); }
+
+template <typename T>
+__global__ void __launch_bounds__(256) mx_quantize_kernel(const MxArgs a)
+{
+    const int group = blockIdx.x, half = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long first = (long long)blockIdx.y * (8 * kQuantRows) + half;
+    const int c = group * kGroup + 8 * lane;
+    const bool in = c < a.channels;  // (channels come in blocks of 32)
+    Chunk8<T> v[kQuantRows];
+#pragma unroll
+    for (int i = 0; i < kQuantRows; ++i) {
+        const long long row = first + 8 * i;
+        v[i].template load<4>((const T*)a.x + row * a.ld_x + c, in && row < a.rows ? 8 : 0, RowForm{false, false});
+    }
+#pragma unroll
+    for (int i = 0; i < kQuantRows; ++i) {
+        const long long row = first + 8 * i;
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i].get(j)) & 0x7fffffffu);
+        top = top_of_block(top);
+        const int e = exponent_of(top);
+        const float up = __uint_as_float((unsigned)(254 - min(e, 253)) << 23);  // 2^-(e - 127), exact; what it makes too small for a float is far below half of the least code
+        unsigned codes = 0;
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = v[i].get(j) * up;
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, s[0], s[1], 1.f, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, s[2], s[3], 1.f, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, s[4], s[5], 1.f, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, s[6], s[7], 1.f, 3);
+        if (row < a.rows) {
+            if (in) *(unsigned*)((unsigned char*)a.codes_out + row * a.ld_codes + c / 2) = e == 255 ? 0 : codes;
+            if ((lane & 3) == 0) ((unsigned char*)a.scales_out)[group * a.ld_scales + row * 8 + (lane >> 2)] = (unsigned char)e;  // (0 behind the last block)
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxArgs a)
+{
+    const int group = blockIdx.x, half = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long first = (long long)blockIdx.y * (8 * kQuantRows) + half;
+    const int c = group * kGroup + 8 * lane;
+    if (c >= a.channels) return;
+    unsigned codes[kQuantRows];
+    int e[kQuantRows];
+#pragma unroll
+    for (int i = 0; i < kQuantRows; ++i) {
+        const long long row = first + 8 * i;
+        codes[i] = 0, e[i] = 0;
+        if (row < a.rows) {
+            codes[i] = *(const unsigned*)((const unsigned char*)a.codes + row * a.ld_codes + c / 2);
+            e[i] = ((const unsigned char*)a.scales)[group * a.ld_scales + row * 8 + (lane >> 2)];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kQuantRows; ++i) {
+        const long long row = first + 8 * i;
+        if (row >= a.rows) break;
+        const float scale = __uint_as_float(e[i] == 0 ? 0x00400000u : e[i] == 255 ? 0x7fc00000u : (unsigned)e[i] << 23);
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            // sign, exponent and fraction put where a float has them, 2^126 too small: 0.5 is a subnormal float there, as it is a subnormal code
+            const unsigned code = codes[i] >> (4 * j);
+            const float size = __uint_as_float((code & 7) << 22) * 0x1p126f;
+            o[j] = __uint_as_float(__float_as_uint(size) | (code & 8) << 28) * scale;
+        }
+        Chunk8<T>::template store<4>((T*)a.y + row * a.ld_y + c, 8, RowForm{true, false}, o);
+    }
+}
+
+// ---- the product ------------------------------------------------------------------------------------------------------------
+// Y = X W^T + bias: A are the rows of W (the contiguous axis of the output), B those of X.  A stage is 256 of the contraction: 128 bytes of codes and 8 of scales a row.  Lane l of an
+// instruction (32 x 32 outputs, 64 of the contraction) has row l % 32 and block l / 32 of two; as a sum has no order, instruction s of a stage takes blocks s and 4 + s of its 8, so that a lane's four
+// scales are four neighbouring bytes, of which the instruction names the s-th.
+
+typedef const __attribute__((address_space(3))) i32x4* lds_i32x4_ptr;
+typedef const __attribute__((address_space(3))) int* lds_int_ptr;
+typedef const __attribute__((address_space(3))) f32x4* lds_f32x4_ptr;
+
+// 4 bytes a lane, as load_to_lds.
+template <int OFFSET>
+__device__ __forceinline__ void load_word_to_lds(const i32x4& buffer, unsigned voff, unsigned lds)
+{
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(buffer), "n"(OFFSET) : "memory", "m0", "scc");
+}
+__device__ __forceinline__ void move_far(i32x4& buffer, long long bytes)
+{
+    const unsigned long long b = ((unsigned long long)(unsigned)buffer[1] << 32 | (unsigned)buffer[0]) + (unsigned long long)bytes;
+    buffer[0] = (int)b;
+    buffer[1] = (int)(b >> 32);
+}
+
+// A tile: WA x WB waves of NA x NB blocks of 32 x 32, RING stages.
+template <int WA, int WB, int NA, int NB, int RING>
+struct Shape {
+    static constexpr int TA = 32 * NA * WA, TB = 32 * NB * WB, WAVES = WA * WB, THREADS = 64 * WAVES;
+    static constexpr int A_BYTES = TA * 128, B_BYTES = TB * 128;
+    static constexpr int A_LOADS = A_BYTES / 1024 / WAVES, B_LOADS = B_BYTES / 1024 / WAVES;  // instructions a wave, 1 KB each: 8 rows
+    static constexpr int CODE_LOADS = A_LOADS + B_LOADS, LOADS = CODE_LOADS + 2;                 // and one each for A's scales and B's, of 32 rows
+    static constexpr int SCALE_BYTES = WAVES * 256, STAGE = A_BYTES + B_BYTES + 2 * SCALE_BYTES, RING_BYTES = RING * STAGE;
+    static constexpr int LDS = RING_BYTES + WAVES * 256;  // (the bias of each wave's outputs)
+    static_assert(NA == 2, "a wave has 64 outputs, one a lane");
+    static_assert(TA <= 32 * WAVES && TB <= 32 * WAVES, "one load a wave for each operand's scales");
+    static_assert(A_BYTES / 1024 % WAVES == 0 && B_BYTES / 1024 % WAVES == 0, "the waves share the loads of a stage evenly");
+    static_assert(RING >= 2 && LDS <= 160 * 1024);
+};
+
+struct TileArgs {
+    const unsigned char *w, *ws, *x, *xs;
+    long long ld_w, ld_ws, ld_x, ld_xs;
+    const void* bias;
+    void* out;
+    long long ld_out, rows_b;  // rows_b: tokens
+    int rows_a, depth;         // outputs, channels
+    int tiles_a, tiles_b, bias_bf16, out_bf16;
+    float* parts;     // where the contraction is split: fp32 [gridDim.y][rows_b][ld_parts], to be joined; else null
+    int ld_parts;
+};
+
+// The bias of an output, 0 where it has none.
+__device__ __forceinline__ float bias_of(const TileArgs& t, int at)
+{
+    if (!t.bias || at >= t.rows_a) return 0.f;
+    return t.bias_bf16 ? (float)((const __bf16*)t.bias)[at] : ((const float*)t.bias)[at];
+}
+
+// Both operands in 4 bits (format 4); byte S of a lane's scales is that of its block.
+template <int S>
+__device__ __forceinline__ f32x16 product(i32x4 a, i32x4 b, f32x16 c, int scale_a, int scale_b)
+{
+    const i32x8 wide_a = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wide_b = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide_a, wide_b, c, 4, 4, S, scale_a, S, scale_b);
+}
+
+// A product's result is wanted here.  (The compiler keeps the scaled products, unlike the plain ones, no nearer to their places than their data does: it moves a whole stage's down past the barrier
+// and the branch behind it, with all operands kept in registers until then.)
+__device__ __forceinline__ void stay_here(f32x16& x) { asm volatile("" : "+v"(x)); }
+
+template <int WA, int WB, int NA, int NB, int RING>
+__global__ void __launch_bounds__(64 * WA * WB) mx_tile_kernel(const TileArgs t)
+{
+    typedef Shape<WA, WB, NA, NB, RING> S;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds_bytes[];
+    const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_bytes;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wa = wave % WA, wb = wave / WA;
+    int tile_a, tile_b;
+    tile_of(blockIdx.x, gridDim.x, t.tiles_a, t.tiles_b, &tile_a, &tile_b);
+    const int a_first = tile_a * S::TA;
+    const long long b_first = (long long)tile_b * S::TB;
+    const int steps_all = (t.depth + kGroup - 1) / kGroup;
+    const int it_first = (int)((long long)steps_all * blockIdx.y / gridDim.y), it_end = (int)((long long)steps_all * (blockIdx.y + 1) / gridDim.y);
+    const int steps = it_end - it_first;  // of this part of the contraction
+    const int rows_a = min(t.rows_a - a_first, S::TA), rows_b = (int)min(t.rows_b - b_first, (long long)S::TB);  // of the tile
+
+    // ---- loads of a stage: codes of A, codes of B, scales of both.  A lane's offsets stay as they are from stage to stage and the buffers move on.
+    // (what `aim` starts from is pinned in registers, so that it is not formed again from the arguments)
+    const unsigned char *w = t.w + a_first * t.ld_w, *x = t.x + b_first * t.ld_x, *ws = t.ws + a_first * 8LL, *xs = t.xs + b_first * 8;
+    int last_w = (int)((rows_a - 1) * t.ld_w), last_x = (int)((rows_b - 1) * t.ld_x), ld_w = (int)t.ld_w, ld_x = (int)t.ld_x;
+    asm("" : "+s"(w), "+s"(x), "+s"(ws), "+s"(xs), "+s"(last_w), "+s"(last_x), "+s"(ld_w), "+s"(ld_x));
+    i32x4 buf_a, buf_b, buf_sa, buf_sb;
+    unsigned voff[S::CODE_LOADS], lds_to = lds;
+    const unsigned voff_s = threadIdx.x * 4;  // (both operands' scales: lane by lane, as they lie)
+    int aimed = 0, plain_until = 0;  // the step that buffers and offsets are for; the first one behind it that takes more than moving the buffers on
+    auto rows_offset = [&](int n, int ld, int left) INLINED {
+        const int r = n * 8 + lane / 8, c = (lane % 8) ^ turn_of<64>(r);
+        return c * 32 < left ? (unsigned)(r * ld + c * 16) : kOutside;
+    };
+    // Buffers and offsets of step `aimed` of this part: the first one, one that the contraction's end cuts short, and those behind the part's last, which read nothing (and are not
+    // moved on any more).
+    auto aim = [&]() INLINED {
+        const int it = it_first + aimed, left = it < it_end ? t.depth - it * kGroup : 0;
+        buf_a = buffer_of(w + it * (kGroup / 2), left > 0 ? last_w + left / 2 : 0);
+        buf_b = buffer_of(x + it * (kGroup / 2), left > 0 ? last_x + left / 2 : 0);
+        buf_sa = buffer_of(ws + it * t.ld_ws, left > 0 ? rows_a * 8 : 0);
+        buf_sb = buffer_of(xs + it * t.ld_xs, left > 0 ? rows_b * 8 : 0);
+        settled(buf_a, buf_b);
+        settled(buf_sa, buf_sb);
+        plain_until = __builtin_amdgcn_readfirstlane(min(t.depth / kGroup, it_end) - it_first);
+        const int rest = min(left, kGroup);
+#pragma unroll
+        for (int i = 0; i < S::A_LOADS; ++i) voff[i] = rows_offset(wave * S::A_LOADS + i, ld_w, rest);
+#pragma unroll
+        for (int i = 0; i < S::B_LOADS; ++i) voff[S::A_LOADS + i] = rows_offset(wave * S::B_LOADS + i, ld_x, rest);
+    };
+    auto advance = [&](unsigned stage) INLINED {  // to the next step, whose place in LDS is `stage`
+        lds_to = lds + stage;
+        if (++aimed < plain_until) {
+            move(buf_a, kGroup / 2);
+            move(buf_b, kGroup / 2);
+            move_far(buf_sa, t.ld_ws);
+            move_far(buf_sb, t.ld_xs);
+        } else
+            aim();
+    };
+    auto load = [&](auto i) INLINED {
+        if constexpr (i < S::A_LOADS)
+            load_to_lds<i * 1024>(buf_a, voff[i], lds_to + wave * (S::A_LOADS * 1024));
+        else if constexpr (i < S::CODE_LOADS)
+            load_to_lds<S::A_BYTES + (i - S::A_LOADS) * 1024>(buf_b, voff[i], lds_to + wave * (S::B_LOADS * 1024));
+        else if constexpr (i == S::CODE_LOADS)
+            load_word_to_lds<S::A_BYTES + S::B_BYTES>(buf_sa, voff_s, lds_to + wave * 256);
+        else
+            load_word_to_lds<S::A_BYTES + S::B_BYTES + S::SCALE_BYTES>(buf_sb, voff_s, lds_to + wave * 256);
+    };
+
+    // ---- operand reads: of 32 rows block 4 h + s of a stage, h = lane / 32: one address for each s, the blocks of 32 rows at constant distances
+    constexpr int SLOTS = 4;
+    auto rows_address = [&](int first, int s) INLINED { return (unsigned)((first + (lane & 31)) * 128 + (((4 * (lane >> 5) + s) ^ turn_of<64>(lane)) << 4)); };
+    unsigned a_zero[SLOTS], b_zero[SLOTS], a_at[SLOTS], b_at[SLOTS], sa_at = 0, sb_at = 0;  // in stage 0, and in the present one
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        a_zero[i] = lds + rows_address(32 * NA * wa, i);
+        b_zero[i] = lds + S::A_BYTES + rows_address(32 * NB * wb, i);
+    }
+    const unsigned s_zero = lds + S::A_BYTES + S::B_BYTES + (lane & 31) * 8 + (lane >> 5) * 4;
+    auto enter = [&](unsigned stage) INLINED {
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) a_at[i] = a_zero[i] + stage, b_at[i] = b_zero[i] + stage;
+        sa_at = s_zero + stage + 32 * NA * wa * 8;
+        sb_at = s_zero + stage + S::SCALE_BYTES + 32 * NB * wb * 8;
+    };
+    i32x4 a[2][NA], b[2][NB];
+    int sa[NA], sb[NB], sa_next[NA], sb_next[NB];
+    constexpr int CODES = NA + NB;
+    // Read n of slot s: codes in the order of first use (a[0], b[0], the rest of a, the rest of b); then the scales, where s is a stage's first.
+    auto read = [&](auto into, auto s, auto n) INLINED {
+        if constexpr (n >= CODES + NA) {
+            sb_next[n - CODES - NA] = *(lds_int_ptr)(size_t)(sb_at + (n - CODES - NA) * 256);
+        } else if constexpr (n >= CODES) {
+            sa_next[n - CODES] = *(lds_int_ptr)(size_t)(sa_at + (n - CODES) * 256);
+        } else if constexpr (n == 0 || (n >= 2 && n <= NA)) {
+            constexpr int i = n == 0 ? 0 : n - 1;
+            a[into][i] = *(lds_i32x4_ptr)(size_t)(a_at[s] + i * 4096);
+        } else {
+            constexpr int j = n == 1 ? 0 : n - NA;
+            b[into][j] = *(lds_i32x4_ptr)(size_t)(b_at[s] + j * 4096);
+        }
+    };
+    auto take_scales = [&](unsigned mask) INLINED {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) sa[i] = sa_next[i] & mask;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sb[j] = sb_next[j] & mask;
+    };
+
+    f32x16 acc[NA][NB];
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+    // ---- the loop, as in the gated projection: a stage is 4 slots; in each the operands of the next slot are read beside the products of this one, across the barrier too; loads take half of
+    // a stage's last slot and half of the next one's first.
+    constexpr int PRODUCTS = NA * NB, READ_IN = PRODUCTS * 3 / 4, EARLY = S::LOADS / 2;
+    // Products of slot `of`; beside them the reads of slot s of the stage entered (not where s is SLOTS), and loads first .. last - 1.
+    auto slot = [&](auto of, auto s, auto first, auto last) INLINED {
+        constexpr int from = of % 2, reads = s == 0 ? 2 * CODES : CODES;
+        auto one = [&](auto n) INLINED {
+            if constexpr (s < SLOTS && n < READ_IN) {
+                auto next = [&](auto r) INLINED { read(Int<1 - from>{}, s, r); };
+                each_of<n * reads / READ_IN, (n + 1) * reads / READ_IN>(next);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            acc[n % NA][n / NA] = product<of>(a[from][n % NA], b[from][n / NA], acc[n % NA][n / NA], sa[n % NA], sb[n / NA]);
+            stay_here(acc[n % NA][n / NA]);
+            __builtin_amdgcn_sched_barrier(0);
+            each_of<first + n * (last - first) / PRODUCTS, first + (n + 1) * (last - first) / PRODUCTS>(load);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each_of<0, PRODUCTS>(one);
+    };
+    // All but `more` of this wave's loads have arrived and its reads are done; after the barrier everybody's.
+    auto settle = [](auto more) INLINED {
+        constexpr int n = more;
+        static_assert(n < 64, "vmcnt is 6 bits");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | (n >> 4) << 14);  // lgkmcnt 0, expcnt unconstrained
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto slots = [&](auto loads) INLINED {
+        auto one = [&](auto s) INLINED { slot(s, Int<s + 1>{}, Int<EARLY>{}, Int<(s == 0 && loads ? S::LOADS : EARLY)>{}); };
+        each_of<0, SLOTS - 1>(one);
+    };
+    if (steps > 0) {
+        aim();
+        each_of<0, S::LOADS>(load);
+#pragma unroll
+        for (int i = 1; i < RING; ++i) {
+            advance(i * S::STAGE);
+            if (i + 1 < RING)
+                each_of<0, S::LOADS>(load);
+            else
+                each_of<0, EARLY>(load);
+        }
+        settle(Int<(RING - 2) * S::LOADS + EARLY>{});
+        enter(0);
+        auto next = [&](auto r) INLINED { read(Int<0>{}, Int<0>{}, r); };
+        each_of<0, 2 * CODES>(next);
+        unsigned stage = 0;
+        for (int it = 0; it + 1 < steps; ++it) {
+            const unsigned next_stage = stage + S::STAGE == S::RING_BYTES ? 0 : stage + S::STAGE;
+            take_scales(~0u);
+            slots(std::true_type{});
+            settle(Int<(RING - 2) * S::LOADS>{});
+            advance(stage);
+            enter(next_stage);
+            __builtin_amdgcn_sched_barrier(0);
+            slot(Int<SLOTS - 1>{}, Int<0>{}, Int<0>{}, Int<EARLY>{});
+            stage = next_stage;
+        }
+        // (what lies behind a row's last scale is whatever it is: there the codes are 0, and so are the scales made)
+        const int blocks = min(max((t.depth - (it_end - 1) * kGroup) / 32 - 4 * (lane >> 5), 0), 4);
+        take_scales(blocks == 4 ? ~0u : (1u << 8 * blocks) - 1);
+        slots(std::false_type{});
+        slot(Int<SLOTS - 1>{}, Int<SLOTS>{}, Int<0>{}, Int<0>{});
+        settle(Int<0>{});  // (nothing may still be on its way to this workgroup's LDS, which is used again, and is given up in the end)
+    }
+
+    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Outputs go through a part of LDS of the wave's own, so that
+    // neighbouring lanes store neighbouring 16 bytes of a row.
+    constexpr int OWN = S::RING_BYTES / S::WAVES / 16 * 16;
+    const unsigned own = lds + wave * OWN;
+    const int first = a_first + 32 * NA * wa;
+    const unsigned bias = lds + S::RING_BYTES + wave * 256;
+    *(__attribute__((address_space(3))) float*)(size_t)(bias + 4 * lane) = t.parts ? 0.f : bias_of(t, first + lane);
+    auto store = [&](auto type, auto to) INLINED {
+        typedef decltype(type) T;
+        typedef T four __attribute__((ext_vector_type(4)));
+        constexpr int PER = 16 / (int)sizeof(T), BYTES = 32 * NA * (int)sizeof(T), PITCH = BYTES + 16, LANES = BYTES / 16, ROWS = 64 / LANES;
+        constexpr int FIT = OWN / (32 * PITCH), TOGETHER = FIT >= NB ? NB : FIT >= 2 && NB % 2 == 0 ? 2 : 1;
+        static_assert(FIT >= 1, "a block fits");
+        const int c = first + lane % LANES * PER;
+        auto some = [&](auto k) INLINED {
+            constexpr int j0 = k * TOGETHER;
+            auto put_block = [&](auto n) INLINED {
+                auto put = [&](auto g) INLINED {
+                    f32x4 x;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = acc[g / 4][j0 + n][4 * (g % 4) + r];
+                    *(__attribute__((address_space(3))) four*)(size_t)(own + (unsigned)((32 * n + (lane & 31)) * PITCH + (8 * g + 4 * (lane >> 5)) * (int)sizeof(T))) =
+                        __builtin_convertvector(x + *(lds_f32x4_ptr)(size_t)(bias + (8 * g + 4 * (lane >> 5)) * 4), four);
+                };
+                each_of<0, 4 * NA>(put);
+            };
+            each_of<0, TOGETHER>(put_block);
+            asm volatile("" ::: "memory");  // (a wave's LDS instructions are executed in order)
+#pragma unroll
+            for (int i = 0; i < TOGETHER * 32 / ROWS; ++i) {
+                const int at = i * ROWS + lane / LANES;
+                const i32x4 x = *(lds_i32x4_ptr)(size_t)(own + (unsigned)(at * PITCH + lane % LANES * 16));
+                const long long row = b_first + 32 * (NB * wb + j0) + at;
+                if (row < t.rows_b && c < t.rows_a) {
+                    T* const o = to(row) + c;
+                    if (c + PER <= t.rows_a) {  // (rows of any length: at any address that its elements allow)
+                        if constexpr (sizeof(T) == 2) *(i32x4_any2*)o = x;
+                        else *(i32x4_any4*)o = x;
+                    } else {
+                        typedef T piece __attribute__((ext_vector_type(PER)));
+                        const piece v = __builtin_bit_cast(piece, x);
+#pragma unroll
+                        for (int e = 0; e < PER - 1; ++e)
+                            if (c + e < t.rows_a) o[e] = v[e];
+                    }
+                }
+            }
+            asm volatile("" ::: "memory");
+        };
+        each_of<0, NB / TOGETHER>(some);
+    };
+    if (t.parts)
+        store(0.f, [&](long long row) INLINED { return t.parts + (blockIdx.y * t.rows_b + row) * t.ld_parts; });
+    else if (t.out_bf16)
+        store((__bf16)0.f, [&](long long row) INLINED { return (__bf16*)t.out + row * t.ld_out; });
+    else
+        store(0.f, [&](long long row) INLINED { return (float*)t.out + row * t.ld_out; });
+}
+
+// The sum of the parts of a split contraction, in order, and the bias to the output; 4 outputs a thread.
+__global__ void __launch_bounds__(256) mx_join_kernel(const TileArgs t, int parts, long long n)
+{
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= n) return;
+    const int each = t.ld_parts / 4;
+    const long long row = id / each, plane = t.rows_b * t.ld_parts;
+    const int c = (int)(id - row * each) * 4;
+    const float* const from = t.parts + row * t.ld_parts + c;
+    f32x4 s = *(const f32x4*)from;
+#pragma unroll 4
+    for (int p = 1; p < parts; ++p) s += *(const f32x4*)(from + p * plane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= t.rows_a) break;
+        const float y = s[e] + bias_of(t, c + e);
+        if (t.out_bf16) ((__bf16*)t.out)[row * t.ld_out + c + e] = (__bf16)y;
+        else ((float*)t.out)[row * t.ld_out + c + e] = y;
+    }
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------------------------
+// Up to 16 MT tokens: bound by the one reading of the weights.  A workgroup takes 16 outputs and all of the contraction, its 8 waves every eighth group of it: weights go straight
+// from memory to the operand registers.  Lane l of an instruction (16 x 16 outputs, 128 of the contraction) has row l % 16 and block l / 16 of four; instruction s of two takes
+// blocks s, 2 + s, 4 + s and 6 + s of a group, so that a lane's codes of a group are 32 neighbouring bytes and its scales two.  The waves' sums are added in order in LDS.
+constexpr int kFewWaves = 8;
+template <int S>
+__device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scale_a, int scale_b)
+{
+    const i32x8 wide_a = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wide_b = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_a, wide_b, c, 4, 4, S, scale_a, S, scale_b);
+}
+template <int MT>
+__global__ void __launch_bounds__(64 * kFewWaves) mx_few_kernel(const TileArgs t)
+{
+    __shared__ f32x4 part[kFewWaves][MT][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = 2 * (lane >> 4);
+    const int f0 = blockIdx.x * 16;
+    const int f = min(f0 + (lane & 15), t.rows_a - 1);
+    const unsigned char* const w = t.w + f * t.ld_w + block * 16;
+    const unsigned char* const ws = t.ws + f * 8LL + block;
+    const unsigned char *x[MT], *xs[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const long long token = min((long long)(16 * m + (lane & 15)), t.rows_b - 1);
+        x[m] = t.x + token * t.ld_x + block * 16;
+        xs[m] = t.xs + token * 8 + block;
+    }
+    f32x4 acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int groups = (t.depth + kGroup - 1) / kGroup;
+    constexpr int AHEAD = MT > 2 ? 1 : 2;  // groups whose loads are in flight together
+    for (int g0 = wave; g0 < groups; g0 += kFewWaves * AHEAD) {
+        i32x4 a[AHEAD][2], b[AHEAD][MT][2];
+        int sa[AHEAD], sb[AHEAD][MT];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int g = g0 + kFewWaves * i, left = t.depth - g * kGroup - block * 32;  // channels from this lane's first block on
+            const i32x4 zero = {0, 0, 0, 0};
+            const int mask = left >= 64 ? 0xffff : left > 0 ? 0xff : 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                a[i][k] = left > 32 * k ? *(const i32x4*)(w + (long long)g * (kGroup / 2) + 16 * k) : zero;
+#pragma unroll
+                for (int m = 0; m < MT; ++m) b[i][m][k] = left > 32 * k ? *(const i32x4*)(x[m] + (long long)g * (kGroup / 2) + 16 * k) : zero;
+            }
+            sa[i] = left > 0 ? *(const unsigned short*)(ws + g * t.ld_ws) & mask : 0;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sb[i][m] = left > 0 ? *(const unsigned short*)(xs[m] + g * t.ld_xs) & mask : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                acc[m] = few_product<0>(a[i][0], b[i][m][0], acc[m], sa[i], sb[i][m]);
+                acc[m] = few_product<1>(a[i][1], b[i][m][1], acc[m], sa[i], sb[i][m]);
+            }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) part[wave][m][lane] = acc[m];
+    __syncthreads();
+    // register r of lane l: output 4 (l / 16) + r, token l % 16
+    for (int at = threadIdx.x; at < MT * 64; at += 64 * kFewWaves) {
+        const int m = at >> 6, l = at & 63;
+        f32x4 s = part[0][m][l];
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) s += part[v][m][l];
+        const long long token = 16 * m + (l & 15);
+        const int c = f0 + 4 * (l >> 4);
+        if (token >= t.rows_b) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= t.rows_a) break;
+            const float y = s[e] + bias_of(t, c + e);
+            if (t.out_bf16) ((__bf16*)t.out)[token * t.ld_out + c + e] = (__bf16)y;
+            else ((float*)t.out)[token * t.ld_out + c + e] = y;
+        }
+    }
+}
+
+template <int WA, int WB, int NA, int NB, int RING>
+hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
+{
+    typedef Shape<WA, WB, NA, NB, RING> S;
+    t.tiles_a = (t.rows_a + S::TA - 1) / S::TA;
+    const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB;
+    if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffffffffLL / S::THREADS) return hipErrorInvalidValue;
+    t.tiles_b = (int)tiles_b;
+    if (parts == 1) t.parts = nullptr;
+    static LdsLimit limit;
+    const hipError_t allowed = limit.ensure((const void*)mx_tile_kernel<WA, WB, NA, NB, RING>, S::LDS);
+    if (allowed != hipSuccess) return allowed;
+    mx_tile_kernel<WA, WB, NA, NB, RING><<<dim3((unsigned)(tiles_b * t.tiles_a), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || parts == 1) return e;
+    const long long n = t.rows_b * (t.ld_parts / 4), blocks = (n + 255) / 256;
+    if (blocks > 0xffffffffLL / 256) return hipErrorInvalidValue;
+    mx_join_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(t, parts, n);
+    return hipGetLastError();
+}
+
+enum TileShape { kFew, kLarge, kMedium, kPair, kDeep };
+struct Plan {
+    TileShape shape;
+    int parts;
+};
+Plan plan_of(long long tokens, int channels, int outputs)
+{
+    if (tokens <= 64) return {kFew, 1};
+    const auto up = [](long long x, long long by) { return (x + by - 1) / by; };
+    const long long large = up(outputs, 256) * up(tokens, 256), small = up(outputs, 128) * up(tokens, 128);
+    if (large >= 192) return {kLarge, 1};
+    const int steps = groups_of(channels);
+    int parts = 1;
+    while (small * parts * 2 <= 256 && steps >= 4 * parts * 2 && parts < 8) parts *= 2;
+    return {small * parts <= 256 ? kDeep : kPair, parts};
+}
+
+size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+size_t codes_bytes(long long tokens, int channels) { return rounded((size_t)tokens * channels / 2); }
+size_t scales_bytes(long long tokens, int channels) { return rounded((size_t)groups_of(channels) * tokens * 8); }
+int parts_pitch(int outputs) { return (outputs + 3) / 4 * 4; }
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const MxArgs& a, int dtype, hipStream_t stream)
+{
+    // (a launch has at most 65535 x 32 rows of a grid's second axis)
+    constexpr long long each = 8 * kQuantRows, most = 65535 * each;
+    for (long long first = 0; first < a.rows; first += most) {
+        MxArgs b = a;
+        b.rows = std::min(a.rows - first, most);
+        b.x = (const char*)a.x + first * a.ld_x * (dtype == CLEAR_BF16 ? 2 : 4);
+        b.codes_out = (char*)a.codes_out + first * a.ld_codes;
+        b.scales_out = (char*)a.scales_out + first * 8;
+        const dim3 grid(groups_of(a.channels), (unsigned)((b.rows + each - 1) / each));
+        if (dtype == CLEAR_BF16) mx_quantize_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(b);
+        else mx_quantize_kernel<float><<<grid, dim3(256), 0, stream>>>(b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_mx_dequantize(const MxArgs& a, int dtype, hipStream_t stream)
+{
+    constexpr long long each = 8 * kQuantRows, most = 65535 * each;
+    for (long long first = 0; first < a.rows; first += most) {
+        MxArgs b = a;
+        b.rows = std::min(a.rows - first, most);
+        b.codes = (const char*)a.codes + first * a.ld_codes;
+        b.scales = (const char*)a.scales + first * 8;
+        b.y = (char*)a.y + first * a.ld_y * (dtype == CLEAR_BF16 ? 2 : 4);
+        const dim3 grid(groups_of(a.channels), (unsigned)((b.rows + each - 1) / each));
+        if (dtype == CLEAR_BF16) mx_dequantize_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(b);
+        else mx_dequantize_kernel<float><<<grid, dim3(256), 0, stream>>>(b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// The tokens in 4 bits, unless they come so, then the parts of a split contraction.
+size_t mx_linear_workspace_bytes(long long tokens, int channels, int outputs, bool quantized)
+{
+    if (tokens == 0) return 0;
+    const int parts = plan_of(tokens, channels, outputs).parts;
+    return (quantized ? 0 : codes_bytes(tokens, channels) + scales_bytes(tokens, channels)) + (parts > 1 ? (size_t)parts * tokens * parts_pitch(outputs) * 4 : 0);
+}
+
+hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
+{
+    TileArgs t = {};
+    t.w = (const unsigned char*)a.w, t.ws = (const unsigned char*)a.ws, t.x = (const unsigned char*)a.x, t.xs = (const unsigned char*)a.xs;
+    t.ld_w = a.ld_w, t.ld_ws = a.ld_ws, t.ld_x = a.ld_x, t.ld_xs = a.ld_xs;
+    t.bias = a.bias, t.bias_bf16 = a.bias_dtype == CLEAR_BF16;
+    t.out = a.y, t.ld_out = a.ld_y, t.out_bf16 = a.out_dtype == CLEAR_BF16;
+    t.rows_a = a.outputs, t.rows_b = a.tokens, t.depth = a.channels;
+    unsigned char* ws = (unsigned char*)a.workspace;
+    if (!a.xs) {
+        MxArgs q = {};
+        q.x = a.x, q.ld_x = a.ld_x;
+        q.codes_out = ws, q.ld_codes = a.channels / 2;
+        q.scales_out = ws + codes_bytes(a.tokens, a.channels), q.ld_scales = a.tokens * 8;
+        q.rows = a.tokens, q.channels = a.channels;
+        const hipError_t e = launch_mx_quantize(q, a.x_dtype, stream);
+        if (e != hipSuccess) return e;
+        t.x = ws, t.ld_x = q.ld_codes, t.xs = (const unsigned char*)q.scales_out, t.ld_xs = q.ld_scales;
+        ws += codes_bytes(a.tokens, a.channels) + scales_bytes(a.tokens, a.channels);
+    }
+    const Plan p = plan_of(a.tokens, a.channels, a.outputs);
+    t.parts = (float*)ws, t.ld_parts = parts_pitch(a.outputs);
+    switch (p.shape) {
+    case kFew: {
+        const dim3 grid((a.outputs + 15) / 16), block(64 * kFewWaves);
+        if (a.tokens <= 16) mx_few_kernel<1><<<grid, block, 0, stream>>>(t);
+        else if (a.tokens <= 32) mx_few_kernel<2><<<grid, block, 0, stream>>>(t);
+        else mx_few_kernel<4><<<grid, block, 0, stream>>>(t);
+        return hipGetLastError();
+    }
+    case kLarge: return launch_tiles<4, 2, 2, 4, 2>(t, p.parts, stream);
+    case kMedium: return launch_tiles<4, 2, 2, 3, 2>(t, p.parts, stream);
+    case kPair: return launch_tiles<2, 2, 2, 2, 2>(t, p.parts, stream);
+    default: return launch_tiles<2, 2, 2, 2, 4>(t, p.parts, stream);
+    }
+}
+
+}  // namespace block
+}  // namespace clear

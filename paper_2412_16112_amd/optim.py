@@ -19,6 +19,7 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ca.ClearAttnError(ca.CLEAR_ERR_INVALID_ARG, "state_bits must be 32 or 8")
         self.hyper = dict(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
+        self.grad_norm = None  # of the last step that was given a bound for it
         self.state_bits = state_bits
         states = [cb.adamw_state(p.detach(), state_bits) for p in self.params]
         # (tuples, and properties without a setter: a step works on these tensors, others in their place would be ignored)
@@ -56,9 +57,10 @@ class AdamW:
         for _, _, _, counts, _ in self._tables:
             counts[:] = [n] * len(counts)
 
-    def step(self, grads=None, grad_scale=None, stream=None, **hyper):
+    def step(self, grads=None, grad_scale=None, stream=None, max_norm=None, **hyper):
         """One step with the parameters' .grad, or with `grads` (a list in their order); entries that are None are skipped: a parameter counts its own updates.  Keyword arguments
-        (lr, ...) hold for this step only.  grad_scale: an fp32 device scalar that the gradients are multiplied by."""
+        (lr, ...) hold for this step only.  grad_scale: an fp32 device scalar that the gradients are multiplied by.  max_norm: with it, the gradients are scaled down to that norm of all of
+        them together (times grad_scale) where they have a larger one; `grad_norm` then is what they had, an fp32 scalar on the device.  The gradients themselves stay as they are."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
@@ -69,6 +71,8 @@ class AdamW:
                 raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "a parameter has moved since the optimizer was made")
             cb._check_scale(grad_scale, params[0].device)
             given.append(cb._set_grads(table, params, [grads[i] for i in members]))
+        if max_norm is not None and any(g is not None for g in grads):
+            self.grad_norm, grad_scale = cb.grad_norm(grads, max_norm=max_norm, grad_scale=grad_scale, stream=stream)
         for (_, params, table, counts, masters), some in zip(self._tables, given):
             for n in sorted(set(counts)):  # (parameters that have had as many updates go together: all of them, unless gradients were missing; those without one are skipped)
                 rows = table if counts.count(n) == len(counts) else table[[c == n for c in counts]]
