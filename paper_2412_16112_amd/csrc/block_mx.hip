@@ -148,6 +148,7 @@ struct TileArgs {
     long long ld_out, rows_b;  // rows_b: tokens
     int rows_a, depth;         // outputs, channels
     int tiles_a, tiles_b, bias_bf16, out_bf16;
+    unsigned tiles;
     float* parts;     // where the contraction is split: fp32 [gridDim.y][rows_b][ld_parts], to be joined; else null
     int ld_parts;
 };
@@ -159,6 +160,14 @@ __device__ __forceinline__ float bias_of(const TileArgs& t, int at)
     return t.bias_bf16 ? (float)((const __bf16*)t.bias)[at] : ((const float*)t.bias)[at];
 }
 
+// Its bits as they lie in memory, 0 where the contraction is split (nothing waits for them here).
+typedef const __attribute__((address_space(4))) TileArgs* tile_args_ptr;
+__device__ __forceinline__ unsigned bias_bits(tile_args_ptr t, int at)
+{
+    if (t->parts || !t->bias || at >= t->rows_a) return 0;
+    return t->bias_bf16 ? ((const unsigned short*)t->bias)[at] : ((const unsigned*)t->bias)[at];
+}
+
 // Both operands in 4 bits (format 4); byte S of a lane's scales is that of its block.
 template <int S>
 __device__ __forceinline__ f32x16 product(i32x4 a, i32x4 b, f32x16 c, int scale_a, int scale_b)
@@ -167,66 +176,99 @@ __device__ __forceinline__ f32x16 product(i32x4 a, i32x4 b, f32x16 c, int scale_
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide_a, wide_b, c, 4, 4, S, scale_a, S, scale_b);
 }
 
+// A lane's or wave's number, or the kernel's arguments, as if they were new.  What a tile needs of them once is formed anew for each tile: kept in registers through all tiles, it would cost
+// the loop its own.
+__device__ __forceinline__ int anew(int lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+__device__ __forceinline__ int anew_scalar(int wave)
+{
+    asm volatile("" : "+s"(wave));
+    return wave;
+}
+__device__ __forceinline__ tile_args_ptr args_anew()
+{
+    tile_args_ptr p = (tile_args_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
 // A product's result is wanted here.  (The compiler keeps the scaled products, unlike the plain ones, no nearer to their places than their data does: it moves a whole stage's down past the barrier
 // and the branch behind it, with all operands kept in registers until then.)
 __device__ __forceinline__ void stay_here(f32x16& x) { asm volatile("" : "+v"(x)); }
 
 template <int WA, int WB, int NA, int NB, int RING>
-__global__ void __launch_bounds__(64 * WA * WB) mx_tile_kernel(const TileArgs t)
+__global__ void __launch_bounds__(64 * WA * WB, 2) mx_tile_kernel(const TileArgs t)  // (two waves a SIMD, 256 registers: with more the compiler takes the products' results to accumulation registers and back)
 {
     typedef Shape<WA, WB, NA, NB, RING> S;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds_bytes[];
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_bytes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wa = wave % WA, wb = wave / WA;
-    int tile_a, tile_b;
-    tile_of(blockIdx.x, gridDim.x, t.tiles_a, t.tiles_b, &tile_a, &tile_b);
-    const int a_first = tile_a * S::TA;
-    const long long b_first = (long long)tile_b * S::TB;
     const int steps_all = (t.depth + kGroup - 1) / kGroup;
     const int it_first = (int)((long long)steps_all * blockIdx.y / gridDim.y), it_end = (int)((long long)steps_all * (blockIdx.y + 1) / gridDim.y);
     const int steps = it_end - it_first;  // of this part of the contraction
-    const int rows_a = min(t.rows_a - a_first, S::TA), rows_b = (int)min(t.rows_b - b_first, (long long)S::TB);  // of the tile
+    const int plain = min(t.depth / kGroup, it_end) - it_first;  // those of them that the contraction's end does not cut short
+    const int rest = min(t.depth - (it_end - 1) * kGroup, kGroup);  // channels of the last step
 
     // ---- loads of a stage: codes of A, codes of B, scales of both.  A lane's offsets stay as they are from stage to stage and the buffers move on.
-    // (what `aim` starts from is pinned in registers, so that it is not formed again from the arguments)
-    const unsigned char *w = t.w + a_first * t.ld_w, *x = t.x + b_first * t.ld_x, *ws = t.ws + a_first * 8LL, *xs = t.xs + b_first * 8;
-    int last_w = (int)((rows_a - 1) * t.ld_w), last_x = (int)((rows_b - 1) * t.ld_x), ld_w = (int)t.ld_w, ld_x = (int)t.ld_x;
-    asm("" : "+s"(w), "+s"(x), "+s"(ws), "+s"(xs), "+s"(last_w), "+s"(last_x), "+s"(ld_w), "+s"(ld_x));
     i32x4 buf_a, buf_b, buf_sa, buf_sb;
     unsigned voff[S::CODE_LOADS], lds_to = lds;
     const unsigned voff_s = threadIdx.x * 4;  // (both operands' scales: lane by lane, as they lie)
-    int aimed = 0, plain_until = 0;  // the step that buffers and offsets are for; the first one behind it that takes more than moving the buffers on
-    auto rows_offset = [&](int n, int ld, int left) INLINED {
-        const int r = n * 8 + lane / 8, c = (lane % 8) ^ turn_of<64>(r);
-        return c * 32 < left ? (unsigned)(r * ld + c * 16) : kOutside;
+    int aimed = 0;                            // the step that buffers and offsets are for
+    auto row_of = [](int n, int l) INLINED { return n * 8 + l / 8; };
+    auto chunk_of = [&](int n, int l) INLINED { return (l % 8) ^ turn_of<64>(row_of(n, l)); };
+    auto place_of = [](int i, int w) INLINED { return i < S::A_LOADS ? w * S::A_LOADS + i : w * S::B_LOADS + i - S::A_LOADS; };
+    // Of a step that the contraction's end cuts short: the chunks behind it are not loaded.
+    auto cut = [&]() INLINED {
+        const int l = anew(lane), v = anew_scalar(wave);
+#pragma unroll
+        for (int i = 0; i < S::CODE_LOADS; ++i)
+            if (chunk_of(place_of(i, v), l) * 32 >= rest) voff[i] = kOutside;
     };
-    // Buffers and offsets of step `aimed` of this part: the first one, one that the contraction's end cuts short, and those behind the part's last, which read nothing (and are not
-    // moved on any more).
-    auto aim = [&]() INLINED {
-        const int it = it_first + aimed, left = it < it_end ? t.depth - it * kGroup : 0;
-        buf_a = buffer_of(w + it * (kGroup / 2), left > 0 ? last_w + left / 2 : 0);
-        buf_b = buffer_of(x + it * (kGroup / 2), left > 0 ? last_x + left / 2 : 0);
-        buf_sa = buffer_of(ws + it * t.ld_ws, left > 0 ? rows_a * 8 : 0);
-        buf_sb = buffer_of(xs + it * t.ld_xs, left > 0 ? rows_b * 8 : 0);
+    int a_first, rows_b;
+    long long b_first;
+    const long long ld_ws = t.ld_ws, ld_xs = t.ld_xs;
+    auto begin = [&](unsigned id) INLINED {  // buffers and offsets of a tile's first step
+        const tile_args_ptr q = args_anew();
+        const int l = anew(lane), v = anew_scalar(wave);
+        int tile_a, tile_b;
+        tile_of(id, q->tiles, q->tiles_a, q->tiles_b, &tile_a, &tile_b);
+        a_first = tile_a * S::TA, b_first = (long long)tile_b * S::TB;
+        const int rows_a = min(q->rows_a - a_first, S::TA);
+        rows_b = (int)min(q->rows_b - b_first, (long long)S::TB);
+        const int left = (q->depth - it_first * kGroup) / 2;  // bytes of a row of codes
+        const long long ld_w = q->ld_w, ld_x = q->ld_x;
+        buf_a = buffer_of(q->w + a_first * ld_w + it_first * (kGroup / 2), (rows_a - 1) * ld_w + left);
+        buf_b = buffer_of(q->x + b_first * ld_x + it_first * (kGroup / 2), (rows_b - 1) * ld_x + left);
+        buf_sa = buffer_of(q->ws + it_first * ld_ws + a_first * 8LL, rows_a * 8);
+        buf_sb = buffer_of(q->xs + it_first * ld_xs + b_first * 8, rows_b * 8);
         settled(buf_a, buf_b);
         settled(buf_sa, buf_sb);
-        plain_until = __builtin_amdgcn_readfirstlane(min(t.depth / kGroup, it_end) - it_first);
-        const int rest = min(left, kGroup);
 #pragma unroll
-        for (int i = 0; i < S::A_LOADS; ++i) voff[i] = rows_offset(wave * S::A_LOADS + i, ld_w, rest);
-#pragma unroll
-        for (int i = 0; i < S::B_LOADS; ++i) voff[S::A_LOADS + i] = rows_offset(wave * S::B_LOADS + i, ld_x, rest);
+        for (int i = 0; i < S::CODE_LOADS; ++i) {
+            const int n = place_of(i, v);
+            voff[i] = (unsigned)(row_of(n, l) * (int)(i < S::A_LOADS ? ld_w : ld_x) + chunk_of(n, l) * 16);
+        }
+        lds_to = lds;
+        aimed = 0;
+        if (plain == 0) cut();
     };
-    auto advance = [&](unsigned stage) INLINED {  // to the next step, whose place in LDS is `stage`
+    // (A buffer that moves on along its rows keeps its length, which is still short of the row behind the last: what it lets through behind the last row's part of the step, no lane's
+    // offset reaches.)
+    auto advance = [&](unsigned stage) INLINED {  // to the next step, whose place in LDS is `stage`; behind the last one nothing is read
         lds_to = lds + stage;
-        if (++aimed < plain_until) {
-            move(buf_a, kGroup / 2);
-            move(buf_b, kGroup / 2);
-            move_far(buf_sa, t.ld_ws);
-            move_far(buf_sb, t.ld_xs);
-        } else
-            aim();
+        move(buf_a, kGroup / 2);
+        move(buf_b, kGroup / 2);
+        move_far(buf_sa, ld_ws);
+        move_far(buf_sb, ld_xs);
+        if (++aimed >= plain) {
+            if (aimed < steps)
+                cut();
+            else
+                buf_a[2] = buf_b[2] = buf_sa[2] = buf_sb[2] = 0;
+        }
     };
     auto load = [&](auto i) INLINED {
         if constexpr (i < S::A_LOADS)
@@ -280,12 +322,6 @@ __global__ void __launch_bounds__(64 * WA * WB) mx_tile_kernel(const TileArgs t)
     };
 
     f32x16 acc[NA][NB];
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
     // ---- the loop, as in the gated projection: a stage is 4 slots; in each the operands of the next slot are read beside the products of this one, across the barrier too; loads take half of
     // a stage's last slot and half of the next one's first.
@@ -320,9 +356,12 @@ __global__ void __launch_bounds__(64 * WA * WB) mx_tile_kernel(const TileArgs t)
         auto one = [&](auto s) INLINED { slot(s, Int<s + 1>{}, Int<EARLY>{}, Int<(s == 0 && loads ? S::LOADS : EARLY)>{}); };
         each_of<0, SLOTS - 1>(one);
     };
-    if (steps > 0) {
-        aim();
-        each_of<0, S::LOADS>(load);
+    const unsigned tiles = t.tiles;
+    unsigned id = blockIdx.x;
+    begin(id);
+    each_of<0, S::LOADS>(load);
+    int stores = 0;  // that this wave has under way since
+    while (true) {
 #pragma unroll
         for (int i = 1; i < RING; ++i) {
             advance(i * S::STAGE);
@@ -331,7 +370,22 @@ __global__ void __launch_bounds__(64 * WA * WB) mx_tile_kernel(const TileArgs t)
             else
                 each_of<0, EARLY>(load);
         }
-        settle(Int<(RING - 2) * S::LOADS + EARLY>{});
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        // (the stores of the tile before lie between the first stage's loads and those of the others: they need not have arrived)
+        constexpr int BEHIND = (RING - 2) * S::LOADS + EARLY;
+        constexpr int NARROW = 4 * NB, WIDE = 8 * NB;  // of a whole tile's outputs in bf16, in fp32
+        if (stores == WIDE)
+            settle(Int<BEHIND + WIDE>{});
+        else if (stores == NARROW)
+            settle(Int<BEHIND + NARROW>{});
+        else
+            settle(Int<BEHIND>{});
+        const unsigned bias_raw = bias_bits(args_anew(), a_first + 32 * NA * wa + lane);  // (asked for here, where it delays nothing)
         enter(0);
         auto next = [&](auto r) INLINED { read(Int<0>{}, Int<0>{}, r); };
         each_of<0, 2 * CODES>(next);
@@ -348,70 +402,95 @@ __global__ void __launch_bounds__(64 * WA * WB) mx_tile_kernel(const TileArgs t)
             stage = next_stage;
         }
         // (what lies behind a row's last scale is whatever it is: there the codes are 0, and so are the scales made)
-        const int blocks = min(max((t.depth - (it_end - 1) * kGroup) / 32 - 4 * (lane >> 5), 0), 4);
+        const int blocks = min(max(rest / 32 - 4 * (lane >> 5), 0), 4);
         take_scales(blocks == 4 ? ~0u : (1u << 8 * blocks) - 1);
         slots(std::false_type{});
         slot(Int<SLOTS - 1>{}, Int<SLOTS>{}, Int<0>{}, Int<0>{});
-        settle(Int<0>{});  // (nothing may still be on its way to this workgroup's LDS, which is used again, and is given up in the end)
-    }
+        settle(Int<0>{});  // (nothing may still be on its way to this workgroup's LDS, which is used again)
 
-    // ---- epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Outputs go through a part of LDS of the wave's own, so that
-    // neighbouring lanes store neighbouring 16 bytes of a row.
-    constexpr int OWN = S::RING_BYTES / S::WAVES / 16 * 16;
-    const unsigned own = lds + wave * OWN;
-    const int first = a_first + 32 * NA * wa;
-    const unsigned bias = lds + S::RING_BYTES + wave * 256;
-    *(__attribute__((address_space(3))) float*)(size_t)(bias + 4 * lane) = t.parts ? 0.f : bias_of(t, first + lane);
-    auto store = [&](auto type, auto to) INLINED {
-        typedef decltype(type) T;
-        typedef T four __attribute__((ext_vector_type(4)));
-        constexpr int PER = 16 / (int)sizeof(T), BYTES = 32 * NA * (int)sizeof(T), PITCH = BYTES + 16, LANES = BYTES / 16, ROWS = 64 / LANES;
-        constexpr int FIT = OWN / (32 * PITCH), TOGETHER = FIT >= NB ? NB : FIT >= 2 && NB % 2 == 0 ? 2 : 1;
-        static_assert(FIT >= 1, "a block fits");
-        const int c = first + lane % LANES * PER;
-        auto some = [&](auto k) INLINED {
-            constexpr int j0 = k * TOGETHER;
-            auto put_block = [&](auto n) INLINED {
-                auto put = [&](auto g) INLINED {
-                    f32x4 x;
+        *(__attribute__((address_space(3))) float*)(size_t)(lds + S::RING_BYTES + wave * 256 + 4 * lane) = __uint_as_float(args_anew()->bias_bf16 ? bias_raw << 16 : bias_raw);
+        // the next tile's first stage is loaded beside the epilogue, which has the rest of LDS
+        const int out_a = a_first, out_rows = rows_b;
+        const long long out_b = b_first;
+        id += gridDim.x;
+        const bool more = id < tiles;
+        if (more) {
+            begin(id);
+            each_of<0, S::LOADS>(load);
+        }
+        // epilogue: register r of acc[i][j] is A row 8 (r / 4) + 4 (lane / 32) + r % 4 and B row lane % 32 of the two blocks.  Outputs go through a part of LDS of the wave's own, so that
+        // neighbouring lanes store neighbouring 16 bytes of a row.
+        constexpr int OWN = (S::RING_BYTES - S::STAGE) / S::WAVES / 16 * 16;
+        const tile_args_ptr q = args_anew();
+        const int l = anew(lane), v = anew_scalar(wave), va = v % WA, vb = v / WA, out_width = q->rows_a;
+        const unsigned own = lds + S::STAGE + v * OWN, bias = lds + S::RING_BYTES + v * 256;
+        const int first = out_a + 32 * NA * va;
+        // BIASED: the bias is added.  WHOLE: the tile has all of its outputs, which needs no looking at each (half of the epilogue's instructions).
+        auto store = [&](auto type, auto whole, auto biased, decltype(type)* to, long long ld) INLINED {
+            typedef decltype(type) T;
+            typedef T four __attribute__((ext_vector_type(4)));
+            constexpr int PER = 16 / (int)sizeof(T), BYTES = 32 * NA * (int)sizeof(T), PITCH = BYTES + 16, LANES = BYTES / 16, ROWS = 64 / LANES;
+            constexpr int FIT = OWN / (32 * PITCH), TOGETHER = FIT >= NB ? NB : FIT >= 2 && NB % 2 == 0 ? 2 : 1;
+            static_assert(FIT >= 1, "a block fits");
+            const int c = first + l % LANES * PER, in = 32 * NB * vb + l / LANES;  // this lane's outputs in its first row, and that in the tile
+            T* o = to + (out_b + in) * ld + c;
+            auto some = [&](auto k) INLINED {
+                constexpr int j0 = k * TOGETHER;
+                auto put_block = [&](auto n) INLINED {
+                    auto put = [&](auto g) INLINED {
+                        f32x4 x;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = acc[g / 4][j0 + n][4 * (g % 4) + r];
-                    *(__attribute__((address_space(3))) four*)(size_t)(own + (unsigned)((32 * n + (lane & 31)) * PITCH + (8 * g + 4 * (lane >> 5)) * (int)sizeof(T))) =
-                        __builtin_convertvector(x + *(lds_f32x4_ptr)(size_t)(bias + (8 * g + 4 * (lane >> 5)) * 4), four);
+                        for (int r = 0; r < 4; ++r) x[r] = acc[g / 4][j0 + n][4 * (g % 4) + r];
+                        if constexpr (biased) x += *(lds_f32x4_ptr)(size_t)(bias + (8 * g + 4 * (l >> 5)) * 4);
+                        *(__attribute__((address_space(3))) four*)(size_t)(own + (unsigned)((32 * n + (l & 31)) * PITCH + (8 * g + 4 * (l >> 5)) * (int)sizeof(T))) =
+                            __builtin_convertvector(x, four);
+                    };
+                    each_of<0, 4 * NA>(put);
                 };
-                each_of<0, 4 * NA>(put);
-            };
-            each_of<0, TOGETHER>(put_block);
-            asm volatile("" ::: "memory");  // (a wave's LDS instructions are executed in order)
+                each_of<0, TOGETHER>(put_block);
+                asm volatile("" ::: "memory");  // (a wave's LDS instructions are executed in order)
 #pragma unroll
-            for (int i = 0; i < TOGETHER * 32 / ROWS; ++i) {
-                const int at = i * ROWS + lane / LANES;
-                const i32x4 x = *(lds_i32x4_ptr)(size_t)(own + (unsigned)(at * PITCH + lane % LANES * 16));
-                const long long row = b_first + 32 * (NB * wb + j0) + at;
-                if (row < t.rows_b && c < t.rows_a) {
-                    T* const o = to(row) + c;
-                    if (c + PER <= t.rows_a) {  // (rows of any length: at any address that its elements allow)
-                        if constexpr (sizeof(T) == 2) *(i32x4_any2*)o = x;
-                        else *(i32x4_any4*)o = x;
-                    } else {
-                        typedef T piece __attribute__((ext_vector_type(PER)));
-                        const piece v = __builtin_bit_cast(piece, x);
+                for (int i = 0; i < TOGETHER * 32 / ROWS; ++i, o += ROWS * ld) {
+                    const i32x4 x = *(lds_i32x4_ptr)(size_t)(own + (unsigned)((i * ROWS + l / LANES) * PITCH + l % LANES * 16));
+                    auto put = [&] {  // (rows of any length: at any address that its elements allow)
+                        if constexpr (sizeof(T) == 2) __builtin_nontemporal_store(x, (i32x4_any2*)o);
+                        else __builtin_nontemporal_store(x, (i32x4_any4*)o);
+                    };
+                    if constexpr (whole) {
+                        put();
+                    } else if (in + 32 * j0 + i * ROWS < out_rows && c < out_width) {
+                        if (c + PER <= out_width) {
+                            put();
+                        } else {
+                            typedef T piece __attribute__((ext_vector_type(PER)));
+                            const piece v = __builtin_bit_cast(piece, x);
 #pragma unroll
-                        for (int e = 0; e < PER - 1; ++e)
-                            if (c + e < t.rows_a) o[e] = v[e];
+                            for (int e = 0; e < PER - 1; ++e)
+                                if (c + e < out_width) o[e] = v[e];
+                        }
                     }
                 }
-            }
-            asm volatile("" ::: "memory");
+                asm volatile("" ::: "memory");
+            };
+            each_of<0, NB / TOGETHER>(some);
         };
-        each_of<0, NB / TOGETHER>(some);
-    };
-    if (t.parts)
-        store(0.f, [&](long long row) INLINED { return t.parts + (blockIdx.y * t.rows_b + row) * t.ld_parts; });
-    else if (t.out_bf16)
-        store((__bf16)0.f, [&](long long row) INLINED { return (__bf16*)t.out + row * t.ld_out; });
-    else
-        store(0.f, [&](long long row) INLINED { return (float*)t.out + row * t.ld_out; });
+        const bool wide = q->parts || !q->out_bf16, whole = out_a + S::TA <= out_width && out_rows == S::TB, biased = q->bias && !q->parts;
+        stores = !whole ? 0 : wide ? WIDE : NARROW;
+        auto store_as = [&](auto type, decltype(type)* to, long long ld) INLINED {
+            if (!whole) store(type, std::false_type{}, std::true_type{}, to, ld);
+            else if (biased) store(type, std::true_type{}, std::true_type{}, to, ld);
+            else store(type, std::true_type{}, std::false_type{}, to, ld);
+        };
+        if (wide)
+            store_as(0.f, q->parts ? q->parts + blockIdx.y * q->rows_b * q->ld_parts : (float*)q->out, q->parts ? q->ld_parts : q->ld_out);
+        else
+            store_as((__bf16)0.f, (__bf16*)q->out, q->ld_out);
+        if (!more) break;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(15 | 7 << 4 | 3 << 14);  // lgkmcnt 0: the epilogue's part of LDS is read
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
 }
 
 // The sum of the parts of a split contraction, in order, and the bias to the output; 4 outputs a thread.
@@ -527,7 +606,9 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     static LdsLimit limit;
     const hipError_t allowed = limit.ensure((const void*)mx_tile_kernel<WA, WB, NA, NB, RING>, S::LDS);
     if (allowed != hipSuccess) return allowed;
-    mx_tile_kernel<WA, WB, NA, NB, RING><<<dim3((unsigned)(tiles_b * t.tiles_a), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
+    t.tiles = (unsigned)(tiles_b * t.tiles_a);
+    const unsigned resident = 256 * (S::LDS <= 80 * 1024 ? 2 : 1);  // workgroups that the CUs hold: a multiple of 8, so that a workgroup's tiles are its XCD's
+    mx_tile_kernel<WA, WB, NA, NB, RING><<<dim3(std::min(t.tiles, resident), parts), dim3(S::THREADS), S::LDS, stream>>>(t);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts == 1) return e;
     const long long n = t.rows_b * (t.ld_parts / 4), blocks = (n + 255) / 256;
@@ -536,7 +617,7 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     return hipGetLastError();
 }
 
-enum TileShape { kFew, kLarge, kMedium, kPair, kDeep };
+enum TileShape { kFew, kLarge, kPair, kDeep };
 struct Plan {
     TileShape shape;
     int parts;
@@ -636,7 +717,6 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
         return hipGetLastError();
     }
     case kLarge: return launch_tiles<4, 2, 2, 4, 2>(t, p.parts, stream);
-    case kMedium: return launch_tiles<4, 2, 2, 3, 2>(t, p.parts, stream);
     case kPair: return launch_tiles<2, 2, 2, 2, 2>(t, p.parts, stream);
     default: return launch_tiles<2, 2, 2, 2, 4>(t, p.parts, stream);
     }
