@@ -32,7 +32,7 @@ EXPORTS = [
     "clear_block_layer_norm_backward", "clear_block_layer_norm_workspace", "clear_block_gated_ff", "clear_block_gated_ff_backward",
     "clear_block_gated_ff_workspace", "clear_block_adamw", "clear_block_adamw_decode", "clear_block_residual_norm",
     "clear_block_residual_norm_backward", "clear_block_residual_norm_workspace", "clear_block_grad_norm", "clear_block_grad_norm_workspace",
-    "clear_block_grad_scale", "clear_block_mx_quantize", "clear_block_mx_dequantize", "clear_block_mx_linear", "clear_block_mx_linear_workspace",
+    "clear_block_grad_clip", "clear_block_grad_scale", "clear_block_mx_quantize", "clear_block_mx_dequantize", "clear_block_mx_linear", "clear_block_mx_linear_workspace",
 ]
 
 
@@ -70,6 +70,7 @@ def lib():
         L.clear_block_residual_norm_backward.argtypes = [vp] * 14 + [ll, ll, i, vp, i, i, i, i, f, f, f, i, i, i, vp, vp]
         L.clear_block_residual_norm_workspace.argtypes = [ll, ll, i, i, i]
         L.clear_block_grad_norm.argtypes = [i, vp, i, d, vp, vp, vp, vp, vp]
+        L.clear_block_grad_clip.argtypes = L.clear_block_grad_norm.argtypes
         L.clear_block_grad_norm_workspace.argtypes = [i, vp]
         L.clear_block_grad_scale.argtypes = [i, vp, vp, vp]
         L.clear_block_mx_quantize.argtypes = [vp, vp, vp, ll, i, ll, ll, ll, i, vp]
@@ -97,6 +98,15 @@ def _refuse(message, status=CLEAR_ERR_INVALID_ARG):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+_codes = {torch.bfloat16: CLEAR_BF16, torch.float32: CLEAR_F32}
+
+
+def _code(t):
+    """ca._dtype_code, by a table."""
+    code = _codes.get(t.dtype)
+    return ca._dtype_code(t) if code is None else code
 
 
 # Handle of torch's current stream of a device, without the Stream object around it (2 us a call) where torch offers that.
@@ -292,34 +302,52 @@ def _record(t, stream):
 
 # ---- gated residual with its norms -----------------------------------------------------------------------------------------
 
-def _norm_kinds(kind, post):
-    if kind not in NORMS or kind is None:
+_kinds = {"layer": CLEAR_NORM_LAYER, "rms": CLEAR_NORM_RMS}
+
+
+def _residual_numbers(x, y, kind, post):
+    """(kind, post, dtype, stream dtype, groups, rows, C) of a call."""
+    if kind not in _kinds:
         _refuse("kind must be 'layer' or 'rms'")
     if post not in NORMS:
         _refuse("post must be None, 'layer' or 'rms'")
-    return NORMS[kind], NORMS[post]
+    if y.shape != x.shape:
+        _refuse("x and y must have one shape", CLEAR_ERR_MISMATCH)
+    return (_kinds[kind], NORMS[post], _code(y), _code(x)) + _rows(x)
 
 
 def _residual_vectors(x, gate, weight, bias, post_weight, post):
     """(gate_per_group, per_group, weight dtype code): gate, weight and bias are [C], or [B, C] for x [B, N, C]; post_weight is [C]."""
-    per_group, code = _norm_weights(x, weight, bias)
-    gate_per_group, _ = _norm_weights(x, gate, None)
-    if post_weight is not None:
-        if post is None:
-            _refuse("post_weight without a post norm")
-        if post_weight.dim() != 1:
-            _refuse("post_weight must be [C]")
-        _norm_weights(x, post_weight, None)
-    given = [v for v in (gate, weight, bias, post_weight) if v is not None]
-    if any(v.dtype != given[0].dtype for v in given):
-        _refuse("gate, weight, bias and post_weight must have one dtype", CLEAR_ERR_MISMATCH)
-    return gate_per_group, per_group, ca._dtype_code(given[0]) if given else CLEAR_F32
+    shape = x.shape
+    one, many = shape[-1:], (shape[0], shape[2]) if len(shape) == 3 else None
+    per_group, dtype = [0, 0, 0, 0], None
+    for i, v in enumerate((gate, weight, bias, post_weight)):
+        if v is None:
+            continue
+        if v.shape != one:
+            if i == 3 or v.shape != many:
+                _refuse("post_weight must be [C]" if i == 3 else "gate, weight and bias must be [C], or [B, C] for a tensor [B, N, C]")
+            per_group[i] = 1
+        if not v.is_contiguous():
+            _refuse("gate, weight, bias and post_weight must be contiguous")
+        if dtype is None:
+            dtype = v.dtype
+        elif v.dtype != dtype:
+            _refuse("gate, weight, bias and post_weight must have one dtype", CLEAR_ERR_MISMATCH)
+    if post_weight is not None and post is None:
+        _refuse("post_weight without a post norm")
+    if weight is not None and bias is not None and per_group[1] != per_group[2]:
+        _refuse("weight and bias must agree in shape", CLEAR_ERR_MISMATCH)
+    some = gate if gate is not None else weight if weight is not None else bias if bias is not None else post_weight
+    return per_group[0], per_group[1] | per_group[2], CLEAR_F32 if some is None else _code(some)
 
 
-def _residual_tensors(x, y):
-    if y.shape != x.shape:
-        _refuse("x and y must have one shape", CLEAR_ERR_MISMATCH)
-    return ca._dtype_code(y), ca._dtype_code(x)
+def _strides_of(named):
+    """(group, row) strides of the tensors (0, 0 for None)."""
+    out = []
+    for name, t in named:
+        out += (0, 0) if t is None else _row_strides(t, name)
+    return out
 
 
 def residual_norm(x, y, gate=None, weight=None, bias=None, post_weight=None, kind="layer", post=None, eps=1e-6, residual_scale=1.0, weight_offset=0.0, post_offset=0.0,
@@ -330,16 +358,17 @@ def residual_norm(x, y, gate=None, weight=None, bias=None, post_weight=None, kin
     kind: the norm of r, post: the norm of y, "layer" or "rms" (post None: none).  gate, weight, bias: [C], or [B, C] for x [B, N, C], post_weight [C], of one dtype; each may be
     None.  x (and r) and y (and h): bf16 or fp32, rows at any stride, not x in bf16 beside y in fp32.  out: (r, h) to write to; r may be x and h may be y.  Returns (r, h), or (r, h, stats)
     with save_stats (for residual_norm_backward)."""
-    kind_code, post_code = _norm_kinds(kind, post)
-    dtype, stream_dtype = _residual_tensors(x, y)
-    groups, rows, C = _rows(x)
+    kind_code, post_code, dtype, stream_dtype, groups, rows, C = _residual_numbers(x, y, kind, post)
     gate_per_group, per_group, wcode = _residual_vectors(x, gate, weight, bias, post_weight, post)
     r, h = (_new_like(x), _new_like(y)) if out is None else out
     _on_device(x, y, gate, weight, bias, post_weight, r, h)
-    if r.shape != x.shape or r.dtype != x.dtype or h.shape != y.shape or h.dtype != y.dtype:
-        _refuse("out must have the shapes and dtypes of x and y", CLEAR_ERR_MISMATCH)
+    if out is None and x.is_contiguous() and y.is_contiguous():
+        strides = _Strides8(*(rows * C if x.dim() == 3 else 0, C) * 4)
+    else:
+        if r.shape != x.shape or r.dtype != x.dtype or h.shape != y.shape or h.dtype != y.dtype:
+            _refuse("out must have the shapes and dtypes of x and y", CLEAR_ERR_MISMATCH)
+        strides = _Strides8(*_strides_of((("x", x), ("y", y), ("r", r), ("h", h))))
     stats = torch.empty((4 if post_code else 2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if save_stats else None
-    strides = _Strides8(*_row_strides(x, "x"), *_row_strides(y, "y"), *_row_strides(r, "r"), *_row_strides(h, "h"))
     _call("clear_block_residual_norm", x.device, stream, x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(weight), _ptr(bias), _ptr(post_weight), r.data_ptr(), h.data_ptr(), _ptr(stats),
           groups, rows, C, strides, gate_per_group, per_group, kind_code, post_code, eps, residual_scale, weight_offset, post_offset, dtype, stream_dtype, wcode)
     if out is not None:
@@ -351,9 +380,7 @@ def residual_norm_backward(dr, dh, x, y, gate, weight, bias, post_weight, stats,
                            need=(True,) * 6, stream=None):
     """clear_block_residual_norm_backward: (dx, dy, d_gate, d_weight, d_bias, d_post_weight) for what residual_norm(..., save_stats=True) was called with; None for a vector that is
     None and where `need` says so.  dr: the gradient of r, or None where nothing came back through it."""
-    kind_code, post_code = _norm_kinds(kind, post)
-    dtype, stream_dtype = _residual_tensors(x, y)
-    groups, rows, C = _rows(x)
+    kind_code, post_code, dtype, stream_dtype, groups, rows, C = _residual_numbers(x, y, kind, post)
     gate_per_group, per_group, wcode = _residual_vectors(x, gate, weight, bias, post_weight, post)
     _on_device(x, y, dr, dh, gate, weight, bias, post_weight, stats)
     if dh.shape != y.shape or dh.dtype != y.dtype or (dr is not None and (dr.shape != x.shape or dr.dtype != x.dtype)):
@@ -369,9 +396,7 @@ def residual_norm_backward(dr, dh, x, y, gate, weight, bias, post_weight, stats,
         if floats < 0:
             _check(CLEAR_ERR_UNSUPPORTED)
         ws = torch.empty(max(1, floats), dtype=torch.float32, device=x.device)
-    strides = []
-    for t, name in ((dr, "dr"), (dh, "dh"), (x, "x"), (y, "y"), (grads[0], "dx"), (grads[1], "dy")):
-        strides += _row_strides(t, name) if t is not None else (0, 0)
+    strides = _strides_of((("dr", dr), ("dh", dh), ("x", x), ("y", y), ("dx", grads[0]), ("dy", grads[1])))
     s = _call("clear_block_residual_norm_backward", x.device, stream, _ptr(dr), dh.data_ptr(), x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(weight), _ptr(post_weight),
               stats.data_ptr(), *map(_ptr, grads), groups, rows, C, _Strides12(*strides), gate_per_group, per_group, kind_code, post_code, residual_scale, weight_offset,
               post_offset, dtype, stream_dtype, wcode, _ptr(ws))
@@ -580,24 +605,26 @@ def adamw_decode(m, m_scale, v, v_scale, stream=None):
 # ---- norm and clipping of gradients ---------------------------------------------------------------------------------------------
 
 def _grad_table(grads):
-    """Descriptors (rows of clear_block_grad's three words) of the gradients that are there, with the device they are on."""
+    """Descriptors (rows of clear_block_grad's three words) of the gradients that are there, these, and the first of them."""
     have = [g for g in grads if g is not None]
     if not have:
         _refuse("there must be a gradient")
-    device = have[0].device
-    if not have[0].is_cuda:
+    first = have[0]
+    if not first.is_cuda:
         _refuse("tensors must be device tensors")
-    if set(map(_device_of, have)) != {device.index}:
+    if set(map(_device_of, have)) != {first.get_device()}:
         _refuse("gradients must be on one device")
     if not all(map(_contiguous, have)):
         _refuse("gradients must be contiguous")
-    dtypes = set(map(_dtype_of, have))
-    codes = {t: ca._dtype_code(next(g for g in have if g.dtype == t)) for t in dtypes}
-    table = np.zeros((len(have), 3), dtype=np.int64)
+    table = np.empty((len(have), 3), dtype=np.int64)
     table[:, 0] = list(map(_ptr_of, have))
     table[:, 1] = list(map(_numel, have))
-    table[:, 2] = next(iter(codes.values())) if len(codes) == 1 else [codes[g.dtype] for g in have]
-    return table, have, device
+    dtypes = list(map(_dtype_of, have))
+    if dtypes.count(first.dtype) == len(dtypes):
+        table[:, 2] = _code(first)
+    else:
+        table[:, 2] = list(map(_code, have))
+    return table, have, first
 
 
 def _grad_kind(norm_type):
@@ -606,62 +633,46 @@ def _grad_kind(norm_type):
     return CLEAR_GRAD_NORM_2 if norm_type == 2 else CLEAR_GRAD_NORM_MAX
 
 
-def _launch_norm(table, device, kind, max_norm, grad_scale, stream):
-    """(norm, factor), both fp32 scalars on the device; factor None without a max_norm."""
-    L = _lib or lib()
-    size = L.clear_block_grad_norm_workspace(len(table), table.ctypes.data)
+def _launch_norm(name, grads, norm_type, max_norm, grad_scale, stream, factor):
+    """The C function `name` on the gradients; (norm, the factor if asked for, the gradients that are there)."""
+    kind = _grad_kind(norm_type)
+    table, have, first = _grad_table(grads)
+    device = first.device
+    _check_scale(grad_scale, device)
+    at = table.ctypes.data
+    size = (_lib or lib()).clear_block_grad_norm_workspace(len(have), at)
     if size < 0:
         _check(CLEAR_ERR_UNSUPPORTED)
-    out = torch.empty(2, dtype=torch.float32, device=device)
-    ws = torch.empty(max(1, size // 8), dtype=torch.float64, device=device)
-    norm, factor = out.unbind(0)
-    s = _call("clear_block_grad_norm", device, stream, len(table), table.ctypes.data, kind, 0.0 if max_norm is None else max_norm, _ptr(grad_scale), norm.data_ptr(),
-              None if max_norm is None else factor.data_ptr(), ws.data_ptr())
+    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)
+    norm, factor, ws = new((), torch.float32), new((), torch.float32) if factor else None, new(size // 8, torch.float64)
+    s = _call(name, device, stream, len(have), at, kind, 0.0 if max_norm is None else max_norm, _ptr(grad_scale), norm.data_ptr(), _ptr(factor), ws.data_ptr())
     if stream is not None:
         _record(ws, s)
-    return norm, None if max_norm is None else factor
+    return norm, factor, have
 
 
 def grad_norm(grads, norm_type=2.0, max_norm=None, grad_scale=None, stream=None):
     """clear_block_grad_norm: the norm of all gradients together (a list of contiguous bf16 and fp32 tensors; None is skipped), as an fp32 scalar on their device: nothing waits for
     it.  norm_type: 2 or math.inf.  grad_scale: an fp32 device scalar that the gradients are multiplied by (the inverse of a loss's scale).  With max_norm: (norm, factor), the factor
     grad_scale * min(1, max_norm / norm) being what adamw_step takes as its grad_scale."""
-    kind = _grad_kind(norm_type)
-    table, _, device = _grad_table(grads)
-    _check_scale(grad_scale, device)
-    norm, factor = _launch_norm(table, device, kind, max_norm, grad_scale, stream)
+    norm, factor, _ = _launch_norm("clear_block_grad_norm", grads, norm_type, max_norm, grad_scale, stream, max_norm is not None)
     return norm if max_norm is None else (norm, factor)
 
 
-def _refuse_shared(table):
-    size = np.where(table[:, 2] == CLEAR_F32, 4, 2) * table[:, 1]
-    at = table[size > 0, 0]
-    order = np.argsort(at)
-    ends = at[order] + size[size > 0][order]
-    if np.any(ends[:-1] > at[order][1:]):
-        _refuse("gradients share memory")
-
-
 def clip_grads(grads, max_norm, norm_type=2.0, grad_scale=None, stream=None):
-    """Scales all gradients in place by grad_scale * min(1, max_norm / norm) and returns their norm, that of grad_scale times them (an fp32 scalar on their device): grad_norm, then clear_block_grad_scale."""
-    kind = _grad_kind(norm_type)
-    table, have, device = _grad_table(grads)
-    _refuse_shared(table)
-    _check_scale(grad_scale, device)
-    norm, factor = _launch_norm(table, device, kind, max_norm, grad_scale, stream)
-    _call("clear_block_grad_scale", device, stream, len(table), table.ctypes.data, factor.data_ptr())
+    """clear_block_grad_clip: scales all gradients in place by grad_scale * min(1, max_norm / norm) and returns their norm, that of grad_scale times them (an fp32 scalar on their device)."""
+    norm, _, have = _launch_norm("clear_block_grad_clip", grads, norm_type, max_norm, grad_scale, stream, False)
     _changed(have)
     return norm
 
 
 def scale_grads(grads, factor, stream=None):
     """clear_block_grad_scale: every gradient times an fp32 device scalar, in place."""
-    table, have, device = _grad_table(grads)
-    _refuse_shared(table)
+    table, have, first = _grad_table(grads)
     if factor is None:
         _refuse("a factor is needed")
-    _check_scale(factor, device)
-    _call("clear_block_grad_scale", device, stream, len(table), table.ctypes.data, factor.data_ptr())
+    _check_scale(factor, first.device)
+    _call("clear_block_grad_scale", first.device, stream, len(have), table.ctypes.data, factor.data_ptr())
     _changed(have)
 
 
@@ -676,7 +687,7 @@ class MX4(collections.namedtuple("MX4", "codes scales")):
         return MX4(self.codes[first:last], self.scales[:, first:last])
 
 
-def _mx_sizes(rows, C):
+def _mx_groups(C):
     if C % MX_BLOCK or C == 0:
         _refuse("channels must be a multiple of %d" % MX_BLOCK, CLEAR_ERR_UNSUPPORTED)
     return -(-C // MX_GROUP)
@@ -689,45 +700,38 @@ def _mx_operand(t, name):
     codes, scales = t
     if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() < 1:
         _refuse("%s: codes and scales must be uint8" % name)
+    rows, ld = _any_rows(codes, name)
     C = 2 * codes.shape[-1]
-    if codes.dim() == 2 and (codes.shape[0] <= 1 or codes.stride(1) == 1):
-        rows, ld = codes.shape[0], codes.stride(0)
-        if rows == 1 and C > 2 and codes.stride(1) != 1:
-            _refuse("%s: the last axis of codes must be contiguous" % name)
-    elif codes.is_contiguous():
-        rows, ld = codes.numel() // max(1, C // 2), C // 2
-    else:
-        _refuse("%s: the last axis of codes must be contiguous, and more than two axes altogether" % name)
-    groups = _mx_sizes(rows, C)
-    if tuple(scales.shape) != (groups, rows, 8):
+    groups = _mx_groups(C)
+    if scales.shape != (groups, rows, 8):
         _refuse("%s: scales must be [%d, %d, 8]" % (name, groups, rows), CLEAR_ERR_MISMATCH)
-    if rows > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 8)):
+    if rows > 0 and not scales.is_contiguous() and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 8)):
         _refuse("%s: scales must be contiguous within a group" % name)
     return rows, C, ld, scales.stride(0)
 
 
 def _any_rows(t, name):
     """(rows, row stride) of a tensor [..., C] whose leading axes are one axis of evenly spaced rows."""
-    if t.dim() < 1:
+    dims = t.dim()
+    if dims < 1:
         _refuse("%s: a tensor of at least one axis is needed" % name)
-    if t.dim() != 2:
-        if not t.is_contiguous():
-            _refuse("%s: a tensor of %d axes must be contiguous" % (name, t.dim()))
-        t = t.reshape(-1, t.shape[-1])
-    if t.shape[0] == 0:
-        return 0, t.shape[1]
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    C = t.shape[-1]
+    if t.is_contiguous():
+        return (t.shape[0] if dims == 2 else t.numel() // C if C else 0), C
+    if dims != 2:
+        _refuse("%s: a tensor of %d axes must be contiguous" % (name, dims))
+    if C > 1 and t.stride(1) != 1:
         _refuse("%s: the last axis must be contiguous" % name)
-    return t.shape[0], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.shape[0], t.stride(0) if t.shape[0] > 1 else C
 
 
 def mx_quantize(x, stream=None):
     """clear_block_mx_quantize: x [..., C] (bf16 or fp32, C a multiple of 32) to 4 bits with a scale for every 32 channels of a row: an MX4."""
-    dtype = ca._dtype_code(x)
+    dtype = _code(x)
     _on_device(x)
     rows, ld = _any_rows(x, "x")
     C = x.shape[-1]
-    groups = _mx_sizes(rows, C)
+    groups = _mx_groups(C)
     codes = torch.empty(x.shape[:-1] + (C // 2,), dtype=torch.uint8, device=x.device)
     scales = torch.empty((groups, rows, 8), dtype=torch.uint8, device=x.device)
     _call("clear_block_mx_quantize", x.device, stream, x.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, C, ld, C // 2, 8 * rows, dtype)
@@ -739,7 +743,7 @@ def mx_dequantize(t, dtype=torch.bfloat16, stream=None):
     rows, C, ld, ld_scales = _mx_operand(t, "t")
     _on_device(*t)
     y = torch.empty(t[0].shape[:-1] + (C,), dtype=dtype, device=t[0].device)
-    _call("clear_block_mx_dequantize", y.device, stream, t[0].data_ptr(), t[1].data_ptr(), y.data_ptr(), rows, C, ld, ld_scales, C, ca._dtype_code(y))
+    _call("clear_block_mx_dequantize", y.device, stream, t[0].data_ptr(), t[1].data_ptr(), y.data_ptr(), rows, C, ld, ld_scales, C, _code(y))
     return y
 
 
@@ -755,27 +759,27 @@ def mx_linear(x, w, bias=None, dtype=None, out=None, stream=None):
         lead, x_code, xp, xsp = x[0].shape[:-1], 0, x[0].data_ptr(), x[1].data_ptr()
     else:
         M, ld_x = _any_rows(x, "x")
-        Cx, ld_xs, lead, x_code, xp, xsp = x.shape[-1], 0, x.shape[:-1], ca._dtype_code(x), x.data_ptr(), None
+        Cx, ld_xs, lead, x_code, xp, xsp = x.shape[-1], 0, x.shape[:-1], _code(x), x.data_ptr(), None
     if Cx != C:
         _refuse("x must be [..., %d]" % C, CLEAR_ERR_MISMATCH)
-    if bias is not None and (tuple(bias.shape) != (F,) or not bias.is_contiguous()):
+    if bias is not None and (bias.shape != (F,) or not bias.is_contiguous()):
         _refuse("bias must be contiguous, [%d]" % F, CLEAR_ERR_MISMATCH)
     device = w[0].device
     if out is None:
         y = torch.empty(tuple(lead) + (F,), dtype=torch.bfloat16 if dtype is None else dtype, device=device)
     else:
         y = out
-        if tuple(y.shape) != tuple(lead) + (F,) or (dtype is not None and y.dtype != dtype):
+        if y.shape != tuple(lead) + (F,) or (dtype is not None and y.dtype != dtype):
             _refuse("out must be %s, of the dtype asked for" % (list(lead) + [F],), CLEAR_ERR_MISMATCH)
     _on_device(w[0], w[1], bias, y, *(x if quantized else (x,)))
     _, ld_y = _any_rows(y, "out")
-    out_code = ca._dtype_code(y)
+    out_code = _code(y)
     size = (_lib or lib()).clear_block_mx_linear_workspace(M, C, F, int(quantized))
     if size < 0:
         _check(CLEAR_ERR_UNSUPPORTED)
     ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     s = _call("clear_block_mx_linear", device, stream, xp, xsp, w[0].data_ptr(), w[1].data_ptr(), _ptr(bias), y.data_ptr(), M, C, F, _Strides5(ld_x, ld_xs, ld_w, ld_ws, ld_y),
-              x_code, 0 if bias is None else ca._dtype_code(bias), out_code, _ptr(ws))
+              x_code, 0 if bias is None else _code(bias), out_code, _ptr(ws))
     if ws is not None and stream is not None:
         _record(ws, s)
     if out is not None:

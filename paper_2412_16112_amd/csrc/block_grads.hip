@@ -24,7 +24,7 @@ struct Launch {
     unsigned char wide[kTensors];  // fp32
     int count;
 };
-static_assert(sizeof(Launch) + 64 <= 4096, "the arguments of a launch are at most 4 KB");
+static_assert(sizeof(Launch) + 96 <= 4096, "the arguments of a launch are at most 4 KB");
 
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((ext_vector_type(4), aligned(2))) unsigned u32x4_any2;
@@ -140,26 +140,31 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const Launch l, dou
     if (threadIdx.x == 0) partials[blockIdx.x] = K::value(part[0]);
 }
 
-// One workgroup: the norm and the factor from the partials.
-__global__ void __launch_bounds__(1024) grad_factor_kernel(const double* partials, long long n, GradFactor f)
+// The factor from the partials, in every thread of a workgroup; `gives`: this one writes it and the norm down.  The order of the sum is the same wherever it is formed.
+__device__ __forceinline__ float factor_of(const double* partials, long long n, const GradFactor& f, bool gives)
 {
-    __shared__ double part[1024];
+    __shared__ double part[kThreads];
     const bool squares = f.kind == CLEAR_GRAD_NORM_2;
     auto join = [&](double a, double b) { return squares ? a + b : a > b || a != a ? a : b; };
     double s = 0;
-    for (long long i = threadIdx.x; i < n; i += 1024) s = join(s, partials[i]);
+#pragma unroll 4
+    for (long long i = threadIdx.x; i < n; i += kThreads) s = join(s, partials[i]);
     part[threadIdx.x] = s;
-    for (int half = 512; half > 0; half /= 2) {
+    for (int half = kThreads / 2; half > 0; half /= 2) {
         __syncthreads();
         if ((int)threadIdx.x < half) part[threadIdx.x] = join(part[threadIdx.x], part[threadIdx.x + half]);
     }
-    if (threadIdx.x == 0) {
-        const double unscale = f.unscale ? (double)*f.unscale : 1.0;
-        const double norm = (squares ? sqrt(part[0]) : part[0]) * fabs(unscale);
+    __syncthreads();
+    const double unscale = f.unscale ? (double)*f.unscale : 1.0;
+    const double norm = (squares ? sqrt(part[0]) : part[0]) * fabs(unscale);
+    const float factor = (float)(unscale * (norm > f.max_norm ? f.max_norm / norm : norm != norm ? norm : 1.0));
+    if (gives && threadIdx.x == 0) {
         if (f.norm) *f.norm = (float)norm;
-        if (f.factor) *f.factor = (float)(unscale * (norm > f.max_norm ? f.max_norm / norm : norm != norm ? norm : 1.0));
+        if (f.factor) *f.factor = factor;
     }
+    return factor;
 }
+__global__ void __launch_bounds__(kThreads) grad_factor_kernel(const double* partials, long long n, GradFactor f) { factor_of(partials, n, f, true); }
 
 __device__ __forceinline__ unsigned pair_of(float lo, float hi)
 {
@@ -193,14 +198,19 @@ __device__ __forceinline__ void scale_chunk(T* p, long long left, float factor)
 }
 
 // A factor of 1 changes nothing: nothing is read.
-__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Launch l, const float* factor)
+__device__ __forceinline__ void scale_all(const Launch& l, float factor)
 {
-    const float f = *factor;
-    if (f == 1.f) return;
+    if (factor == 1.f) return;
     const unsigned chunks = l.first[l.count];
-    for (unsigned chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-        with_chunk(l, chunk, [&](auto* p, long long left, auto full) { scale_chunk<full>(p, left, f); });
-    }
+    for (unsigned chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x)
+        with_chunk(l, chunk, [&](auto* p, long long left, auto full) { scale_chunk<full>(p, left, factor); });
+}
+__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Launch l, const float* factor) { scale_all(l, *factor); }
+// Clipping: every workgroup forms the factor for itself (of at most 16 KB of partials a launch), which a launch of its own and the wait for it would cost more than: 26 small tensors
+// LATER us, clipped by two launches behind the norm's LATER.
+__global__ void __launch_bounds__(kThreads) grad_clip_kernel(const Launch l, const double* partials, long long n, GradFactor f, int gives)
+{
+    scale_all(l, factor_of(partials, n, f, gives && blockIdx.x == 0));
 }
 
 long long chunks_of(const clear_block_grad& t) { return (t.n * (t.dtype == CLEAR_F32 ? 4 : 2) + kChunkBytes - 1) / kChunkBytes; }
@@ -250,22 +260,45 @@ long long grad_norm_partials(int n, const clear_block_grad* tensors)
     return partials;
 }
 
-hipError_t launch_grad_norm(int n, const clear_block_grad* tensors, const GradFactor& f, void* workspace, hipStream_t stream)
+static hipError_t launch_partials(int n, const clear_block_grad* tensors, int kind, void* workspace, hipStream_t stream, long long* partials)
 {
-    long long partials = 0;
-    const hipError_t e = each_launch(n, tensors, [&](const Launch& l, long long chunks) {
+    *partials = 0;
+    return each_launch(n, tensors, [&](const Launch& l, long long chunks) {
         const unsigned blocks = blocks_of(chunks);
-        double* const to = (double*)workspace + partials;
-        partials += blocks;
-        if (f.kind == CLEAR_GRAD_NORM_2)
+        double* const to = (double*)workspace + *partials;
+        *partials += blocks;
+        if (kind == CLEAR_GRAD_NORM_2)
             grad_norm_kernel<Squares><<<dim3(blocks), dim3(kThreads), 0, stream>>>(l, to);
         else
             grad_norm_kernel<Largest><<<dim3(blocks), dim3(kThreads), 0, stream>>>(l, to);
         return hipGetLastError();
     });
+}
+
+hipError_t launch_grad_norm(int n, const clear_block_grad* tensors, const GradFactor& f, void* workspace, hipStream_t stream)
+{
+    long long partials;
+    const hipError_t e = launch_partials(n, tensors, f.kind, workspace, stream, &partials);
     if (e != hipSuccess) return e;
-    grad_factor_kernel<<<dim3(1), dim3(1024), 0, stream>>>((const double*)workspace, partials, f);
+    grad_factor_kernel<<<dim3(1), dim3(kThreads), 0, stream>>>((const double*)workspace, partials, f);
     return hipGetLastError();
+}
+
+hipError_t launch_grad_clip(int n, const clear_block_grad* tensors, const GradFactor& f, void* workspace, hipStream_t stream)
+{
+    long long partials;
+    hipError_t e = launch_partials(n, tensors, f.kind, workspace, stream, &partials);
+    if (e != hipSuccess) return e;
+    if (partials == 0) {  // nothing to clip: the norm is 0
+        grad_factor_kernel<<<dim3(1), dim3(kThreads), 0, stream>>>((const double*)workspace, partials, f);
+        return hipGetLastError();
+    }
+    int gives = 1;
+    return each_launch(n, tensors, [&](const Launch& l, long long chunks) {
+        grad_clip_kernel<<<dim3(blocks_of(chunks)), dim3(kThreads), 0, stream>>>(l, (const double*)workspace, partials, f, gives);
+        gives = 0;
+        return hipGetLastError();
+    });
 }
 
 hipError_t launch_grad_scale(int n, const clear_block_grad* tensors, const float* factor, hipStream_t stream)

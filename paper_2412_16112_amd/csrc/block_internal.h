@@ -90,6 +90,7 @@ struct GradFactor {
     float *norm, *factor;
 };
 hipError_t launch_grad_norm(int n, const clear_block_grad* tensors, const GradFactor& f, void* workspace, hipStream_t stream);
+hipError_t launch_grad_clip(int n, const clear_block_grad* tensors, const GradFactor& f, void* workspace, hipStream_t stream);
 hipError_t launch_grad_scale(int n, const clear_block_grad* tensors, const float* factor, hipStream_t stream);
 long long grad_norm_partials(int n, const clear_block_grad* tensors);
 

@@ -1,5 +1,8 @@
 // C ABI of the gated residual with its norms, the norm of gradients and the operands in 4 bits (include/clear_block.h): argument checks and launches.
+#include <algorithm>
 #include <cmath>
+#include <utility>
+#include <vector>
 
 #include "block_checks.h"
 #include "block_internal.h"
@@ -160,24 +163,58 @@ long long clear_block_grad_norm_workspace(int n_tensors, const clear_block_grad*
     return check_grads(n_tensors, tensors) == CLEAR_OK ? grad_norm_partials(n_tensors, tensors) * 8 : -1;
 }
 
-int clear_block_grad_norm(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, const float* unscale, float* norm, float* factor, void* workspace, void* stream)
+namespace {
+
+int check_norm(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, bool factor, const float* unscale, const float* norm, const float* factor_out, const void* workspace)
 {
     const int rc = check_grads(n_tensors, tensors);
     if (rc != CLEAR_OK) return rc;
     if (kind != CLEAR_GRAD_NORM_2 && kind != CLEAR_GRAD_NORM_MAX) return invalid("kind must be CLEAR_GRAD_NORM_2 or CLEAR_GRAD_NORM_MAX");
-    if (!norm && !factor) return invalid("norm or factor must be non-NULL");
     if (factor && !(max_norm >= 0)) return invalid("max_norm must be >= 0");
-    if (!aligned(unscale, 4) || !aligned(norm, 4) || !aligned(factor, 4) || !aligned(workspace, 8)) return invalid("pointers must be aligned to their elements");
+    if (!aligned(unscale, 4) || !aligned(norm, 4) || !aligned(factor_out, 4) || !aligned(workspace, 8)) return invalid("pointers must be aligned to their elements");
     if (!workspace && grad_norm_partials(n_tensors, tensors) > 0) return invalid("workspace must be non-NULL");
-    GradFactor f;
-    f.kind = kind, f.max_norm = max_norm, f.unscale = unscale, f.norm = norm, f.factor = factor;
+    return CLEAR_OK;
+}
+// Whether no two tensors, which are written, share memory.
+int check_apart(int n_tensors, const clear_block_grad* tensors) noexcept
+{
+    try {
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        spans.reserve(n_tensors);
+        for (int i = 0; i < n_tensors; ++i)
+            if (tensors[i].data && tensors[i].n > 0) spans.emplace_back((uintptr_t)tensors[i].data, (uintptr_t)tensors[i].data + (uintptr_t)tensors[i].n * size_of(tensors[i].dtype));
+        std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i)
+            if (spans[i].first < spans[i - 1].second) return invalid("gradients share memory");
+    } catch (...) {
+        return fail(CLEAR_ERR_ALLOC, "out of host memory");
+    }
+    return CLEAR_OK;
+}
+
+}  // namespace
+
+int clear_block_grad_norm(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, const float* unscale, float* norm, float* factor, void* workspace, void* stream)
+{
+    const int rc = check_norm(n_tensors, tensors, kind, max_norm, factor != nullptr, unscale, norm, factor, workspace);
+    if (rc != CLEAR_OK) return rc;
+    if (!norm && !factor) return invalid("norm or factor must be non-NULL");
+    const GradFactor f = {kind, max_norm, unscale, norm, factor};
     return launched(launch_grad_norm(n_tensors, tensors, f, workspace, (hipStream_t)stream), "gradient norm launch failed: ");
+}
+
+int clear_block_grad_clip(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, const float* unscale, float* norm, float* factor, void* workspace, void* stream)
+{
+    int rc = check_norm(n_tensors, tensors, kind, max_norm, true, unscale, norm, factor, workspace);
+    if (rc != CLEAR_OK || (rc = check_apart(n_tensors, tensors)) != CLEAR_OK) return rc;
+    const GradFactor f = {kind, max_norm, unscale, norm, factor};
+    return launched(launch_grad_clip(n_tensors, tensors, f, workspace, (hipStream_t)stream), "gradient clipping launch failed: ");
 }
 
 int clear_block_grad_scale(int n_tensors, const clear_block_grad* tensors, const float* factor, void* stream)
 {
-    const int rc = check_grads(n_tensors, tensors);
-    if (rc != CLEAR_OK) return rc;
+    int rc = check_grads(n_tensors, tensors);
+    if (rc != CLEAR_OK || (rc = check_apart(n_tensors, tensors)) != CLEAR_OK) return rc;
     if (!factor || !aligned(factor, 4)) return invalid("factor must be a pointer to a float");
     return launched(launch_grad_scale(n_tensors, tensors, factor, (hipStream_t)stream), "gradient scaling launch failed: ");
 }

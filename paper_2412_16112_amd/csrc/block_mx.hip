@@ -617,21 +617,33 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     return hipGetLastError();
 }
 
-enum TileShape { kFew, kLarge, kPair, kDeep };
+// Form, tile shape and number of parts that the contraction is split into, by the time that they are expected to take with weights from memory: rounds of workgroups over the 256 CUs, each
+// of a part's steps (256 of the contraction) and of what a tile costs beside.  The constants, in us, were fitted to 800 timings at 8 to 4608 tokens and five shapes of 1536 x 4096 to
+// 4096 x 11264: the chosen form takes 1.3 % longer than the best of them on average, at most 17 %.  A tile of 256 x 256 alone on its CU takes 1.55 us a step, one of 128 x 128 with four stages in flight 0.58, two of
+// 128 x 128 with two stages each 1.07 (1000 tokens at 9728 x 2432: 64, 27 and 41 us, 4608 at 2432 x 9728: 65, 94 and 76).
+enum TileShape { kFew, kLarge, kPair, kDeep };  // few tokens; 256 x 256; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
 struct Plan {
     TileShape shape;
     int parts;
 };
 Plan plan_of(long long tokens, int channels, int outputs)
 {
-    if (tokens <= 64) return {kFew, 1};
     const auto up = [](long long x, long long by) { return (x + by - 1) / by; };
-    const long long large = up(outputs, 256) * up(tokens, 256), small = up(outputs, 128) * up(tokens, 128);
-    if (large >= 192) return {kLarge, 1};
-    const int steps = groups_of(channels);
-    int parts = 1;
-    while (small * parts * 2 <= 256 && steps >= 4 * parts * 2 && parts < 8) parts *= 2;
-    return {small * parts <= 256 ? kDeep : kPair, parts};
+    // (few tokens, here and in tiles: 8 at 2432 x 9728 7.1 and 10.5, at 4096 x 11264 9.8 and 13.0; 32 at 4096 x 4096 7.1 and 10.8, at 2432 x 9728 12.0 and 11.1, at 4096 x 11264 18.6 and 13.4)
+    if (tokens <= 16 || (tokens <= 32 && (long long)channels * outputs <= 1 << 24)) return {kFew, 1};
+    const long long steps = groups_of(channels), large = up(outputs, 256) * up(tokens, 256), small = up(outputs, 128) * up(tokens, 128);
+    Plan best = {kLarge, 1};
+    double best_us = 0;
+    for (int parts = 1; parts <= 8 && (parts == 1 || steps >= 3 * parts); ++parts) {
+        const double each = (double)up(steps, parts);
+        // (the parts are written and read once more)
+        const double join = parts == 1 ? 0 : 3 + (2.2 * parts + 0.5) * tokens * outputs * 4 / 4e6;
+        const double us[3] = {up(large * parts, 256) * (each * 1.55 + 6) + join, (small * parts <= 256 ? each + 2.5 : up(small * parts, 512) * (each * 1.07 + 4.5)) + join,
+                              up(small * parts, 256) * (each * 0.58 + 4.4) + join};
+        for (int i = 0; i < 3; ++i)
+            if (best_us == 0 || us[i] < best_us) best_us = us[i], best = {(TileShape)(kLarge + i), parts};
+    }
+    return best;
 }
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -712,8 +724,7 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
     case kFew: {
         const dim3 grid((a.outputs + 15) / 16), block(64 * kFewWaves);
         if (a.tokens <= 16) mx_few_kernel<1><<<grid, block, 0, stream>>>(t);
-        else if (a.tokens <= 32) mx_few_kernel<2><<<grid, block, 0, stream>>>(t);
-        else mx_few_kernel<4><<<grid, block, 0, stream>>>(t);
+        else mx_few_kernel<2><<<grid, block, 0, stream>>>(t);
         return hipGetLastError();
     }
     case kLarge: return launch_tiles<4, 2, 2, 4, 2>(t, p.parts, stream);
