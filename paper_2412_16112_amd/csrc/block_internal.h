@@ -152,6 +152,11 @@ struct Chunk8;
 template <>
 struct Chunk8<__bf16> {
     bf16x8 v;
+    __device__ __forceinline__ void fill(float x)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (__bf16)x;
+    }
     template <int GAP>
     __device__ __forceinline__ void load(const __bf16* p, int n, RowForm form)
     {
@@ -205,6 +210,7 @@ struct Chunk8<__bf16> {
 template <>
 struct Chunk8<float> {
     f32x4 lo, hi;
+    __device__ __forceinline__ void fill(float x) { lo = hi = f32x4{x, x, x, x}; }
     template <int GAP>
     __device__ __forceinline__ void load(const float* p, int n, RowForm form)
     {

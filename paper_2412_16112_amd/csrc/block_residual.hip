@@ -26,7 +26,24 @@ __host__ __device__ constexpr bool sums_in_lds(int team, bool wide) { return bac
 template <typename T, typename TS, int TEAM>
 using RowLayout = Layout<std::conditional_t<sizeof(T) == 4 && sizeof(TS) == 4, float, __bf16>, TEAM, 1, false>;
 
-template <typename T, typename TS, typename TW, int TEAM>
+// A lane's part of a vector, or 1 where there is none (the formulas need no branches then).
+template <int GAP, typename TW>
+__device__ __forceinline__ void load_or_ones(Chunk8<TW>& to, const TW* p, int n, RowForm form)
+{
+    if (p) to.template load<GAP>(p, n, form);
+    else to.fill(1.f);
+}
+// Whether every lane of this wave has 8 channels (a branch that the whole wave takes).
+template <typename L>
+__device__ __forceinline__ bool whole_wave(int lane, int channels)
+{
+    const int last = lane | 63, n = channels - L::first(last, 0);
+    return __builtin_amdgcn_readfirstlane(n >= L::P::first(4) + (L::GAP == 4 ? 8 : 4));
+}
+template <typename TW>
+__device__ __forceinline__ const TW* vector_of(const void* p, int set, int channels) { return p ? (const TW*)p + (long long)set * channels : nullptr; }
+
+template <typename T, typename TS, typename TW, bool POST, int TEAM>
 __global__ void __launch_bounds__(64 * forward_waves(TEAM)) residual_forward_kernel(ResidualArgs a, long long row_first)
 {
     constexpr int WAVES = forward_waves(TEAM), TEAMS = WAVES / TEAM;
@@ -45,21 +62,26 @@ __global__ void __launch_bounds__(64 * forward_waves(TEAM)) residual_forward_ker
     vy.template load<L::GAP>((const T*)a.y + g * a.st[2] + r * a.st[3] + c, n, form);
     vx.template load<L::GAP>((const TS*)a.x + g * a.st[0] + r * a.st[1] + c, n, form);
     Chunk8<TW> cg, cp, cw, cb;  // (asked for here: they arrive while the sums are formed)
-    const TW* const w = a.w ? (const TW*)a.w + (a.per_group ? (long long)g * C : 0) : nullptr;
-    const TW* const b = a.b ? (const TW*)a.b + (a.per_group ? (long long)g * C : 0) : nullptr;
-    if (a.pw) cp.template load<L::GAP>((const TW*)a.pw + c, n, form);
-    if (a.gate) cg.template load<L::GAP>((const TW*)a.gate + (a.gate_per_group ? (long long)g * C : 0) + c, n, form);
-    if (w) cw.template load<L::GAP>(w + c, n, form);
+    const TW* const w = vector_of<TW>(a.w, a.per_group ? g : 0, C);
+    const TW* const b = vector_of<TW>(a.b, a.per_group ? g : 0, C);
+    const TW* const gate = vector_of<TW>(a.gate, a.gate_per_group ? g : 0, C);
+    const float offset = w ? a.offset : 0.f, post_offset = a.pw ? a.post_offset : 0.f;
+    if (POST) load_or_ones<L::GAP>(cp, a.pw ? (const TW*)a.pw + c : nullptr, n, form);
+    load_or_ones<L::GAP>(cg, gate ? gate + c : nullptr, n, form);
+    load_or_ones<L::GAP>(cw, w ? w + c : nullptr, n, form);
     if (b) cb.template load<L::GAP>(b + c, n, form);
-    bool own[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) own[j] = L::P::own(j, n, form);
-
+    else cb.fill(0.f);
+    const bool all = whole_wave<L>(lane, C);
     int turn = 0;
     auto sum = [&](auto value) {  // of value(j) over the row's channels
         float s[1] = {0.f};
+        if (all) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += own[j] ? value(j) : 0.f;
+            for (int j = 0; j < 8; ++j) s[0] += value(j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[0] += L::P::own(j, n, form) ? value(j) : 0.f;
+        }
         team_sum<TEAM>(s, slots[turn], wave);
         turn ^= 1;
         return s[0];
@@ -73,22 +95,19 @@ __global__ void __launch_bounds__(64 * forward_waves(TEAM)) residual_forward_ker
     float v[8], mean_y = 0.f, rstd_y = 1.f, mean, rstd;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = vy.get(j);
-    if (a.post != CLEAR_NORM_NONE) {
+    if (POST) {
         size_of_row(v, a.post, &mean_y, &rstd_y);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = (v[j] - mean_y) * rstd_y;
-            if (a.pw) v[j] *= a.post_offset + cp.get(j);
-        }
+        for (int j = 0; j < 8; ++j) v[j] = (v[j] - mean_y) * rstd_y * (post_offset + cp.get(j));
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = a.scale * vx.get(j) + (a.gate ? cg.get(j) * v[j] : v[j]);
+    for (int j = 0; j < 8; ++j) v[j] = a.scale * vx.get(j) + cg.get(j) * v[j];
     size_of_row(v, a.kind, &mean, &rstd);
     if (!live) return;
     if (a.stats && lane == 0) {
         a.stats[row] = mean;
         a.stats[total + row] = rstd;
-        if (a.post != CLEAR_NORM_NONE) {
+        if (POST) {
             a.stats[2 * total + row] = mean_y;
             a.stats[3 * total + row] = rstd_y;
         }
@@ -97,18 +116,14 @@ __global__ void __launch_bounds__(64 * forward_waves(TEAM)) residual_forward_ker
     // (r and h may lie on x and y: what the team's waves read of these has arrived before the sum over r)
     Chunk8<TS>::template store<L::GAP>((TS*)a.r + g * a.st[4] + r * a.st[5] + c, n, form, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        v[j] = (v[j] - mean) * rstd;
-        if (w) v[j] *= a.offset + cw.get(j);
-        if (b) v[j] += cb.get(j);
-    }
+    for (int j = 0; j < 8; ++j) v[j] = (v[j] - mean) * rstd * (offset + cw.get(j)) + cb.get(j);
     Chunk8<T>::template store<L::GAP>((T*)a.h + g * a.st[6] + r * a.st[7] + c, n, form, v);
 }
 
 // Workgroup (p, set) of the grid takes rows p TEAMS + team, then every gridDim.x TEAMS further ones, of the set (a group where anything is a group's own, else everything),
 // writes their dx and dy and adds up in registers what the vectors' gradients are sums of; the teams' sums are added in order and become partial p of the set.
 //     d = dr + norm'(dh (offset + w)),   dx = a d,   dz = gate d,   dy = post'(dz (post_offset + post weight))
-template <typename T, typename TS, typename TW, int TEAM>
+template <typename T, typename TS, typename TW, bool POST, int TEAM>
 __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(TS) > 4)) residual_backward_kernel(ResidualArgs a)
 {
     constexpr bool WIDE = sizeof(T) + sizeof(TS) > 4;
@@ -124,12 +139,15 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
     const long long in_set = sets ? a.rows : (long long)a.groups * a.rows;
     const long long first = sets ? (long long)set * a.rows : 0;
     const long long total = (long long)a.groups * a.rows;
-    const bool layer = a.kind == CLEAR_NORM_LAYER, post = a.post != CLEAR_NORM_NONE, post_layer = a.post == CLEAR_NORM_LAYER;
+    const bool layer = a.kind == CLEAR_NORM_LAYER, post_layer = a.post == CLEAR_NORM_LAYER;
     const float inv_c = 1.f / (float)C;
     Chunk8<TW> cg, cp, cw;
-    if (a.w) cw.template load<L::GAP>((const TW*)a.w + (a.per_group ? (long long)set * C : 0) + c, n, form);
-    if (a.gate) cg.template load<L::GAP>((const TW*)a.gate + (a.gate_per_group ? (long long)set * C : 0) + c, n, form);
-    if (a.pw) cp.template load<L::GAP>((const TW*)a.pw + c, n, form);
+    const TW* const w = vector_of<TW>(a.w, a.per_group ? set : 0, C);
+    const TW* const gate = vector_of<TW>(a.gate, a.gate_per_group ? set : 0, C);
+    const float offset = w ? a.offset : 0.f, post_offset = a.pw ? a.post_offset : 0.f;
+    load_or_ones<L::GAP>(cw, w ? w + c : nullptr, n, form);
+    load_or_ones<L::GAP>(cg, gate ? gate + c : nullptr, n, form);
+    if (POST) load_or_ones<L::GAP>(cp, a.pw ? (const TW*)a.pw + c : nullptr, n, form);
     const shared_float sum = (shared_float)lds;  // (LDS by a pointer of its own address space: as in the layer norm's backward pass)
     float sums[IN_LDS ? 1 : kSums][8];
     // Sum k, which is wanted where `wanted` is not null, and v more.
@@ -144,10 +162,10 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
             for (int j = 0; j < 8; ++j) sums[k][j] += v[j];
         }
     };
-    constexpr std::integral_constant<int, 0> GATE{};
-    constexpr std::integral_constant<int, 1> WEIGHT{};
-    constexpr std::integral_constant<int, 2> BIAS{};
-    constexpr std::integral_constant<int, 3> POST{};
+    constexpr std::integral_constant<int, 0> SUM_GATE{};
+    constexpr std::integral_constant<int, 1> SUM_WEIGHT{};
+    constexpr std::integral_constant<int, 2> SUM_BIAS{};
+    constexpr std::integral_constant<int, 3> SUM_POST{};
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         if constexpr (IN_LDS) {
@@ -165,21 +183,31 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
         int g, r;
         bool live;
     };
+    // (Where the tensors lie is read from the kernel's arguments again for every row: kept, it would take more scalar registers than there are.)
+    typedef const __attribute__((address_space(4))) ResidualArgs* args_ptr;
+    auto args_anew = [] {
+        args_ptr p = (args_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(p));
+        return p;
+    };
     auto fetch = [&](long long base, Row* to) {  // (a row that is not there: the set's first, with gradients of 0)
+        const args_ptr q = args_anew();
         to->live = base + team < in_set;
         const long long row = first + (to->live ? base + team : 0);
-        const int g = (int)row / a.rows, r = (int)row - g * a.rows;
+        const int g = (int)row / q->rows, r = (int)row - g * q->rows;
         to->g = g, to->r = r;
-        to->mean = a.stats[row];
-        to->rstd = a.stats[total + row];
-        to->mean_y = post ? a.stats[2 * total + row] : 0.f;
-        to->rstd_y = post ? a.stats[3 * total + row] : 1.f;
+        to->mean = q->stats[row];
+        to->rstd = q->stats[total + row];
+        if (POST) {
+            to->mean_y = q->stats[2 * total + row];
+            to->rstd_y = q->stats[3 * total + row];
+        }
         const int m = to->live ? n : 0;
         const RowForm f = to->live ? form : RowForm{false, false};
-        to->x.template load<L::GAP>((const TS*)a.x + g * a.st[4] + r * a.st[5] + c, n, form);
-        to->y.template load<L::GAP>((const T*)a.y + g * a.st[6] + r * a.st[7] + c, n, form);
-        to->dh.template load<L::GAP>((const T*)a.dh + g * a.st[2] + r * a.st[3] + c, m, f);
-        to->dr.template load<L::GAP>((const TS*)a.dr + g * a.st[0] + r * a.st[1] + c, a.dr ? m : 0, a.dr ? f : RowForm{false, false});
+        to->x.template load<L::GAP>((const TS*)q->x + g * q->st[4] + r * q->st[5] + c, n, form);
+        to->y.template load<L::GAP>((const T*)q->y + g * q->st[6] + r * q->st[7] + c, n, form);
+        to->dh.template load<L::GAP>((const T*)q->dh + g * q->st[2] + r * q->st[3] + c, m, f);
+        to->dr.template load<L::GAP>((const TS*)q->dr + g * q->st[0] + r * q->st[1] + c, q->dr ? m : 0, q->dr ? f : RowForm{false, false});
     };
     constexpr bool AHEAD = WIDE ? !IN_LDS : TEAM < 16;  // the next row's loads are under way while a row is worked on, where there are registers for it
     Row now, next;
@@ -197,10 +225,10 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
         const bool live = now.live;
         // of element j: the sublayer's output in its unit form, as it goes to the gate, and the sum in its unit form
         auto unit_y = [&](int j) { return (now.y.get(j) - mean_y) * rstd_y; };
-        auto post_w = [&](int j) { return a.pw ? a.post_offset + cp.get(j) : 1.f; };
-        auto out_y = [&](int j) { return post ? unit_y(j) * post_w(j) : now.y.get(j); };
-        auto unit = [&](int j) { return (a.scale * now.x.get(j) + (a.gate ? cg.get(j) * out_y(j) : out_y(j)) - mean) * rstd; };
-        auto grad = [&](int j) { return a.w ? now.dh.get(j) * (a.offset + cw.get(j)) : now.dh.get(j); };
+        auto post_w = [&](int j) { return post_offset + cp.get(j); };
+        auto out_y = [&](int j) { return POST ? unit_y(j) * post_w(j) : now.y.get(j); };
+        auto unit = [&](int j) { return (a.scale * now.x.get(j) + cg.get(j) * out_y(j) - mean) * rstd; };
+        auto grad = [&](int j) { return now.dh.get(j) * (offset + cw.get(j)); };
         float s[2] = {0.f, 0.f}, h[8], v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -212,10 +240,10 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
         if (live) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = now.dh.get(j) * h[j];
-            add(WEIGHT, a.dw, v);
+            add(SUM_WEIGHT, a.dw, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = now.dh.get(j);
-            add(BIAS, a.db, v);
+            add(SUM_BIAS, a.db, v);
         }
         if (!a.rows_out) continue;  // (weight and bias alone)
         team_sum<TEAM>(s, slots[turn], wave);
@@ -226,12 +254,13 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
         for (int j = 0; j < 8; ++j) {
             d[j] = now.dr.get(j) + rstd * (grad(j) - s0 - h[j] * s1);
             v[j] = d[j] * out_y(j);
-            h[j] = a.gate ? d[j] * cg.get(j) : d[j];  // dz
+            h[j] = d[j] * cg.get(j);  // dz
             d[j] *= a.scale;
         }
-        if (live) add(GATE, a.dgate, v);
-        if (live && c < C && a.dx) Chunk8<TS>::template store<L::GAP>((TS*)a.dx + now.g * a.st[8] + now.r * a.st[9] + c, n, form, d);
-        if (post) {
+        if (live) add(SUM_GATE, a.dgate, v);
+        const args_ptr q = args_anew();
+        if (live && c < C && q->dx) Chunk8<TS>::template store<L::GAP>((TS*)q->dx + now.g * q->st[8] + now.r * q->st[9] + c, n, form, d);
+        if (POST) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float u = unit_y(j), dz = L::P::own(j, n, form) ? h[j] : 0.f;
@@ -240,14 +269,14 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
                 t[0] += h[j];
                 t[1] += h[j] * u;
             }
-            if (live) add(POST, a.dpw, v);
+            if (live) add(SUM_POST, a.dpw, v);
             team_sum<TEAM>(t, slots[turn], wave);
             turn ^= 1;
             const float t0 = post_layer ? t[0] * inv_c : 0.f, t1 = t[1] * inv_c;
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = rstd_y * (h[j] - t0 - unit_y(j) * t1);
         }
-        if (live && c < C && a.dy) Chunk8<T>::template store<L::GAP>((T*)a.dy + now.g * a.st[10] + now.r * a.st[11] + c, n, form, h);
+        if (live && c < C && q->dy) Chunk8<T>::template store<L::GAP>((T*)q->dy + now.g * q->st[10] + now.r * q->st[11] + c, n, form, h);
     }
     const int wide = padded(C);
     float* out = a.ws + ((long long)set * gridDim.x + blockIdx.x) * a.sums * wide;
@@ -295,10 +324,10 @@ __global__ void __launch_bounds__(64 * backward_waves(TEAM, sizeof(T) + sizeof(T
         }
         out += wide;
     };
-    give_sum(a.dgate, mine[GATE]);
-    give_sum(a.dw, mine[WEIGHT]);
-    give_sum(a.db, mine[BIAS]);
-    give_sum(a.dpw, mine[POST]);
+    give_sum(a.dgate, mine[SUM_GATE]);
+    give_sum(a.dw, mine[SUM_WEIGHT]);
+    give_sum(a.db, mine[SUM_BIAS]);
+    give_sum(a.dpw, mine[SUM_POST]);
 }
 
 struct Joined {
@@ -359,7 +388,7 @@ void with_team(int team, F&& call)
     }
 }
 
-template <typename T, typename TS, typename TW>
+template <typename T, typename TS, typename TW, bool POST>
 hipError_t forward(const ResidualArgs& a, hipStream_t stream)
 {
     hipError_t e = hipSuccess;
@@ -369,14 +398,14 @@ hipError_t forward(const ResidualArgs& a, hipStream_t stream)
         const long long rows = (long long)a.groups * a.rows;
         for (long long first = 0; first < rows && e == hipSuccess; first += most * teams) {
             const long long blocks = std::min(most, (rows - first + teams - 1) / teams);
-            residual_forward_kernel<T, TS, TW, TEAM><<<dim3((unsigned)blocks), dim3(threads), 0, stream>>>(a, first);
+            residual_forward_kernel<T, TS, TW, POST, TEAM><<<dim3((unsigned)blocks), dim3(threads), 0, stream>>>(a, first);
             e = hipGetLastError();
         }
     });
     return e;
 }
 
-template <typename T, typename TS, typename TW>
+template <typename T, typename TS, typename TW, bool POST>
 hipError_t backward(ResidualArgs a, hipStream_t stream)
 {
     const int sets = a.per_group || a.gate_per_group ? a.groups : 1;
@@ -402,11 +431,11 @@ hipError_t backward(ResidualArgs a, hipStream_t stream)
             if constexpr (sums_in_lds(TEAM, WIDE)) {
                 constexpr size_t all = 64 * waves * kSums * 32;  // (at most 128 KB)
                 static LdsLimit limit;
-                e = limit.ensure((const void*)residual_backward_kernel<T, TS, TW, TEAM>, all);
+                e = limit.ensure((const void*)residual_backward_kernel<T, TS, TW, POST, TEAM>, all);
                 if (e != hipSuccess) return;
                 lds = all;
             }
-            residual_backward_kernel<T, TS, TW, TEAM><<<dim3(partials, sets), dim3(64 * waves), lds, stream>>>(a);
+            residual_backward_kernel<T, TS, TW, POST, TEAM><<<dim3(partials, sets), dim3(64 * waves), lds, stream>>>(a);
             e = hipGetLastError();
         });
     }
@@ -440,12 +469,12 @@ int residual_partials(long long groups, long long rows, int channels, long long 
 
 hipError_t launch_residual_forward(const ResidualArgs& a, int dtype, int stream_dtype, int weight_dtype, hipStream_t stream)
 {
-    return with_types(dtype, stream_dtype, weight_dtype, [&](auto t, auto ts, auto tw) { return forward<decltype(t), decltype(ts), decltype(tw)>(a, stream); });
+    return with_types(dtype, stream_dtype, weight_dtype, [&](auto t, auto ts, auto tw) { return a.post ? forward<decltype(t), decltype(ts), decltype(tw), true>(a, stream) : forward<decltype(t), decltype(ts), decltype(tw), false>(a, stream); });
 }
 
 hipError_t launch_residual_backward(const ResidualArgs& a, int dtype, int stream_dtype, int weight_dtype, hipStream_t stream)
 {
-    return with_types(dtype, stream_dtype, weight_dtype, [&](auto t, auto ts, auto tw) { return backward<decltype(t), decltype(ts), decltype(tw)>(a, stream); });
+    return with_types(dtype, stream_dtype, weight_dtype, [&](auto t, auto ts, auto tw) { return a.post ? backward<decltype(t), decltype(ts), decltype(tw), true>(a, stream) : backward<decltype(t), decltype(ts), decltype(tw), false>(a, stream); });
 }
 
 }  // namespace block
