@@ -4,6 +4,7 @@
 // magnitude lies in [4, 8): 2^e, e = max(floor(log2 max |x|) - 2, -127), stored as e + 127; a code is the nearest to x / 2^e, halfway the one whose fraction is 0, and over 6 it is 6.  Scales lie in
 // groups of 8 blocks (256 channels, a stage of the product's contraction): [groups][rows][8], so that a tile's scales of a stage are one piece of memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "block_tiles.h"
 
@@ -21,7 +22,7 @@ int groups_of(int channels) { return (channels + kGroup - 1) / kGroup; }
 // ---- to 4 bits and back ---------------------------------------------------------------------------------------------------
 // Memory-bound.  A lane has 8 channels (4 lanes a block, half a wave a group), kQuantRows rows one after the other; a workgroup the same group of kQuantRows x 8 rows, whose scales are
 // one piece.
-constexpr int kQuantRows = 4;
+constexpr int kQuantRows = 2;
 
 __device__ __forceinline__ unsigned top_of_block(unsigned bits)  // the largest of 4 neighbouring lanes
 {
@@ -30,6 +31,9 @@ __device__ __forceinline__ unsigned top_of_block(unsigned bits)  // the largest 
 }
 // Stored exponent of a block by the bits of its largest magnitude (a NaN's or an infinity's make it 255, which stands for NaN).
 __device__ __forceinline__ int exponent_of(unsigned top) { return top >= 0x7f800000u ? 255 : max((int)(top >> 23) - 2, 0); }
+
+// 2^-(e - 127) of a stored exponent, exact; what it makes too small for a float is far below half of the least code.
+__device__ __forceinline__ float up_of(int e) { return __uint_as_float((unsigned)(254 - min(e, 253)) << 23); }
 
 template <typename T>
 __global__ void __launch_bounds__(256) mx_quantize_kernel(const MxArgs a)
@@ -52,7 +56,7 @@ __global__ void __launch_bounds__(256) mx_quantize_kernel(const MxArgs a)
         for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i].get(j)) & 0x7fffffffu);
         top = top_of_block(top);
         const int e = exponent_of(top);
-        const float up = __uint_as_float((unsigned)(254 - min(e, 253)) << 23);  // 2^-(e - 127), exact; what it makes too small for a float is far below half of the least code
+        const float up = up_of(e);
         unsigned codes = 0;
         float s[8];
 #pragma unroll
@@ -525,44 +529,110 @@ __device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scal
     const i32x8 wide_a = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wide_b = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_a, wide_b, c, 4, 4, S, scale_a, S, scale_b);
 }
-template <int MT>
+// Tokens that come as numbers and are at most kDirect go to 4 bits here: a wave takes the channels of its groups, 4 a lane, and its operands go through LDS.  (A launch of its own for that takes 3 us and
+// as many of the host's: one token at 4 096 x 11 264 LATER us from Python, LATER with it.)
+constexpr int kDirect = 4;
+struct DirectGroup {
+    unsigned short codes[kDirect][64];  // (a lane's 4 codes)
+    unsigned char scales[kDirect][8];
+};
+template <typename T>
+struct FourOf;
+template <>
+struct FourOf<__bf16> {
+    typedef bf16x4_any type;
+};
+template <>
+struct FourOf<float> {
+    typedef f32x4_any type;
+};
+template <typename T>
+__device__ __forceinline__ void direct_group(DirectGroup* to, const T* x, long long ld_x, int tokens, int c, int channels, int lane)
+{
+    f32x4 v[kDirect];
+#pragma unroll
+    for (int m = 0; m < kDirect; ++m)
+        v[m] = m < tokens && c < channels ? __builtin_convertvector(*(const typename FourOf<T>::type*)(x + m * ld_x + c), f32x4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < kDirect; ++m) {
+        if (m >= tokens) break;
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[m][j]) & 0x7fffffffu);
+        top = top_of_block(top);
+        top = max(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x141, 0xf, 0xf, true));  // (the other four lanes of the block's eight)
+        const int e = exponent_of(top);
+        const f32x4 s = v[m] * up_of(e);
+        unsigned codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, s[0], s[1], 1.f, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, s[2], s[3], 1.f, 1);
+        to->codes[m][lane] = e == 255 ? 0 : (unsigned short)codes;
+        if ((lane & 7) == 0) to->scales[m][lane >> 3] = (unsigned char)e;
+    }
+}
+
+// T: of the tokens, or void where they come in 4 bits.
+template <int MT, typename T>
 __global__ void __launch_bounds__(64 * kFewWaves) mx_few_kernel(const TileArgs t)
 {
+    constexpr bool DIRECT = !std::is_void<T>::value;
+    static_assert(!DIRECT || MT == 1);
+    constexpr int AHEAD = 2;  // groups whose loads are in flight together
     __shared__ f32x4 part[kFewWaves][MT][64];
+    __shared__ __attribute__((aligned(16))) DirectGroup direct[DIRECT ? kFewWaves : 1][DIRECT ? AHEAD : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = 2 * (lane >> 4);
     const int f0 = blockIdx.x * 16;
     const int f = min(f0 + (lane & 15), t.rows_a - 1);
     const unsigned char* const w = t.w + f * t.ld_w + block * 16;
     const unsigned char* const ws = t.ws + f * 8LL + block;
     const unsigned char *x[MT], *xs[MT];
+    if (!DIRECT) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const long long token = min((long long)(16 * m + (lane & 15)), t.rows_b - 1);
-        x[m] = t.x + token * t.ld_x + block * 16;
-        xs[m] = t.xs + token * 8 + block;
+        for (int m = 0; m < MT; ++m) {
+            const long long token = min((long long)(16 * m + (lane & 15)), t.rows_b - 1);
+            x[m] = t.x + token * t.ld_x + block * 16;
+            xs[m] = t.xs + token * 8 + block;
+        }
     }
     f32x4 acc[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int groups = (t.depth + kGroup - 1) / kGroup;
-    constexpr int AHEAD = MT > 2 ? 1 : 2;  // groups whose loads are in flight together
     for (int g0 = wave; g0 < groups; g0 += kFewWaves * AHEAD) {
         i32x4 a[AHEAD][2], b[AHEAD][MT][2];
         int sa[AHEAD], sb[AHEAD][MT];
+        const i32x4 zero = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int g = g0 + kFewWaves * i, left = t.depth - g * kGroup - block * 32;  // channels from this lane's first block on
-            const i32x4 zero = {0, 0, 0, 0};
             const int mask = left >= 64 ? 0xffff : left > 0 ? 0xff : 0;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 a[i][k] = left > 32 * k ? *(const i32x4*)(w + (long long)g * (kGroup / 2) + 16 * k) : zero;
+                if (!DIRECT) {
 #pragma unroll
-                for (int m = 0; m < MT; ++m) b[i][m][k] = left > 32 * k ? *(const i32x4*)(x[m] + (long long)g * (kGroup / 2) + 16 * k) : zero;
+                    for (int m = 0; m < MT; ++m) b[i][m][k] = left > 32 * k ? *(const i32x4*)(x[m] + (long long)g * (kGroup / 2) + 16 * k) : zero;
+                }
             }
             sa[i] = left > 0 ? *(const unsigned short*)(ws + g * t.ld_ws) & mask : 0;
+            if (!DIRECT) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) sb[i][m] = left > 0 ? *(const unsigned short*)(xs[m] + g * t.ld_xs) & mask : 0;
+                for (int m = 0; m < MT; ++m) sb[i][m] = left > 0 ? *(const unsigned short*)(xs[m] + g * t.ld_xs) & mask : 0;
+            }
+        }
+        if constexpr (DIRECT) {
+            const int token = lane & 15;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) direct_group<T>(&direct[wave][i], (const T*)t.x, t.ld_x, (int)t.rows_b, (g0 + kFewWaves * i) * kGroup + 4 * lane, t.depth, lane);
+            asm volatile("" ::: "memory");  // (a wave's LDS instructions are executed in order)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const DirectGroup& d = direct[wave][i];
+                const bool in = token < (int)t.rows_b;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) b[i][0][k] = in ? *(const i32x4*)((const unsigned char*)d.codes[token & (kDirect - 1)] + 16 * (block + k)) : zero;
+                sb[i][0] = in ? *(const unsigned short*)(d.scales[token & (kDirect - 1)] + block) : 0;
+            }
+            asm volatile("" ::: "memory");
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
@@ -693,7 +763,7 @@ hipError_t launch_mx_dequantize(const MxArgs& a, int dtype, hipStream_t stream)
 // The tokens in 4 bits, unless they come so, then the parts of a split contraction.
 size_t mx_linear_workspace_bytes(long long tokens, int channels, int outputs, bool quantized)
 {
-    if (tokens == 0) return 0;
+    if (tokens == 0 || (!quantized && tokens <= kDirect)) return 0;
     const int parts = plan_of(tokens, channels, outputs).parts;
     return (quantized ? 0 : codes_bytes(tokens, channels) + scales_bytes(tokens, channels)) + (parts > 1 ? (size_t)parts * tokens * parts_pitch(outputs) * 4 : 0);
 }
@@ -706,6 +776,12 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
     t.bias = a.bias, t.bias_bf16 = a.bias_dtype == CLEAR_BF16;
     t.out = a.y, t.ld_out = a.ld_y, t.out_bf16 = a.out_dtype == CLEAR_BF16;
     t.rows_a = a.outputs, t.rows_b = a.tokens, t.depth = a.channels;
+    const dim3 few_grid((a.outputs + 15) / 16), few_block(64 * kFewWaves);
+    if (!a.xs && a.tokens <= kDirect) {
+        if (a.x_dtype == CLEAR_BF16) mx_few_kernel<1, __bf16><<<few_grid, few_block, 0, stream>>>(t);
+        else mx_few_kernel<1, float><<<few_grid, few_block, 0, stream>>>(t);
+        return hipGetLastError();
+    }
     unsigned char* ws = (unsigned char*)a.workspace;
     if (!a.xs) {
         MxArgs q = {};
@@ -721,12 +797,10 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
     const Plan p = plan_of(a.tokens, a.channels, a.outputs);
     t.parts = (float*)ws, t.ld_parts = parts_pitch(a.outputs);
     switch (p.shape) {
-    case kFew: {
-        const dim3 grid((a.outputs + 15) / 16), block(64 * kFewWaves);
-        if (a.tokens <= 16) mx_few_kernel<1><<<grid, block, 0, stream>>>(t);
-        else mx_few_kernel<2><<<grid, block, 0, stream>>>(t);
+    case kFew:
+        if (a.tokens <= 16) mx_few_kernel<1, void><<<few_grid, few_block, 0, stream>>>(t);
+        else mx_few_kernel<2, void><<<few_grid, few_block, 0, stream>>>(t);
         return hipGetLastError();
-    }
     case kLarge: return launch_tiles<4, 2, 2, 4, 2>(t, p.parts, stream);
     case kPair: return launch_tiles<2, 2, 2, 2, 2>(t, p.parts, stream);
     default: return launch_tiles<2, 2, 2, 2, 4>(t, p.parts, stream);

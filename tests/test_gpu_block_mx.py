@@ -93,7 +93,7 @@ def product(values, w, bias, dtype):
     return want, (wv.shape[1] / 64 + 16) * 2 * ref.FP32 * size + ref.half_step(dtype) * want.abs()
 
 
-SIZES = [(1, 32, 1), (1, 256, 16), (1, 2432, 300), (5, 288, 17), (16, 512, 100), (17, 1056, 40), (33, 768, 65), (64, 2080, 31), (65, 2432, 300), (128, 256, 128), (130, 608, 515), (257, 2400, 777),
+SIZES = [(1, 32, 1), (1, 256, 16), (1, 2432, 300), (2, 96, 33), (3, 8192, 50), (4, 1056, 40), (5, 288, 17), (16, 512, 100), (17, 1056, 40), (33, 768, 65), (64, 2080, 31), (65, 2432, 300), (128, 256, 128), (130, 608, 515), (257, 2400, 777),
          (300, 4096, 256), (100, 8192, 130), (520, 96, 1030), (2100, 512, 3001)]
 
 
