@@ -15,7 +15,7 @@ namespace block {
 namespace {
 
 constexpr int kThreads = 256, kTensors = 160, kLoads = 4, kChunkBytes = kThreads * 16 * kLoads;
-constexpr int kMostBlocks = 2048;  // workgroups of a launch: 8 a CU
+constexpr int kMostBlocks = 1024;  // workgroups of a launch: 4 a CU (113 M bf16 gradients 47 us; 2048 51, 4096 52)
 
 struct Launch {
     void* data[kTensors];
@@ -206,7 +206,7 @@ __device__ __forceinline__ void scale_all(const Launch& l, float factor)
         with_chunk(l, chunk, [&](auto* p, long long left, auto full) { scale_chunk<full>(p, left, factor); });
 }
 __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Launch l, const float* factor) { scale_all(l, *factor); }
-// Clipping: every workgroup forms the factor for itself (of at most 16 KB of partials a launch), which a launch of its own and the wait for it would cost more than: 26 small tensors
+// Clipping: every workgroup forms the factor for itself (of at most 8 KB of partials a launch), which a launch of its own and the wait for it would cost more than: 26 small tensors
 // LATER us, clipped by two launches behind the norm's LATER.
 __global__ void __launch_bounds__(kThreads) grad_clip_kernel(const Launch l, const double* partials, long long n, GradFactor f, int gives)
 {
