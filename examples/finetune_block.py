@@ -2,7 +2,7 @@
 block of its model (arXiv 2412.16112, Sec. 3.3), with every operator of this library that a training step of it meets:
 
     adaptive layer norm -> projections (torch) -> rotary positions of two image axes -> CLEAR local attention
-    -> layer norm -> gated feed-forward projection -> projection (torch) -> loss -> backward -> AdamW, states in 8 bits
+    -> residual with the next layer norm -> gated feed-forward projection -> projection (torch) -> loss -> backward -> AdamW, gradients clipped, states in 8 bits
 
     python examples/finetune_block.py [--grid 32] [--heads 8] [--steps 20] [--radius 4]
 
@@ -15,7 +15,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2412_16112_amd import clear_block as cb  # noqa: E402
-from paper_2412_16112_amd.autograd import clear_attention, gated_ff, layer_norm, rotary  # noqa: E402
+from paper_2412_16112_amd.autograd import clear_attention, gated_ff, layer_norm, residual_norm, rotary  # noqa: E402
 from paper_2412_16112_amd.optim import AdamW  # noqa: E402
 
 HEAD_DIM = 64
@@ -48,8 +48,8 @@ class Block:
         q, k, v = (t.transpose(1, 2) for t in linear(h, "qkv").view(B, N, 3, self.heads, HEAD_DIM).unbind(2))  # [B, H, N, d], as the projection stored them
         q, k = rotary(q, k, self.places[:, None].expand(2, B, N), self.freqs)
         a = clear_attention(q, k, v, self.n_text, self.grid, self.grid, radius)
-        x = x + linear(a.transpose(1, 2).reshape(B, N, width), "out")
-        return x + linear(gated_ff(layer_norm(x, w["scale"], w["shift"]), w["gate"], w["up"]), "down")
+        x, h = residual_norm(x, linear(a.transpose(1, 2).reshape(B, N, width), "out"), weight=w["scale"], bias=w["shift"])
+        return x + linear(gated_ff(h, w["gate"], w["up"]), "down")
 
 
 def finetune(n_text=32, grid=32, heads=8, radius=4, steps=20, lr=1e-3, seed=0, state_bits=8, say=print):
@@ -67,8 +67,7 @@ def finetune(n_text=32, grid=32, heads=8, radius=4, steps=20, lr=1e-3, seed=0, s
         off = (student(x, scale, shift, radius) - want).float()
         loss = off.square().mean() / (want - x).float().square().mean()
         loss.backward()
-        norm = torch.stack([p.grad.float().square().sum() for p in params]).sum().sqrt()
-        opt.step(grad_scale=torch.clamp(1.0 / norm, max=1.0))  # gradients clipped to a norm of 1, without waiting for it
+        opt.step(max_norm=1.0)  # gradients clipped to a norm of 1, without waiting for it
         opt.zero_grad()
         losses.append(loss.detach())
         if say and (step % 5 == 0 or step + 1 == steps):

@@ -1,4 +1,4 @@
-"""torch.autograd entry points for the CLEAR local attention and for the operators around it - rotary, layer_norm, gated_ff -
+"""torch.autograd entry points for the CLEAR local attention and for the operators around it - rotary, layer_norm, residual_norm, gated_ff -
 (argument marshalling only: forward and backward both run in the HIP library).
 
     from paper_2412_16112_amd.autograd import clear_attention
@@ -151,6 +151,38 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0):
     if any(w is not None and w.dim() == 2 and w.shape[0] > 65535 for w in (weight, bias)):
         raise ca.ClearAttnError(ca.CLEAR_ERR_UNSUPPORTED, "gradients: at most 65535 items with a weight each")
     return LayerNormFunction.apply(x, weight, bias, eps, weight_offset)
+
+
+class ResidualNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(fctx, x, y, gate, weight, bias, post_weight, eps, how):
+        r, h, stats = cb.residual_norm(x, y, gate, weight, bias, post_weight, eps=eps, save_stats=True, **how)
+        fctx.save_for_backward(x, y, gate, weight, bias, post_weight, stats)
+        fctx.set_materialize_grads(False)
+        fctx.how = how
+        return r, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(fctx, dr, dh):
+        x, y, gate, weight, bias, post_weight, stats = fctx.saved_tensors
+        need = fctx.needs_input_grad[:6]
+        if dr is None and dh is None:
+            return (None,) * 8
+        dh = y.new_zeros(y.shape) if dh is None else _rows_ok(dh)
+        return cb.residual_norm_backward(None if dr is None else _rows_ok(dr), dh, x, y, gate, weight, bias, post_weight, stats, need=need, **fctx.how) + (None, None)
+
+
+def residual_norm(x, y, gate=None, weight=None, bias=None, post_weight=None, kind="layer", post=None, eps=1e-6, residual_scale=1.0, weight_offset=0.0, post_offset=0.0):
+    """clear_block.residual_norm, differentiable in x, y, gate, weight, bias and post_weight: (r, h)."""
+    own = lambda t: t if t is None else t.contiguous()
+    x, y, gate, weight, bias, post_weight = _rows_ok(x), _rows_ok(y), own(gate), own(weight), own(bias), own(post_weight)
+    how = dict(kind=kind, post=post, residual_scale=residual_scale, weight_offset=weight_offset, post_offset=post_offset)
+    if _no_gradients(x, y, gate, weight, bias, post_weight):
+        return cb.residual_norm(x, y, gate, weight, bias, post_weight, eps=eps, **how)
+    if any(v is not None and v.dim() == 2 and v.shape[0] > 65535 for v in (gate, weight, bias)):
+        raise ca.ClearAttnError(ca.CLEAR_ERR_UNSUPPORTED, "gradients: at most 65535 items with a vector each")
+    return ResidualNormFunction.apply(x, y, gate, weight, bias, post_weight, eps, how)
 
 
 class GatedFFFunction(torch.autograd.Function):

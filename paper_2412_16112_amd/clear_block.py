@@ -647,7 +647,9 @@ def _launch_norm(name, grads, norm_type, max_norm, grad_scale, stream, factor):
     norm, factor, ws = new((), torch.float32), new((), torch.float32) if factor else None, new(size // 8, torch.float64)
     s = _call(name, device, stream, len(have), at, kind, 0.0 if max_norm is None else max_norm, _ptr(grad_scale), norm.data_ptr(), _ptr(factor), ws.data_ptr())
     if stream is not None:
-        _record(ws, s)
+        for t in (ws, norm, factor):  # (the factor may go to a step on that stream, and is nobody's then)
+            if t is not None:
+                _record(t, s)
     return norm, factor, have
 
 

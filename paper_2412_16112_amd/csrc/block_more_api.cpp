@@ -112,10 +112,7 @@ int clear_block_residual_norm_backward(const void* dR, const void* dH, const voi
         if (dX && !apart(all[4], beside_x, 5, extent, channels, &beside_x[0])) return invalid("dX must be dR itself or must not overlap it, and must not overlap another tensor");
         if (dY && !apart(all[5], beside_y, 4, extent, channels, &beside_y[1])) return invalid("dY must be dH itself or must not overlap it, and must not overlap another tensor");
     }
-    if (!some && (!sums || groups == 0)) {
-        // (no rows: dX and dY have no elements; shared vectors have gradients of 0, those of no groups none)
-        if (!sums) return CLEAR_OK;
-    }
+    if (!some && !sums) return CLEAR_OK;  // (dX and dY have no elements)
     ResidualArgs a = {};
     a.x = X, a.y = Y, a.gate = gate, a.w = weight, a.pw = post_weight, a.dr = dR, a.dh = dH, a.dx = dX, a.dy = dY;
     a.dgate = d_gate, a.dw = d_weight, a.db = d_bias, a.dpw = d_post_weight;
@@ -124,7 +121,7 @@ int clear_block_residual_norm_backward(const void* dR, const void* dH, const voi
     for (int i = 0; i < 12; ++i) a.st[i] = strides[i];
     a.per_group = per_group != 0, a.gate_per_group = gate_per_group != 0, a.kind = kind, a.post = post;
     a.scale = residual_scale, a.offset = weight_offset, a.post_offset = post_offset;
-    if (groups == 0) {  // vectors of no groups have no elements
+    if (groups == 0) {  // vectors of no groups have no elements; shared ones have gradients of 0
         if (a.gate_per_group) a.dgate = nullptr;
         if (a.per_group) a.dw = a.db = nullptr;
         a.gate_per_group = a.per_group = 0;
