@@ -670,7 +670,7 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     typedef Shape<WA, WB, NA, NB, RING> S;
     t.tiles_a = (t.rows_a + S::TA - 1) / S::TA;
     const long long tiles_b = (t.rows_b + S::TB - 1) / S::TB;
-    if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffffffffLL / S::THREADS) return hipErrorInvalidValue;
+    if (tiles_b > 0x7fffffffLL || tiles_b * t.tiles_a > 0xffff0000LL) return hipErrorInvalidValue;  // (outputs that no memory holds)
     t.tiles_b = (int)tiles_b;
     if (parts == 1) t.parts = nullptr;
     static LdsLimit limit;
