@@ -368,7 +368,7 @@ def residual_norm(x, y, gate=None, weight=None, bias=None, post_weight=None, kin
         if r.shape != x.shape or r.dtype != x.dtype or h.shape != y.shape or h.dtype != y.dtype:
             _refuse("out must have the shapes and dtypes of x and y", CLEAR_ERR_MISMATCH)
         strides = _Strides8(*_strides_of((("x", x), ("y", y), ("r", r), ("h", h))))
-    stats = torch.empty((4 if post_code else 2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if save_stats else None
+    stats = torch.empty((4 if post_code else 2,) + x.shape[:-1], dtype=torch.float32, device=x.device) if save_stats else None
     _call("clear_block_residual_norm", x.device, stream, x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(weight), _ptr(bias), _ptr(post_weight), r.data_ptr(), h.data_ptr(), _ptr(stats),
           groups, rows, C, strides, gate_per_group, per_group, kind_code, post_code, eps, residual_scale, weight_offset, post_offset, dtype, stream_dtype, wcode)
     if out is not None:
@@ -385,7 +385,7 @@ def residual_norm_backward(dr, dh, x, y, gate, weight, bias, post_weight, stats,
     _on_device(x, y, dr, dh, gate, weight, bias, post_weight, stats)
     if dh.shape != y.shape or dh.dtype != y.dtype or (dr is not None and (dr.shape != x.shape or dr.dtype != x.dtype)):
         _refuse("dr and dh must have the shapes and dtypes of x and y", CLEAR_ERR_MISMATCH)
-    if stats.dtype != torch.float32 or not stats.is_contiguous() or tuple(stats.shape) != (4 if post_code else 2,) + tuple(x.shape[:-1]):
+    if stats.dtype != torch.float32 or not stats.is_contiguous() or stats.shape != (4 if post_code else 2,) + x.shape[:-1]:
         _refuse("stats must be what residual_norm(..., save_stats=True) gave for x and y")
     grads = [_new_like(v) if v is not None and n else None for v, n in zip((x, y, gate, weight, bias, post_weight), need)]
     if all(g is None for g in grads):
@@ -396,7 +396,10 @@ def residual_norm_backward(dr, dh, x, y, gate, weight, bias, post_weight, stats,
         if floats < 0:
             _check(CLEAR_ERR_UNSUPPORTED)
         ws = torch.empty(max(1, floats), dtype=torch.float32, device=x.device)
-    strides = _strides_of((("dr", dr), ("dh", dh), ("x", x), ("y", y), ("dx", grads[0]), ("dy", grads[1])))
+    if x.is_contiguous() and y.is_contiguous() and dh.is_contiguous() and (dr is None or dr.is_contiguous()):
+        strides = (rows * C if x.dim() == 3 else 0, C) * 6
+    else:
+        strides = _strides_of((("dr", dr), ("dh", dh), ("x", x), ("y", y), ("dx", grads[0]), ("dy", grads[1])))
     s = _call("clear_block_residual_norm_backward", x.device, stream, _ptr(dr), dh.data_ptr(), x.data_ptr(), y.data_ptr(), _ptr(gate), _ptr(weight), _ptr(post_weight),
               stats.data_ptr(), *map(_ptr, grads), groups, rows, C, _Strides12(*strides), gate_per_group, per_group, kind_code, post_code, residual_scale, weight_offset,
               post_offset, dtype, stream_dtype, wcode, _ptr(ws))
