@@ -1,6 +1,9 @@
 // The norm of all gradients of a model with the factor that clips it, and the scaling of all gradients in place.  Memory-bound: every gradient is read once for the norm, and read
 // and written once where it is scaled.
 //
+// 113 M bf16 gradients 41 us (5.5 TB/s), with the factor 47; 98 MB of bf16 matrices and fp32 vectors clipped 58 (24 and 34, the second reading from the memory side's cache).  (Ranges of chunks a workgroup with the next
+// chunk's loads ahead: the same for the norm, scaling 10 % slower.)
+//
 // Squares are formed and added in fp64: they can neither overflow nor vanish, sums of 10^8 of them lose nothing, and the vector unit has the rate (a bf16 gradient's conversion and fma beside 2 bytes
 // of memory).  The largest magnitude is the largest of the values' bits without their signs, as whole numbers: a NaN is larger than everything.
 //
@@ -207,7 +210,7 @@ __device__ __forceinline__ void scale_all(const Launch& l, float factor)
 }
 __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Launch l, const float* factor) { scale_all(l, *factor); }
 // Clipping: every workgroup forms the factor for itself (of at most 8 KB of partials a launch), which a launch of its own and the wait for it would cost more than: 26 small tensors
-// LATER us, clipped by two launches behind the norm's LATER.
+// 6.8 us, norm and scaling apart 12.4.
 __global__ void __launch_bounds__(kThreads) grad_clip_kernel(const Launch l, const double* partials, long long n, GradFactor f, int gives)
 {
     scale_all(l, factor_of(partials, n, f, gives && blockIdx.x == 0));

@@ -20,8 +20,8 @@ typedef __attribute__((ext_vector_type(8))) int i32x8;
 int groups_of(int channels) { return (channels + kGroup - 1) / kGroup; }
 
 // ---- to 4 bits and back ---------------------------------------------------------------------------------------------------
-// Memory-bound.  A lane has 8 channels (4 lanes a block, half a wave a group), kQuantRows rows one after the other; a workgroup the same group of kQuantRows x 8 rows, whose scales are
-// one piece.
+// Memory-bound: 16 717 x 2 432 bf16 17 us there (5.9 TB/s), 19 back (5.3); 65 536 x 4 096 117 and 120 (four or eight rows a lane: 3 to 10 % slower).  A lane has 8 channels (4 lanes a block, half a
+// wave a group), kQuantRows rows one after the other; a workgroup the same group of kQuantRows x 8 rows, whose scales are one piece.
 constexpr int kQuantRows = 2;
 
 __device__ __forceinline__ unsigned top_of_block(unsigned bits)  // the largest of 4 neighbouring lanes
@@ -111,6 +111,12 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxArgs a)
 // Y = X W^T + bias: A are the rows of W (the contiguous axis of the output), B those of X.  A stage is 256 of the contraction: 128 bytes of codes and 8 of scales a row.  Lane l of an
 // instruction (32 x 32 outputs, 64 of the contraction) has row l % 32 and block l / 32 of two; as a sum has no order, instruction s of a stage takes blocks s and 4 + s of its 8, so that a lane's four
 // scales are four neighbouring bytes, of which the instruction names the s-th.
+//
+// The largest tile is 256 x 256 for 8 waves of 64 x 128, one workgroup a CU.  A workgroup goes on to further tiles, the next one's first stage under way during the epilogue, and stores past the caches (16 717 x
+// 2 432 x 9 728 246 us with a workgroup a tile, 213 to 235 now by the part's clock).  16 384 x 16 384 x 8 192: 960 us, 4.6 PFLOP/s, the matrix pipe busy 67 % at 1.63 GHz: the part is at
+// its power limit, and 4 waves of 128 x 128, which read a third less from LDS, take the same 1.75 us a stage (and 10 us more for a tile's end).  With 2 432 channels, ten stages, 48 % at 1.9 GHz: a tile's end, whose 128 KB
+// all CUs store at about the same time, costs 5 us beside 17 of stages.  Tried without gain: all of the next tile's first stages asked for before the epilogue (- 4 %), lines fetched to L2 two stages ahead (- 8 %), loads
+// all in one slot or a quarter of them early, wave priorities around the barrier (all within 2 %).
 
 typedef const __attribute__((address_space(3))) i32x4* lds_i32x4_ptr;
 typedef const __attribute__((address_space(3))) int* lds_int_ptr;
@@ -519,9 +525,10 @@ __global__ void __launch_bounds__(256) mx_join_kernel(const TileArgs t, int part
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
-// Up to 16 MT tokens: bound by the one reading of the weights.  A workgroup takes 16 outputs and all of the contraction, its 8 waves every eighth group of it: weights go straight
-// from memory to the operand registers.  Lane l of an instruction (16 x 16 outputs, 128 of the contraction) has row l % 16 and block l / 16 of four; instruction s of two takes
-// blocks s, 2 + s, 4 + s and 6 + s of a group, so that a lane's codes of a group are 32 neighbouring bytes and its scales two.  The waves' sums are added in order in LDS.
+// Up to 16 MT tokens: bound by the one reading of the weights (one token at 4 096 x 11 264: 8.4 us, 2.9 TB/s, of which 3 are a launch's start and end).  A workgroup takes 16 outputs and all of the
+// contraction, its 8 waves every eighth group of it: weights go straight from memory to the operand registers.  Lane l of an instruction (16 x 16 outputs, 128 of the contraction) has row l % 16 and
+// block l / 16 of four; instruction s of two takes blocks s, 2 + s, 4 + s and 6 + s of a group, so that a lane's codes of a group are 32 neighbouring bytes and its scales two.  The waves' sums are added
+// in order in LDS.
 constexpr int kFewWaves = 8;
 template <int S>
 __device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scale_a, int scale_b)
@@ -530,7 +537,7 @@ __device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scal
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_a, wide_b, c, 4, 4, S, scale_a, S, scale_b);
 }
 // Tokens that come as numbers and are at most kDirect go to 4 bits here: a wave takes the channels of its groups, 4 a lane, and its operands go through LDS.  (A launch of its own for that takes 3 us and
-// as many of the host's: one token at 4 096 x 11 264 LATER us from Python, LATER with it.)
+// as many of the host's: one token at 4 096 x 11 264 11 us from Python, 15 with it.)
 constexpr int kDirect = 4;
 struct DirectGroup {
     unsigned short codes[kDirect][64];  // (a lane's 4 codes)

@@ -4,6 +4,9 @@
 //
 // A team of TEAM waves holds a row, 8 channels a lane, in registers between its statistics and its results; r goes into its norm as it is, in fp32, before it is rounded for
 // memory, and the backward pass forms it again from x and y, which it reads in the place of r: as many bytes, and no rounding between the two.
+//
+// 2 x 4 608 x 2 432 bf16: forward 39 us (4.6 TB/s), backward 52 (5.2), 4.6 for the join of the sums; 16 896 x 4 096 bf16 with an fp32 stream and both norms 162 forward (5.1); 16 717 x 1 111 fp32 with both norms 62 and 91 (4.8 and
+// 4.9).  Beside the bytes, what counts is instructions: a choice for each element by what is absent (no gate, no post norm), and masks where a row is whole, cost the backward pass 10 to 18 %.
 #include <algorithm>
 #include <type_traits>
 
@@ -19,7 +22,7 @@ constexpr int kSums = 4;  // of the gate, weight, bias, post weight
 __host__ __device__ constexpr int forward_waves(int team) { return team >= 3 ? team : 4; }
 // As many waves as have the registers: for bf16 128 each, with fp32 among the rows 256 where a team is not wider.
 __host__ __device__ constexpr int backward_waves(int team, bool wide) { return wide && team <= 8 ? 8 / team * team : 16 / team * team; }
-// Where a wave has 128 registers the sums over rows are in LDS, each lane's own in a place of its own, else in registers.
+// Where a wave has 128 registers the sums over rows are in LDS, each lane's own in a place of its own, else in registers.  (12 waves of 168 registers instead: 2 x 4 608 x 2 432 bf16 67 -> 76 us.)
 __host__ __device__ constexpr bool sums_in_lds(int team, bool wide) { return backward_waves(team, wide) > 8; }
 
 // Both rows of a type lie in eights a lane, but fp32 alone in fours, so that neighbouring lanes load neighbouring 16 bytes.
