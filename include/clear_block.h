@@ -199,10 +199,12 @@ int clear_block_grad_norm(int n_tensors, const clear_block_grad* tensors, int ki
                           void* stream);
 /* Bytes of that workspace (host only); -1 for tensors that the calls refuse. */
 long long clear_block_grad_norm_workspace(int n_tensors, const clear_block_grad* tensors);
-/* The same, and every element of every tensor times the factor, in place, in a launch less than with clear_block_grad_scale behind it and to the same bits.  No two tensors may share memory. */
+/* The same, and every element of every tensor times the factor, in place, in a launch less than with clear_block_grad_scale behind it and to the same bits.  No two tensors may
+ * share memory, with each other, unscale, norm, factor or the workspace. */
 int clear_block_grad_clip(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, const float* unscale, float* norm, float* factor, void* workspace,
                           void* stream);
-/* Every element of every tensor times *factor, in fp32, rounded once, in place.  A factor of 1 leaves everything as it is and reads nothing.  No two tensors may share memory. */
+/* Every element of every tensor times *factor, in fp32, rounded once, in place.  A factor of 1 leaves everything as it is and reads nothing.  No two tensors may share
+ * memory, nor may the factor lie in one. */
 int clear_block_grad_scale(int n_tensors, const clear_block_grad* tensors, const float* factor, void* stream);
 
 /* ---- Operands in 4 bits -----------------------------------------------------------------------------------------------------

@@ -689,6 +689,8 @@ class MX4(collections.namedtuple("MX4", "codes scales")):
     __slots__ = ()
 
     def rows(self, first, last):
+        if self.codes.dim() != 2:
+            _refuse("a range of rows is one of a matrix of two axes")
         return MX4(self.codes[first:last], self.scales[:, first:last])
 
 
@@ -723,15 +725,19 @@ def _any_rows(t, name):
     C = t.shape[-1]
     if t.is_contiguous():
         return (t.shape[0] if dims == 2 else t.numel() // C if C else 0), C
-    if dims != 2:
-        _refuse("%s: a tensor of %d axes must be contiguous" % (name, dims))
-    if C > 1 and t.stride(1) != 1:
+    if C > 1 and t.stride(-1) != 1:
         _refuse("%s: the last axis must be contiguous" % name)
-    return t.shape[0], t.stride(0) if t.shape[0] > 1 else C
+    rows, ld = 1, C
+    for n, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n > 1:
+            if rows > 1 and stride != rows * ld:
+                _refuse("%s: the rows must be evenly spaced" % name)
+            rows, ld = rows * n, ld if rows > 1 else stride
+    return rows, ld
 
 
 def mx_quantize(x, stream=None):
-    """clear_block_mx_quantize: x [..., C] (bf16 or fp32, C a multiple of 32) to 4 bits with a scale for every 32 channels of a row: an MX4."""
+    """clear_block_mx_quantize: x [..., C] (bf16 or fp32, C a multiple of 32, rows evenly spaced) to 4 bits with a scale for every 32 channels of a row: an MX4."""
     dtype = _code(x)
     _on_device(x)
     rows, ld = _any_rows(x, "x")
@@ -754,7 +760,7 @@ def mx_dequantize(t, dtype=torch.bfloat16, stream=None):
 
 def mx_linear(x, w, bias=None, dtype=None, out=None, stream=None):
     """clear_block_mx_linear: x w^T + bias for w [F, C] in 4 bits (an MX4) and x [..., C]: an MX4, or bf16 or fp32, which the call takes to 4 bits first.  bias: [F], bf16 or fp32, or None.
-    Returns [..., F] of `dtype` (bf16 by default), or out."""
+    Returns [..., F] of `dtype` (bf16 by default), or out.  No gradient goes through it."""
     F, C, ld_w, ld_ws = _mx_operand(w, "w")
     if w[0].dim() != 2 or F < 1:
         _refuse("w must be [F, C], F >= 1")

@@ -1,6 +1,7 @@
 // C ABI of the gated residual with its norms, the norm of gradients and the operands in 4 bits (include/clear_block.h): argument checks and launches.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <utility>
 #include <vector>
 
@@ -172,17 +173,23 @@ int check_norm(int n_tensors, const clear_block_grad* tensors, int kind, double 
     if (!workspace && grad_norm_partials(n_tensors, tensors) > 0) return invalid("workspace must be non-NULL");
     return CLEAR_OK;
 }
-// Whether no two tensors, which are written, share memory.
-int check_apart(int n_tensors, const clear_block_grad* tensors) noexcept
+// Whether no two tensors, which are written, share memory with each other or with the scalars and partials that other workgroups read or write meanwhile.
+struct Beside {
+    const void* p;
+    long long bytes;
+};
+int check_apart(int n_tensors, const clear_block_grad* tensors, std::initializer_list<Beside> beside) noexcept
 {
     try {
         std::vector<std::pair<uintptr_t, uintptr_t>> spans;
-        spans.reserve(n_tensors);
+        spans.reserve(n_tensors + beside.size());
         for (int i = 0; i < n_tensors; ++i)
             if (tensors[i].data && tensors[i].n > 0) spans.emplace_back((uintptr_t)tensors[i].data, (uintptr_t)tensors[i].data + (uintptr_t)tensors[i].n * size_of(tensors[i].dtype));
+        for (const Beside& b : beside)
+            if (b.p && b.bytes > 0) spans.emplace_back((uintptr_t)b.p, (uintptr_t)b.p + (uintptr_t)b.bytes);
         std::sort(spans.begin(), spans.end());
         for (size_t i = 1; i < spans.size(); ++i)
-            if (spans[i].first < spans[i - 1].second) return invalid("gradients share memory");
+            if (spans[i].first < spans[i - 1].second) return invalid("gradients share memory with each other, or with a scalar or the workspace");
     } catch (...) {
         return fail(CLEAR_ERR_ALLOC, "out of host memory");
     }
@@ -203,7 +210,9 @@ int clear_block_grad_norm(int n_tensors, const clear_block_grad* tensors, int ki
 int clear_block_grad_clip(int n_tensors, const clear_block_grad* tensors, int kind, double max_norm, const float* unscale, float* norm, float* factor, void* workspace, void* stream)
 {
     int rc = check_norm(n_tensors, tensors, kind, max_norm, true, unscale, norm, factor, workspace);
-    if (rc != CLEAR_OK || (rc = check_apart(n_tensors, tensors)) != CLEAR_OK) return rc;
+    if (rc != CLEAR_OK) return rc;
+    const Beside partials = {workspace, grad_norm_partials(n_tensors, tensors) * 8};
+    if ((rc = check_apart(n_tensors, tensors, {{unscale, 4}, {norm, 4}, {factor, 4}, partials})) != CLEAR_OK) return rc;
     const GradFactor f = {kind, max_norm, unscale, norm, factor};
     return launched(launch_grad_clip(n_tensors, tensors, f, workspace, (hipStream_t)stream), "gradient clipping launch failed: ");
 }
@@ -211,8 +220,9 @@ int clear_block_grad_clip(int n_tensors, const clear_block_grad* tensors, int ki
 int clear_block_grad_scale(int n_tensors, const clear_block_grad* tensors, const float* factor, void* stream)
 {
     int rc = check_grads(n_tensors, tensors);
-    if (rc != CLEAR_OK || (rc = check_apart(n_tensors, tensors)) != CLEAR_OK) return rc;
+    if (rc != CLEAR_OK) return rc;
     if (!factor || !aligned(factor, 4)) return invalid("factor must be a pointer to a float");
+    if ((rc = check_apart(n_tensors, tensors, {{factor, 4}})) != CLEAR_OK) return rc;
     return launched(launch_grad_scale(n_tensors, tensors, factor, (hipStream_t)stream), "gradient scaling launch failed: ");
 }
 

@@ -144,6 +144,17 @@ def test_layouts(M):
     assert torch.equal(cb.mx_linear(t, w, bias.cuda()), y)
 
 
+def test_one_part_of_a_wider_projection():
+    # [B, N, 3 C], a C of it: rows evenly spaced over both leading axes
+    wide = torch.randn(2, 65, 3 * 288, dtype=BF, device="cuda")
+    w = cb.mx_quantize(torch.randn(70, 288, device="cuda"))
+    for part in wide.split(288, -1):
+        assert torch.equal(cb.mx_quantize(part).codes, cb.mx_quantize(part.contiguous()).codes)
+        into = torch.full((2, 65, 100), 7.0, dtype=BF, device="cuda")
+        cb.mx_linear(part, w, out=into[..., 9:79])
+        assert torch.equal(into[..., 9:79], cb.mx_linear(part.contiguous(), w)) and bool((into[..., :9] == 7).all()) and bool((into[..., 79:] == 7).all())
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_nan_stays_in_its_row(M):
     x, w, _ = operands(M, 512, 150, BF)

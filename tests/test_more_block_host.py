@@ -106,6 +106,19 @@ def test_clip_refusals(change, status):
     assert norm("clear_block_grad_clip", **change) == status
 
 
+@pytest.mark.parametrize("change", [
+    dict(unscale=P[0] + 100), dict(unscale=P[1] + 4 * 32), dict(norm=P[0] + 1996), dict(factor=P[1]), dict(norm=P[2]), dict(factor=P[2]), dict(norm=P[4]), dict(workspace=P[0]), dict(workspace=P[1] + 128),
+    dict(tensors=grads(SOME[0], (P[5] + 8, 3, F32))),
+], ids=str)
+def test_clip_refuses_scalars_and_partials_among_the_gradients(change):
+    assert norm("clear_block_grad_clip", **change) == INVALID
+
+
+@pytest.mark.parametrize("factor", [P[0], P[0] + 1996, P[1] + 128])
+def test_scale_refuses_a_factor_among_the_gradients(factor):
+    assert cb.lib().clear_block_grad_scale(2, grads(*SOME), factor, None) == INVALID
+
+
 @pytest.mark.parametrize("n,tensors,factor,status", [
     (2, grads(*SOME), None, INVALID), (2, grads(*SOME), P[3] + 2, INVALID), (-1, grads(*SOME), P[3], INVALID), (2, None, P[3], INVALID), (2, grads((P[0], 100, BF), (P[0] + 198, 5, BF)), P[3], INVALID),
     (0, None, P[3], OK), (2, grads((P[0], 0, BF), (None, 7, F32)), P[3], OK),
@@ -195,8 +208,19 @@ MX = cb.MX4(torch.zeros(5, 32, dtype=torch.uint8), torch.zeros(1, 5, 8, dtype=to
     lambda: cb.residual_norm_backward(X, X, X, X, None, None, None, None, X), lambda: cb.grad_norm([]), lambda: cb.grad_norm([None]), lambda: cb.grad_norm([V]), lambda: cb.grad_norm([V], norm_type=1),
     lambda: cb.clip_grads([V], 1.0), lambda: cb.scale_grads([V], V[0]), lambda: cb.mx_quantize(X), lambda: cb.mx_dequantize(MX), lambda: cb.mx_dequantize(X), lambda: cb.mx_dequantize((X, X)),
     lambda: cb.mx_dequantize(cb.MX4(MX.codes, MX.scales[:, :4])), lambda: cb.mx_dequantize(cb.MX4(MX.codes[:, :20], MX.scales)), lambda: cb.mx_dequantize(cb.MX4(MX.codes.t(), MX.scales)),
+    lambda: cb.MX4(MX.codes[None], MX.scales).rows(0, 1), lambda: cb.MX4(MX.codes[0], MX.scales[:, :1]).rows(0, 16),
     lambda: cb.mx_linear(X, MX), lambda: cb.mx_linear(X, X), lambda: cb.mx_linear(X[..., :32], MX), lambda: cb.mx_linear(MX, MX), lambda: cb.mx_linear(X, MX, bias=V),
 ])
 def test_binding_refusals(bad):
     with pytest.raises(ca.ClearAttnError):
         bad()
+
+
+def test_rows_of_tensors_of_many_axes():
+    t = torch.zeros(3, 4, 5, 96)
+    assert cb._any_rows(t, "t") == (60, 96) and cb._any_rows(t[..., 32:64], "t") == (60, 96) and cb._any_rows(t[:, :, 2, :32], "t") == (12, 480) and cb._any_rows(t[:, 1:2, 3:4, :64], "t") == (3, 1920)
+    assert cb._any_rows(t[1, 2, 3:4, :32], "t") == (1, 32) and cb._any_rows(t[0, 0, 0], "t") == (1, 96) and cb._any_rows(t[:0, :, :, :32], "t")[0] == 0
+    assert cb._any_rows(t[:1, :1, :1, :32].expand(3, 4, 5, 32), "t") == (60, 0)
+    for bad in (t[:, 1:3, :, :32], t.transpose(0, 1), t[:, :, :2], t.expand(2, 3, 4, 5, 96)[..., :32], t[..., ::2]):
+        with pytest.raises(ca.ClearAttnError):
+            cb._any_rows(bad, "t")
