@@ -525,11 +525,10 @@ __global__ void __launch_bounds__(256) mx_join_kernel(const TileArgs t, int part
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
-// Up to 16 MT tokens: bound by the one reading of the weights (one token at 4 096 x 11 264: 8.4 us, 2.9 TB/s, of which 3 are a launch's start and end).  A workgroup takes 16 outputs and all of the
-// contraction, its 8 waves every eighth group of it: weights go straight from memory to the operand registers.  Lane l of an instruction (16 x 16 outputs, 128 of the contraction) has row l % 16 and
-// block l / 16 of four; instruction s of two takes blocks s, 2 + s, 4 + s and 6 + s of a group, so that a lane's codes of a group are 32 neighbouring bytes and its scales two.  The waves' sums are added
-// in order in LDS.
-constexpr int kFewWaves = 8;
+// Up to 16 MT tokens: bound by the one reading of the weights.  A workgroup takes 16 outputs and all of the contraction, its 8 or 16 waves every 8th or 16th group of it: weights go straight from memory
+// to the operand registers.  Lane l of an instruction (16 x 16 outputs, 128 of the contraction) has row l % 16 and block l / 16 of four; instruction s of two takes blocks s, 2 + s, 4 + s and 6 + s of a
+// group, so that a lane's codes of a group are 32 neighbouring bytes and its scales two.  The waves' sums are added in order in LDS.
+// One token at 4 096 x 11 264: 7.7 us a launch in a graph (3.2 TB/s, of which some 3 us are a launch's start and end); three or four groups ahead in place of two 10.
 template <int S>
 __device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scale_a, int scale_b)
 {
@@ -537,11 +536,12 @@ __device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scal
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_a, wide_b, c, 4, 4, S, scale_a, S, scale_b);
 }
 // Tokens that come as numbers and are at most kDirect go to 4 bits here: a wave takes the channels of its groups, 4 a lane, and its operands go through LDS.  (A launch of its own for that takes 3 us and
-// as many of the host's: one token at 4 096 x 11 264 11 us from Python, 15 with it.)
+// as many of the host's: one token at 4 096 x 11 264 10 us from Python, 15 with it.)
 constexpr int kDirect = 4;
+template <int N>
 struct DirectGroup {
-    unsigned short codes[kDirect][64];  // (a lane's 4 codes)
-    unsigned char scales[kDirect][8];
+    unsigned short codes[N][64];  // (a lane's 4 codes)
+    unsigned char scales[N][8];
 };
 template <typename T>
 struct FourOf;
@@ -553,15 +553,18 @@ template <>
 struct FourOf<float> {
     typedef f32x4_any type;
 };
-template <typename T>
-__device__ __forceinline__ void direct_group(DirectGroup* to, const T* x, long long ld_x, int tokens, int c, int channels, int lane)
+template <typename T, int N>
+__device__ __forceinline__ void load_direct(f32x4 (&v)[N], const T* x, long long ld_x, int tokens, int c, int channels)
 {
-    f32x4 v[kDirect];
 #pragma unroll
-    for (int m = 0; m < kDirect; ++m)
+    for (int m = 0; m < N; ++m)
         v[m] = m < tokens && c < channels ? __builtin_convertvector(*(const typename FourOf<T>::type*)(x + m * ld_x + c), f32x4) : f32x4{0.f, 0.f, 0.f, 0.f};
+}
+template <int N>
+__device__ __forceinline__ void direct_group(DirectGroup<N>* to, const f32x4 (&v)[N], int tokens, int lane)
+{
 #pragma unroll
-    for (int m = 0; m < kDirect; ++m) {
+    for (int m = 0; m < N; ++m) {
         if (m >= tokens) break;
         unsigned top = 0;
 #pragma unroll
@@ -577,15 +580,15 @@ __device__ __forceinline__ void direct_group(DirectGroup* to, const T* x, long l
     }
 }
 
-// T: of the tokens, or void where they come in 4 bits.
-template <int MT, typename T>
-__global__ void __launch_bounds__(64 * kFewWaves) mx_few_kernel(const TileArgs t)
+// T: of the tokens, of which there are N at most, or void where they come in 4 bits.
+template <int MT, typename T, int N, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) mx_few_kernel(const TileArgs t)
 {
     constexpr bool DIRECT = !std::is_void<T>::value;
     static_assert(!DIRECT || MT == 1);
     constexpr int AHEAD = 2;  // groups whose loads are in flight together
-    __shared__ f32x4 part[kFewWaves][MT][64];
-    __shared__ __attribute__((aligned(16))) DirectGroup direct[DIRECT ? kFewWaves : 1][DIRECT ? AHEAD : 1];
+    __shared__ f32x4 part[WAVES][MT][64];
+    __shared__ __attribute__((aligned(16))) DirectGroup<N> direct[DIRECT ? WAVES : 1][DIRECT ? AHEAD : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = 2 * (lane >> 4);
     const int f0 = blockIdx.x * 16;
     const int f = min(f0 + (lane & 15), t.rows_a - 1);
@@ -600,17 +603,35 @@ __global__ void __launch_bounds__(64 * kFewWaves) mx_few_kernel(const TileArgs t
             xs[m] = t.xs + token * 8 + block;
         }
     }
+    // this thread's four outputs of the end, whose bias is asked for here, where it delays nothing (of several tokens that are numbers, behind the sums: registers)
+    const int c = f0 + 4 * (lane >> 4);
+    f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+    auto load_bias = [&] {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[e] = bias_of(t, c + e);
+    };
+    if (N == 1 && wave < MT) load_bias();
     f32x4 acc[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int groups = (t.depth + kGroup - 1) / kGroup;
-    for (int g0 = wave; g0 < groups; g0 += kFewWaves * AHEAD) {
+    for (int g0 = wave; g0 < groups; g0 += WAVES * AHEAD) {
+        // (One token is read first: it comes from near and goes to 4 bits while the weights are on their way: 4 096 x 11 264 8.9 -> 7.7 us.  Of several, the registers for that would cost more: 11.3 -> 14.0.)
+        f32x4 v[DIRECT ? AHEAD : 1][N];
+        auto load_tokens = [&](int i) {
+            if constexpr (DIRECT) load_direct<T>(v[i], (const T*)t.x, t.ld_x, (int)t.rows_b, (g0 + WAVES * i) * kGroup + 4 * lane, t.depth);
+        };
+        if constexpr (DIRECT && N == 1) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) load_tokens(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         i32x4 a[AHEAD][2], b[AHEAD][MT][2];
         int sa[AHEAD], sb[AHEAD][MT];
         const i32x4 zero = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int g = g0 + kFewWaves * i, left = t.depth - g * kGroup - block * 32;  // channels from this lane's first block on
+            const int g = g0 + WAVES * i, left = t.depth - g * kGroup - block * 32;  // channels from this lane's first block on
             const int mask = left >= 64 ? 0xffff : left > 0 ? 0xff : 0;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -627,17 +648,21 @@ __global__ void __launch_bounds__(64 * kFewWaves) mx_few_kernel(const TileArgs t
             }
         }
         if constexpr (DIRECT) {
+            if constexpr (N == 1) __builtin_amdgcn_sched_barrier(0);
             const int token = lane & 15;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) direct_group<T>(&direct[wave][i], (const T*)t.x, t.ld_x, (int)t.rows_b, (g0 + kFewWaves * i) * kGroup + 4 * lane, t.depth, lane);
+            for (int i = 0; i < AHEAD; ++i) {
+                if constexpr (N > 1) load_tokens(i);
+                direct_group(&direct[wave][i], v[i], (int)t.rows_b, lane);
+            }
             asm volatile("" ::: "memory");  // (a wave's LDS instructions are executed in order)
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                const DirectGroup& d = direct[wave][i];
+                const DirectGroup<N>& d = direct[wave][i];
                 const bool in = token < (int)t.rows_b;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) b[i][0][k] = in ? *(const i32x4*)((const unsigned char*)d.codes[token & (kDirect - 1)] + 16 * (block + k)) : zero;
-                sb[i][0] = in ? *(const unsigned short*)(d.scales[token & (kDirect - 1)] + block) : 0;
+                for (int k = 0; k < 2; ++k) b[i][0][k] = in ? *(const i32x4*)((const unsigned char*)d.codes[token & (N - 1)] + 16 * (block + k)) : zero;
+                sb[i][0] = in ? *(const unsigned short*)(d.scales[token & (N - 1)] + block) : 0;
             }
             asm volatile("" ::: "memory");
         }
@@ -653,22 +678,30 @@ __global__ void __launch_bounds__(64 * kFewWaves) mx_few_kernel(const TileArgs t
     for (int m = 0; m < MT; ++m) part[wave][m][lane] = acc[m];
     __syncthreads();
     // register r of lane l: output 4 (l / 16) + r, token l % 16
-    for (int at = threadIdx.x; at < MT * 64; at += 64 * kFewWaves) {
-        const int m = at >> 6, l = at & 63;
-        f32x4 s = part[0][m][l];
+    if (wave >= MT) return;
+    f32x4 s = part[0][wave][lane];
 #pragma unroll
-        for (int v = 1; v < kFewWaves; ++v) s += part[v][m][l];
-        const long long token = 16 * m + (l & 15);
-        const int c = f0 + 4 * (l >> 4);
-        if (token >= t.rows_b) continue;
+    for (int v = 1; v < WAVES; ++v) s += part[v][wave][lane];
+    if (N > 1) load_bias();
+    s += bias;
+    const long long token = 16 * wave + (lane & 15);
+    if (token >= t.rows_b) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (c + e >= t.rows_a) break;
-            const float y = s[e] + bias_of(t, c + e);
-            if (t.out_bf16) ((__bf16*)t.out)[token * t.ld_out + c + e] = (__bf16)y;
-            else ((float*)t.out)[token * t.ld_out + c + e] = y;
-        }
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= t.rows_a) break;
+        if (t.out_bf16) ((__bf16*)t.out)[token * t.ld_out + c + e] = (__bf16)s[e];
+        else ((float*)t.out)[token * t.ld_out + c + e] = s[e];
     }
+}
+
+template <int MT, typename T, int N>
+hipError_t launch_few(const TileArgs& t, hipStream_t stream)
+{
+    // Where a CU has one workgroup and 8 waves more than a turn's work, 16: 11 264 x 4 096 11.4 -> 8.2 us; at 4 096 x 11 264 7.7 -> 10.5, at 2 048 x 2 048 and 16 tokens 3.8 -> 4.0.
+    const dim3 grid((t.rows_a + 15) / 16);
+    if (grid.x <= 256 && groups_of(t.depth) > 8 * MT) mx_few_kernel<MT, T, N, 16><<<grid, dim3(64 * 16), 0, stream>>>(t);
+    else mx_few_kernel<MT, T, N, 8><<<grid, dim3(64 * 8), 0, stream>>>(t);
+    return hipGetLastError();
 }
 
 template <int WA, int WB, int NA, int NB, int RING>
@@ -783,11 +816,10 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
     t.bias = a.bias, t.bias_bf16 = a.bias_dtype == CLEAR_BF16;
     t.out = a.y, t.ld_out = a.ld_y, t.out_bf16 = a.out_dtype == CLEAR_BF16;
     t.rows_a = a.outputs, t.rows_b = a.tokens, t.depth = a.channels;
-    const dim3 few_grid((a.outputs + 15) / 16), few_block(64 * kFewWaves);
     if (!a.xs && a.tokens <= kDirect) {
-        if (a.x_dtype == CLEAR_BF16) mx_few_kernel<1, __bf16><<<few_grid, few_block, 0, stream>>>(t);
-        else mx_few_kernel<1, float><<<few_grid, few_block, 0, stream>>>(t);
-        return hipGetLastError();
+        const bool half = a.x_dtype == CLEAR_BF16;
+        if (a.tokens == 1) return half ? launch_few<1, __bf16, 1>(t, stream) : launch_few<1, float, 1>(t, stream);
+        return half ? launch_few<1, __bf16, kDirect>(t, stream) : launch_few<1, float, kDirect>(t, stream);
     }
     unsigned char* ws = (unsigned char*)a.workspace;
     if (!a.xs) {
@@ -804,10 +836,7 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
     const Plan p = plan_of(a.tokens, a.channels, a.outputs);
     t.parts = (float*)ws, t.ld_parts = parts_pitch(a.outputs);
     switch (p.shape) {
-    case kFew:
-        if (a.tokens <= 16) mx_few_kernel<1, void><<<few_grid, few_block, 0, stream>>>(t);
-        else mx_few_kernel<2, void><<<few_grid, few_block, 0, stream>>>(t);
-        return hipGetLastError();
+    case kFew: return a.tokens <= 16 ? launch_few<1, void, 1>(t, stream) : launch_few<2, void, 1>(t, stream);
     case kLarge: return launch_tiles<4, 2, 2, 4, 2>(t, p.parts, stream);
     case kPair: return launch_tiles<2, 2, 2, 2, 2>(t, p.parts, stream);
     default: return launch_tiles<2, 2, 2, 2, 4>(t, p.parts, stream);

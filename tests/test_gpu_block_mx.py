@@ -94,7 +94,7 @@ def product(values, w, bias, dtype):
 
 
 SIZES = [(1, 32, 1), (1, 256, 16), (1, 2432, 300), (2, 96, 33), (3, 8192, 50), (4, 1056, 40), (5, 288, 17), (16, 512, 100), (17, 1056, 40), (33, 768, 65), (64, 2080, 31), (65, 2432, 300), (128, 256, 128), (130, 608, 515), (257, 2400, 777),
-         (300, 4096, 256), (100, 8192, 130), (520, 96, 1030), (2100, 512, 3001)]
+         (300, 4096, 256), (100, 8192, 130), (520, 96, 1030), (2100, 512, 3001), (16, 2336, 80), (30, 4640, 70), (1, 4384, 4100), (2, 4384, 4100)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=str)

@@ -109,7 +109,7 @@ def test_clip_refusals(change, status):
 @pytest.mark.parametrize("change", [
     dict(unscale=P[0] + 100), dict(unscale=P[1] + 4 * 32), dict(norm=P[0] + 1996), dict(factor=P[1]), dict(norm=P[2]), dict(factor=P[2]), dict(norm=P[4]), dict(workspace=P[0]), dict(workspace=P[1] + 128),
     dict(tensors=grads(SOME[0], (P[5] + 8, 3, F32))),
-], ids=str)
+])
 def test_clip_refuses_scalars_and_partials_among_the_gradients(change):
     assert norm("clear_block_grad_clip", **change) == INVALID
 

@@ -125,8 +125,9 @@ LARGE, PAIR, DEEP = (4, 2, 2, 4, 2), (2, 2, 2, 2, 2), (2, 2, 2, 2, 4)
 
 
 @pytest.mark.parametrize("tokens,channels,outputs,want", [
-    (1, 4096, 11264, [("mx_few_kernel", (1,), 704)]), (4, 4096, 11264, [("mx_few_kernel", (1,), 704)]), (5, 4096, 11264, ["quantize", ("mx_few_kernel", (1,), 704)]),
-    (17, 4096, 4096, ["quantize", ("mx_few_kernel", (2,), 256)]), (17, 4096, 11264, ["quantize", ("mx_tile_kernel", DEEP, 88), "join"]), (333, 2432, 7297, ["quantize", ("mx_tile_kernel", DEEP, 174)]),
+    (1, 4096, 11264, [("mx_few_kernel", (1, 1, 8), 704)]), (4, 4096, 11264, [("mx_few_kernel", (1, 4, 8), 704)]), (5, 4096, 11264, ["quantize", ("mx_few_kernel", (1, 1, 8), 704)]),
+    (1, 11264, 4096, [("mx_few_kernel", (1, 1, 16), 256)]), (3, 2304, 4096, [("mx_few_kernel", (1, 4, 16), 256)]), (1, 2048, 2048, [("mx_few_kernel", (1, 1, 8), 128)]),
+    (17, 4096, 4096, ["quantize", ("mx_few_kernel", (2, 1, 8), 256)]), (32, 4352, 3840, ["quantize", ("mx_few_kernel", (2, 1, 16), 240)]), (17, 4096, 11264, ["quantize", ("mx_tile_kernel", DEEP, 88), "join"]), (333, 2432, 7297, ["quantize", ("mx_tile_kernel", DEEP, 174)]),
     (2000, 1536, 4096, ["quantize", ("mx_tile_kernel", PAIR, 512)]), (16717, 2432, 9728, ["quantize", ("mx_tile_kernel", LARGE, 256)]), (100, 9728, 2432, ["quantize", ("mx_tile_kernel", DEEP, 19), "join"]),
     (2 ** 31 - 1, 32, 1, ["quantize"] * 2049 + [("mx_tile_kernel", PAIR, 512)]),
 ])
