@@ -1,7 +1,7 @@
 // The norm of all gradients of a model with the factor that clips it, and the scaling of all gradients in place.  Memory-bound: every gradient is read once for the norm, and read
 // and written once where it is scaled.
 //
-// 113 M bf16 gradients 41 us (5.5 TB/s), with the factor 47; 98 MB of bf16 matrices and fp32 vectors clipped 58 (24 and 34, the second reading from the memory side's cache).  (Ranges of chunks a workgroup with the next
+// 113 M bf16 gradients 40 us (5.6 TB/s) and 4 for the factor; 98 MB of bf16 matrices and fp32 vectors clipped 58 (24 and 34, the second reading from the memory side's cache).  (Ranges of chunks a workgroup with the next
 // chunk's loads ahead: the same for the norm, scaling 10 % slower.)
 //
 // Squares are formed and added in fp64: they can neither overflow nor vanish, sums of 10^8 of them lose nothing, and the vector unit has the rate (a bf16 gradient's conversion and fma beside 2 bytes
