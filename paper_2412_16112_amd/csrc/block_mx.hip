@@ -727,11 +727,19 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Form, tile shape and number of parts that the contraction is split into, by the time that they are expected to take with weights from memory: rounds of workgroups over the 256 CUs, each
-// of a part's steps (256 of the contraction) and of what a tile costs beside.  The constants, in us, were fitted to 800 timings at 8 to 4608 tokens and five shapes of 1536 x 4096 to
-// 4096 x 11264: the chosen form takes 1.3 % longer than the best of them on average, at most 17 %.  A tile of 256 x 256 alone on its CU takes 1.55 us a step, one of 128 x 128 with four stages in flight 0.58, two of
-// 128 x 128 with two stages each 1.07 (1000 tokens at 9728 x 2432: 64, 27 and 41 us, 4608 at 2432 x 9728: 65, 94 and 76).
-enum TileShape { kFew, kLarge, kPair, kDeep };  // few tokens; 256 x 256; 128 x 128, two workgroups a CU; 128 x 128, one a CU with four stages in flight
+// Form, tile shape and number of parts that the contraction is split into, by the time that they are expected to take with weights from memory: where no CU has two tiles, a part's steps (256 of the
+// contraction) and what a tile costs beside; else rounds of as many tiles as the chip holds at once.  The constants, in us, were fitted to 3000 timings at 8 to 3000 tokens and eleven shapes of 608 x 3000 to
+// 4096 x 11264: the chosen form takes 0.5 % longer than the best of them on average, at most 11 %.  (77 tokens at 4096 x 11264: 64 x 64 12.5 us, 64 x 128 12.1, 128 x 128 14.3; at 4096 x 4096 8.2, 9.2 and 11.9; 333 at
+// 2432 x 7297 13.8, 12.6 and 11.7; 1000 at 2432 x 9728 39.9, 29.6 and 31.0, 256 x 256 25.6.)
+enum TileShape { kLarge, kPair, kDeep, kSmall, kFlat, kFew };  // kPair: two workgroups a CU, kDeep: one with four stages in flight
+struct Cost {
+    int outputs, tokens;                 // of a tile
+    int at_once;                         // tiles that the chip holds
+    double step_alone, tile_alone;       // where it holds more than a tile a CU and has not to
+    double step, round, start;
+} constexpr kCosts[] = {
+    {256, 256, 256, 0, 0, 1.34, 7.4, -1.3}, {128, 128, 512, 0.88, 3.6, 1.03, 1.6, 3.6}, {128, 128, 256, 0, 0, 0.52, 3.0, 1.7}, {64, 64, 512, 0.25, 3.3, 0.41, 1.3, 4.5}, {64, 128, 512, 0.44, 4.0, 0.65, 1.3, 3.6},
+};
 struct Plan {
     TileShape shape;
     int parts;
@@ -739,19 +747,21 @@ struct Plan {
 Plan plan_of(long long tokens, int channels, int outputs)
 {
     const auto up = [](long long x, long long by) { return (x + by - 1) / by; };
-    // (few tokens, here and in tiles: 8 at 2432 x 9728 7.1 and 10.5, at 4096 x 11264 9.8 and 13.0; 32 at 4096 x 4096 7.1 and 10.8, at 2432 x 9728 12.0 and 11.1, at 4096 x 11264 18.6 and 13.4)
-    if (tokens <= 16 || (tokens <= 32 && (long long)channels * outputs <= 1 << 24)) return {kFew, 1};
-    const long long steps = groups_of(channels), large = up(outputs, 256) * up(tokens, 256), small = up(outputs, 128) * up(tokens, 128);
+    // (few tokens, here and in tiles: 8 at 2432 x 9728 6.5 and 7.3, at 4096 x 11264 8.5 and 9.2; 32 at 4096 x 4096 6.6 and 8.2, at 2432 x 7297 6.4 and 7.4, at 2432 x 9728 12.8 and 7.5)
+    if (tokens <= 16 || (tokens <= 32 && (long long)channels * outputs <= 20 << 20)) return {kFew, 1};
+    const long long steps = groups_of(channels);
     Plan best = {kLarge, 1};
     double best_us = 0;
     for (int parts = 1; parts <= 8 && (parts == 1 || steps >= 3 * parts); ++parts) {
         const double each = (double)up(steps, parts);
         // (the parts are written and read once more)
-        const double join = parts == 1 ? 0 : 3 + (2.2 * parts + 0.5) * tokens * outputs * 4 / 4e6;
-        const double us[3] = {up(large * parts, 256) * (each * 1.55 + 6) + join, (small * parts <= 256 ? each + 2.5 : up(small * parts, 512) * (each * 1.07 + 4.5)) + join,
-                              up(small * parts, 256) * (each * 0.58 + 4.4) + join};
-        for (int i = 0; i < 3; ++i)
-            if (best_us == 0 || us[i] < best_us) best_us = us[i], best = {(TileShape)(kLarge + i), parts};
+        const double join = parts == 1 ? 0 : 3.7 + (1.35 * parts - 0.1) * tokens * outputs * 4 / 4e6;
+        for (int i = kLarge; i <= kFlat; ++i) {
+            const Cost& c = kCosts[i];
+            const long long tiles = up(outputs, c.outputs) * up(tokens, c.tokens) * parts;
+            const double us = join + (tiles <= 256 && c.at_once > 256 ? each * c.step_alone + c.tile_alone : up(tiles, c.at_once) * (each * c.step + c.round) + c.start);
+            if (best_us == 0 || us < best_us) best_us = us, best = {(TileShape)i, parts};
+        }
     }
     return best;
 }
@@ -839,7 +849,9 @@ hipError_t launch_mx_linear(const MxLinearArgs& a, hipStream_t stream)
     case kFew: return a.tokens <= 16 ? launch_few<1, void, 1>(t, stream) : launch_few<2, void, 1>(t, stream);
     case kLarge: return launch_tiles<4, 2, 2, 4, 2>(t, p.parts, stream);
     case kPair: return launch_tiles<2, 2, 2, 2, 2>(t, p.parts, stream);
-    default: return launch_tiles<2, 2, 2, 2, 4>(t, p.parts, stream);
+    case kDeep: return launch_tiles<2, 2, 2, 2, 4>(t, p.parts, stream);
+    case kSmall: return launch_tiles<1, 2, 2, 1, 4>(t, p.parts, stream);
+    default: return launch_tiles<1, 4, 2, 1, 3>(t, p.parts, stream);
     }
 }
 

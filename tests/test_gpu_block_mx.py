@@ -111,6 +111,21 @@ def test_products(size, dtype, out, with_bias):
     assert torch.equal(cb.mx_linear(x, w, None if bias is None else bias.cuda(), dtype=out), y)
 
 
+@pytest.mark.parametrize("size", [(9000, 2432, 4100), (4500, 288, 4100), (70000, 64, 50), (600, 1024, 2048), (1500, 2432, 2432), (1200, 352, 4096), (333, 2432, 7297)], ids=str)
+@pytest.mark.parametrize("out,with_bias", [(BF, True), (F32, False), (F32, True)])
+def test_many_tiles(size, out, with_bias):
+    # every tile shape, whole and ragged, one tile and several a workgroup; the sums in 64 bits on the GPU
+    M, C, F = size
+    x, w, bias = operands(M, C, F, BF)
+    t, bias = cb.mx_quantize(x), bias.cuda() if with_bias else None
+    values, wv = (ref.decoded(a.codes.cpu(), a.scales.cpu()).cuda() for a in (t, w))
+    y = cb.mx_linear(t, w, bias, dtype=out)
+    want, most = torch.matmul(values, wv.t().contiguous()), torch.matmul(values.abs(), wv.abs().t().contiguous())
+    if with_bias:
+        want, most = want + bias.double(), most + bias.double().abs()
+    ref.check(y, want, (C / 64 + 16) * 2 * ref.FP32 * most + ref.half_step(out) * want.abs(), "product")
+
+
 def test_one_element_at_a_time():
     """Rows of the unit matrix: every output is one weight, wherever it lies in the tile and the contraction."""
     C, F = 672, 300

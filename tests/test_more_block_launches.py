@@ -121,15 +121,16 @@ def linear(lib, tokens, channels, outputs, quantized):
     return launches(lib)
 
 
-LARGE, PAIR, DEEP = (4, 2, 2, 4, 2), (2, 2, 2, 2, 2), (2, 2, 2, 2, 4)
+LARGE, PAIR, DEEP, SMALL, FLAT = (4, 2, 2, 4, 2), (2, 2, 2, 2, 2), (2, 2, 2, 2, 4), (1, 2, 2, 1, 4), (1, 4, 2, 1, 3)
 
 
 @pytest.mark.parametrize("tokens,channels,outputs,want", [
     (1, 4096, 11264, [("mx_few_kernel", (1, 1, 8), 704)]), (4, 4096, 11264, [("mx_few_kernel", (1, 4, 8), 704)]), (5, 4096, 11264, ["quantize", ("mx_few_kernel", (1, 1, 8), 704)]),
     (1, 11264, 4096, [("mx_few_kernel", (1, 1, 16), 256)]), (3, 2304, 4096, [("mx_few_kernel", (1, 4, 16), 256)]), (1, 2048, 2048, [("mx_few_kernel", (1, 1, 8), 128)]),
-    (17, 4096, 4096, ["quantize", ("mx_few_kernel", (2, 1, 8), 256)]), (32, 4352, 3840, ["quantize", ("mx_few_kernel", (2, 1, 16), 240)]), (17, 4096, 11264, ["quantize", ("mx_tile_kernel", DEEP, 88), "join"]), (333, 2432, 7297, ["quantize", ("mx_tile_kernel", DEEP, 174)]),
-    (2000, 1536, 4096, ["quantize", ("mx_tile_kernel", PAIR, 512)]), (16717, 2432, 9728, ["quantize", ("mx_tile_kernel", LARGE, 256)]), (100, 9728, 2432, ["quantize", ("mx_tile_kernel", DEEP, 19), "join"]),
-    (2 ** 31 - 1, 32, 1, ["quantize"] * 2049 + [("mx_tile_kernel", PAIR, 512)]),
+    (17, 4096, 4096, ["quantize", ("mx_few_kernel", (2, 1, 8), 256)]), (32, 4352, 3840, ["quantize", ("mx_few_kernel", (2, 1, 16), 240)]), (17, 4096, 11264, ["quantize", ("mx_tile_kernel", SMALL, 176)]),
+    (77, 4096, 11264, ["quantize", ("mx_tile_kernel", FLAT, 176)]), (333, 2432, 7297, ["quantize", ("mx_tile_kernel", DEEP, 174)]), (64, 9728, 2432, ["quantize", ("mx_tile_kernel", SMALL, 38), "join"]),
+    (1000, 1536, 4096, ["quantize", ("mx_tile_kernel", DEEP, 256)]), (800, 4096, 6000, ["quantize", ("mx_tile_kernel", PAIR, 329)]), (16717, 2432, 9728, ["quantize", ("mx_tile_kernel", LARGE, 256)]),
+    (2 ** 31 - 1, 32, 1, ["quantize"] * 2049 + [("mx_tile_kernel", FLAT, 512)]),
 ])
 def test_forms_of_the_product(lib, tokens, channels, outputs, want):
     made = linear(lib, tokens, channels, outputs, False)
