@@ -665,7 +665,10 @@ def grad_norm(grads, norm_type=2.0, max_norm=None, grad_scale=None, stream=None)
 
 
 def clip_grads(grads, max_norm, norm_type=2.0, grad_scale=None, stream=None):
-    """clear_block_grad_clip: scales all gradients in place by grad_scale * min(1, max_norm / norm) and returns their norm, that of grad_scale times them (an fp32 scalar on their device)."""
+    """clear_block_grad_clip: scales all gradients in place by grad_scale * min(1, max_norm / norm) and returns their norm, that of grad_scale times them (an fp32 scalar on their device).
+    max_norm: a number >= 0."""
+    if max_norm is None:
+        _refuse("max_norm must be a number: gradients are not clipped without a bound")
     norm, _, have = _launch_norm("clear_block_grad_clip", grads, norm_type, max_norm, grad_scale, stream, False)
     _changed(have)
     return norm
