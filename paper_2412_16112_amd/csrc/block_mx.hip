@@ -539,10 +539,11 @@ __device__ __forceinline__ f32x4 few_product(i32x4 a, i32x4 b, f32x4 c, int scal
 // as many of the host's: one token at 4 096 x 11 264 10 us from Python, 15 with it.)
 constexpr int kDirect = 4;
 template <int N>
-struct DirectGroup {
-    unsigned short codes[N][64];  // (a lane's 4 codes)
+struct alignas(16) DirectGroup {
+    unsigned short codes[N][64];  // (a lane's 4 codes; read 16 bytes at a time, which alignment each of a wave's groups has: 144 bytes of one token, 544 of four)
     unsigned char scales[N][8];
 };
+static_assert(sizeof(DirectGroup<1>) % 16 == 0 && sizeof(DirectGroup<kDirect>) % 16 == 0);
 template <typename T>
 struct FourOf;
 template <>
@@ -588,7 +589,7 @@ __global__ void __launch_bounds__(64 * WAVES) mx_few_kernel(const TileArgs t)
     static_assert(!DIRECT || MT == 1);
     constexpr int AHEAD = 2;  // groups whose loads are in flight together
     __shared__ f32x4 part[WAVES][MT][64];
-    __shared__ __attribute__((aligned(16))) DirectGroup<N> direct[DIRECT ? WAVES : 1][DIRECT ? AHEAD : 1];
+    __shared__ DirectGroup<N> direct[DIRECT ? WAVES : 1][DIRECT ? AHEAD : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, block = 2 * (lane >> 4);
     const int f0 = blockIdx.x * 16;
     const int f = min(f0 + (lane & 15), t.rows_a - 1);
