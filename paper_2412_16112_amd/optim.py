@@ -60,7 +60,7 @@ class AdamW:
     def step(self, grads=None, grad_scale=None, stream=None, max_norm=None, **hyper):
         """One step with the parameters' .grad, or with `grads` (a list in their order); entries that are None are skipped: a parameter counts its own updates.  Keyword arguments
         (lr, ...) hold for this step only.  grad_scale: an fp32 device scalar that the gradients are multiplied by.  max_norm: with it, the gradients are scaled down to that norm of all of
-        them together (times grad_scale) where they have a larger one; `grad_norm` then is what they had, an fp32 scalar on the device.  The gradients themselves stay as they are."""
+        them together (times grad_scale) where they have a larger one; `grad_norm` then is what they had, an fp32 scalar on the device (0 where there is no gradient).  The gradients themselves stay as they are."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "one gradient for each parameter")
@@ -71,14 +71,19 @@ class AdamW:
                 raise ca.ClearAttnError(ca.CLEAR_ERR_MISMATCH, "a parameter has moved since the optimizer was made")
             cb._check_scale(grad_scale, params[0].device)
             given.append(cb._set_grads(table, params, [grads[i] for i in members]))
-        if max_norm is not None and any(g is not None for g in grads):
-            self.grad_norm, grad_scale = cb.grad_norm(grads, max_norm=max_norm, grad_scale=grad_scale, stream=stream)
+        norm = self.grad_norm
+        if max_norm is not None:
+            if any(g is not None for g in grads):
+                norm, grad_scale = cb.grad_norm(grads, max_norm=max_norm, grad_scale=grad_scale, stream=stream)
+            else:
+                norm = torch.zeros((), dtype=torch.float32, device=self.params[0].device) if self.params else None
         for (_, params, table, counts, masters), some in zip(self._tables, given):
             for n in sorted(set(counts)):  # (parameters that have had as many updates go together: all of them, unless gradients were missing; those without one are skipped)
                 rows = table if counts.count(n) == len(counts) else table[[c == n for c in counts]]
                 cb._launch(rows, params[0], self.state_bits == 8, n + 1, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], grad_scale, stream)
             counts[:] = [c + 1 for c in counts] if some is None else [c + (i in some) for i, c in enumerate(counts)]
             cb._updated(some, params, masters)
+        self.grad_norm = norm  # (not of a step that was refused)
 
     def state_dict(self):
         """What load_state_dict takes: the states themselves (not copies), the masters, each parameter's number of updates and the numbers of a step."""
