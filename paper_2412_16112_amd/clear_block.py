@@ -740,7 +740,8 @@ def _any_rows(t, name):
 
 
 def mx_quantize(x, stream=None):
-    """clear_block_mx_quantize: x [..., C] (bf16 or fp32, C a multiple of 32, rows evenly spaced) to 4 bits with a scale for every 32 channels of a row: an MX4."""
+    """clear_block_mx_quantize: x [..., C] (bf16 or fp32, C a multiple of 32, rows evenly spaced) to 4 bits with a scale for every 32 channels of a row: an MX4 (whole numbers: no gradient goes back
+    through them)."""
     dtype = _code(x)
     _on_device(x)
     rows, ld = _any_rows(x, "x")
@@ -763,11 +764,13 @@ def mx_dequantize(t, dtype=torch.bfloat16, stream=None):
 
 def mx_linear(x, w, bias=None, dtype=None, out=None, stream=None):
     """clear_block_mx_linear: x w^T + bias for w [F, C] in 4 bits (an MX4) and x [..., C]: an MX4, or bf16 or fp32, which the call takes to 4 bits first.  bias: [F], bf16 or fp32, or None.
-    Returns [..., F] of `dtype` (bf16 by default), or out.  No gradient goes through it."""
+    Returns [..., F] of `dtype` (bf16 by default), or out.  It has no backward pass: an x or a bias that requires a gradient is refused where gradients are on (torch.no_grad(), or detach())."""
     F, C, ld_w, ld_ws = _mx_operand(w, "w")
     if w[0].dim() != 2 or F < 1:
         _refuse("w must be [F, C], F >= 1")
     quantized = isinstance(x, tuple)
+    if torch.is_grad_enabled() and ((not quantized and x.requires_grad) or (bias is not None and bias.requires_grad)):
+        _refuse("no gradient goes through a 4-bit product: x and bias must not require one (torch.no_grad(), or detach())", CLEAR_ERR_UNSUPPORTED)
     if quantized:
         M, Cx, ld_x, ld_xs = _mx_operand(x, "x")
         lead, x_code, xp, xsp = x[0].shape[:-1], 0, x[0].data_ptr(), x[1].data_ptr()
