@@ -25,12 +25,12 @@ def _run(cmd):
 
 
 def build(verbose=False, extra_flags=()):
-    """Compile every source for gfx950, as many at a time as there are processors, and link the shared library.  Always recompiles."""
+    """Compile every source for gfx950, as many at a time as there are processors but at most 8, and link the shared library; extra_flags go to every command.  Always recompiles."""
     tmp = LIB + ".tmp%d" % os.getpid()
     with tempfile.TemporaryDirectory() as objects, concurrent.futures.ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
         paths = [os.path.join(objects, s + ".o") for s in SOURCES]
         cmds = [["hipcc", *FLAGS, *extra_flags, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, paths)]
-        link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *paths, "-o", tmp]
+        link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-Wno-unused-command-line-argument", *extra_flags, *paths, "-o", tmp]
         if verbose:
             print("\n".join(" ".join(c) for c in cmds + [link]), flush=True)
         for out in list(pool.map(_run, cmds)) + [_run(link)]:
