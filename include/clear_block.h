@@ -183,8 +183,8 @@ long long clear_block_residual_norm_workspace(long long groups, long long rows, 
  * Over n_tensors tensors together, of any types and sizes (data NULL or n = 0: not there):
  *     norm = |u| sqrt(sum g^2)  (CLEAR_GRAD_NORM_2)  or  |u| max |g|  (CLEAR_GRAD_NORM_MAX),   factor = u * min(1, max_norm / norm)
  * with u = *unscale, a device fp32 scalar (NULL: 1; the inverse of a loss's scale), to the device fp32 scalars norm and factor (either may be NULL; max_norm >= 0 counts for factor alone).
- * The factor is what clear_block_adamw takes as grad_scale, and clear_block_grad_scale.  Squares and sums are fp64: no gradient is too large or too small to be squared.  A NaN among the
- * gradients makes norm and factor NaN; an infinity makes norm infinite and factor 0.  workspace: clear_block_grad_norm_workspace bytes, 8-byte aligned.
+ * The factor is what clear_block_adamw takes as grad_scale, and clear_block_grad_scale.  Squares and sums are fp64: no gradient is too large or too small to be squared.  The factor is u where
+ * norm <= max_norm (both 0, or both infinite, too).  A NaN among the gradients makes norm and factor NaN; an infinity makes norm infinite and, with a finite max_norm, factor 0.  workspace: clear_block_grad_norm_workspace bytes, 8-byte aligned.
  * `tensors` is a HOST array, read before the call returns; a captured graph repeats its tensors.  n <= 2^35. */
 typedef enum {
     CLEAR_GRAD_NORM_2 = 0,

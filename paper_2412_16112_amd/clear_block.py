@@ -356,8 +356,8 @@ def residual_norm(x, y, gate=None, weight=None, bias=None, post_weight=None, kin
         r = residual_scale * x + gate * post(y) * (post_offset + post_weight),   h = norm(r) * (weight_offset + weight) + bias
 
     kind: the norm of r, post: the norm of y, "layer" or "rms" (post None: none).  gate, weight, bias: [C], or [B, C] for x [B, N, C], post_weight [C], of one dtype; each may be
-    None.  x (and r) and y (and h): bf16 or fp32, rows at any stride, not x in bf16 beside y in fp32.  out: (r, h) to write to; r may be x and h may be y.  Returns (r, h), or (r, h, stats)
-    with save_stats (for residual_norm_backward)."""
+    None.  x (and r) and y (and h): bf16 or fp32, rows at any stride, not x in bf16 beside y in fp32.  out: (r, h) to write to; r may be x and h may be y, else they must not share
+    memory with each other, an input or a vector.  Returns (r, h), or (r, h, stats) with save_stats (for residual_norm_backward)."""
     kind_code, post_code, dtype, stream_dtype, groups, rows, C = _residual_numbers(x, y, kind, post)
     gate_per_group, per_group, wcode = _residual_vectors(x, gate, weight, bias, post_weight, post)
     r, h = (_new_like(x), _new_like(y)) if out is None else out
@@ -659,14 +659,14 @@ def _launch_norm(name, grads, norm_type, max_norm, grad_scale, stream, factor):
 def grad_norm(grads, norm_type=2.0, max_norm=None, grad_scale=None, stream=None):
     """clear_block_grad_norm: the norm of all gradients together (a list of contiguous bf16 and fp32 tensors; None is skipped), as an fp32 scalar on their device: nothing waits for
     it.  norm_type: 2 or math.inf.  grad_scale: an fp32 device scalar that the gradients are multiplied by (the inverse of a loss's scale).  With max_norm: (norm, factor), the factor
-    grad_scale * min(1, max_norm / norm) being what adamw_step takes as its grad_scale."""
+    grad_scale * min(1, max_norm / norm) (grad_scale where norm <= max_norm, be it 0 or infinite) being what adamw_step takes as its grad_scale."""
     norm, factor, _ = _launch_norm("clear_block_grad_norm", grads, norm_type, max_norm, grad_scale, stream, max_norm is not None)
     return norm if max_norm is None else (norm, factor)
 
 
 def clip_grads(grads, max_norm, norm_type=2.0, grad_scale=None, stream=None):
     """clear_block_grad_clip: scales all gradients in place by grad_scale * min(1, max_norm / norm) and returns their norm, that of grad_scale times them (an fp32 scalar on their device).
-    max_norm: a number >= 0."""
+    max_norm: a number >= 0; with math.inf the gradients are scaled by grad_scale alone."""
     if max_norm is None:
         _refuse("max_norm must be a number: gradients are not clipped without a bound")
     norm, _, have = _launch_norm("clear_block_grad_clip", grads, norm_type, max_norm, grad_scale, stream, False)
