@@ -209,8 +209,9 @@ __device__ __forceinline__ void scale_all(const Launch& l, float factor)
         with_chunk(l, chunk, [&](auto* p, long long left, auto full) { scale_chunk<full>(p, left, factor); });
 }
 __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const Launch l, const float* factor) { scale_all(l, *factor); }
-// Clipping: every workgroup forms the factor for itself (of at most 8 KB of partials a launch), which a launch of its own and the wait for it would cost more than: 26 small tensors
-// 6.8 us, norm and scaling apart 12.4.
+// Clipping: every workgroup forms the factor for itself, which a launch of its own and the wait for it would cost more than: 26 small tensors 6.8 us, norm and scaling apart 12.4.  It reads all partials for that, at most 8 KB
+// for each launch of the norm (160 tensors), from the caches: work that grows with the square of the launches.  Tensors of 25 000 fp32, clipped, and norm and scaling apart: 160 11 us and 22, 1000 (7 launches) 89 and 115, 3000
+// (19 launches) 374 and 375.
 __global__ void __launch_bounds__(kThreads) grad_clip_kernel(const Launch l, const double* partials, long long n, GradFactor f, int gives)
 {
     scale_all(l, factor_of(partials, n, f, gives && blockIdx.x == 0));

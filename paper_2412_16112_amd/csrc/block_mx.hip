@@ -731,7 +731,8 @@ hipError_t launch_tiles(TileArgs t, int parts, hipStream_t stream)
 // Form, tile shape and number of parts that the contraction is split into, by the time that they are expected to take with weights from memory: where no CU has two tiles, a part's steps (256 of the
 // contraction) and what a tile costs beside; else rounds of as many tiles as the chip holds at once.  The constants, in us, were fitted to 3000 timings at 8 to 3000 tokens and eleven shapes of 608 x 3000 to
 // 4096 x 11264: the chosen form takes 0.5 % longer than the best of them on average, at most 11 %.  (77 tokens at 4096 x 11264: 64 x 64 12.5 us, 64 x 128 12.1, 128 x 128 14.3; at 4096 x 4096 8.2, 9.2 and 11.9; 333 at
-// 2432 x 7297 13.8, 12.6 and 11.7; 1000 at 2432 x 9728 39.9, 29.6 and 31.0, 256 x 256 25.6.)
+// 2432 x 7297 13.8, 12.6 and 11.7; 1000 at 2432 x 9728 39.9, 29.6 and 31.0, 256 x 256 25.6.)  One shape for the whole product: a last round of few tiles takes as long as a full one (tokens in 4 bits at 2432 x 9728: 1500
+// 25.7 us, 2000 37.3, 3000 48.8, 4608 71.4; at 4096 x 11264 1000 28.4, 1500, which are 264 tiles, 55.2, 2000 57.6).
 enum TileShape { kLarge, kPair, kDeep, kSmall, kFlat, kFew };  // kPair: two workgroups a CU, kDeep: one with four stages in flight
 struct Cost {
     int outputs, tokens;                 // of a tile
@@ -776,7 +777,7 @@ int parts_pitch(int outputs) { return (outputs + 3) / 4 * 4; }
 
 hipError_t launch_mx_quantize(const MxArgs& a, int dtype, hipStream_t stream)
 {
-    // (a launch has at most 65535 x 32 rows of a grid's second axis)
+    // (a launch has at most 65535 workgroups along its grid's second axis, of 8 kQuantRows rows each)
     constexpr long long each = 8 * kQuantRows, most = 65535 * each;
     for (long long first = 0; first < a.rows; first += most) {
         MxArgs b = a;

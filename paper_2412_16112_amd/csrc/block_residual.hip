@@ -6,7 +6,9 @@
 // memory, and the backward pass forms it again from x and y, which it reads in the place of r: as many bytes, and no rounding between the two.
 //
 // 2 x 4 608 x 2 432 bf16: forward 39 us (4.6 TB/s), backward 52 (5.2), 4.6 for the join of the sums; 16 896 x 4 096 bf16 with an fp32 stream and both norms 162 forward (5.1); 16 717 x 1 111 fp32 with both norms 62 and 91 (4.8 and
-// 4.9).  Beside the bytes, what counts is instructions: a choice for each element by what is absent (no gate, no post norm), and masks where a row is whole, cost the backward pass 10 to 18 %.
+// 4.9).  bf16 with an fp32 stream: 2 x 4 608 x 2 432 forward 49 us (5.4), backward with its sums 82 (4.9).  4 096 rows of 8 192: bf16 forward 56 (4.8), backward 92 (4.4), with a norm before too 83 (3.2) and 104 (3.9); with an
+// fp32 stream backward 127 (4.7), fp32 166 (4.8).  The widest rows have one team a workgroup, whose loads, barriers and stores follow each other: bf16 of 7 000 channels with both norms, the slowest, 79 forward (2.9) and
+// 96 backward (3.6).  Beside the bytes, what counts is instructions: a choice for each element by what is absent (no gate, no post norm), and masks where a row is whole, cost the backward pass 10 to 18 %.
 #include <algorithm>
 #include <type_traits>
 
@@ -463,7 +465,8 @@ hipError_t with_types(int dtype, int stream_dtype, int weight_dtype, F&& f)
 
 int residual_partials(long long groups, long long rows, int channels, long long sets)
 {
-    // 256 workgroups, one for each CU, or as many as there are rows for; the sets share them.
+    // 256 workgroups, one for each CU, or as many as there are rows for in bf16; the sets share them, rounded down.  (The workspace is asked for without a type.  With fp32 among the rows a workgroup has fewer teams, which
+    // take several rows one after the other where all would fit at once: 77 fp32 rows of 2 432 channels are 26 workgroups of three rows each.)
     const int team = team_of(channels);
     const long long teams = backward_waves(team, false) / team, in_set = sets > 1 || groups == 1 ? rows : groups * rows;
     if (in_set == 0 || sets == 0) return 0;
